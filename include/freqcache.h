@@ -19,6 +19,10 @@
  *                    the full cached K/V, O-projection and the SwiGLU MLP, and
  *                    scattered back into the token cache (Sec. 1, 2.2, 5.2).
  *
+ * Beside it, for what an episode keeps beyond the frame window and for the tokens of an
+ * answer: a token cache in 8 bits, written, attended to and cut down by fc_qcache_append,
+ * fc_qcache_attention and fc_qcache_evict.
+ *
  * Conventions for every call:
  *   - Pointers are DEVICE pointers unless marked (host).  The caller allocates
  *     and owns every buffer; the library never frees or keeps caller pointers
@@ -223,6 +227,43 @@ typedef struct {
   float rms_eps;            /* 1e-6 */
   const uint16_t *g, *w1, *b1, *w2, *b2;
 } fc_merger_desc;
+
+/* The 8-bit token cache: what an episode keeps of its past beyond the frame window, and
+ * what the tokens of an answer attend to.  Keys are held rotated, so rows may be dropped
+ * without moving the others' positions.  Numbers are e4m3 (OCP, 0x7f / 0xff NaN); a number
+ * stands for its code times the scale of its block of FC_QCACHE_BLOCK rows and key-value
+ * head.  Scales are powers of two, at least 2^-100.  Rows behind those held are never read
+ * for a result and may hold anything; every call leaves them as they are.  (host struct) */
+#define FC_QCACHE_BLOCK 64
+typedef struct {
+  uint8_t *k;               /* [B][n_kv][capacity][head_dim]                               */
+  uint8_t *v;               /* [B][n_kv][capacity / 64][head_dim][64]: by columns of a block */
+  float *k_scale, *v_scale; /* [B][n_kv][capacity / 64]                                    */
+  float *weight;            /* [B][n_kv][capacity] attention weight received so far, or NULL */
+  int32_t n_kv_heads;
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t capacity;         /* rows of each item and head; a multiple of 64, up to 2^30 */
+} fc_qcache;
+
+/* Rotary positions on up to three axes (time, row, column): the rotary pairs
+ * (i, i + head_dim / 2) are split into sections of section[0..2] pairs (sum head_dim / 2),
+ * pair i turned by pos[axis of its section] theta^(-2 i / head_dim).  All zero: one axis.
+ * (host struct) */
+typedef struct {
+  double theta;             /* > 1, e.g. 1e6 */
+  int32_t section[3];
+} fc_rope_axes;
+
+/* Rows of queries, keys and values of new tokens, e.g. the parts of one projection's rows:
+ * element (b, i, h, x) of q lies at q[b q_item + i q_row + h head_dim + x] (bf16, device;
+ * strides in elements, multiples of 8, not negative; pointers 16-byte aligned).
+ * q may be NULL (keys and values only).  (host struct) */
+typedef struct {
+  const uint16_t *q, *k, *v;
+  int64_t q_row, k_row, v_row;
+  int64_t q_item, k_item, v_item;
+  int32_t n_heads;          /* query heads, a multiple of the cache's n_kv_heads */
+} fc_qkv_rows;
 
 /* Library version string. */
 const char *fc_version(void);
@@ -448,6 +489,61 @@ fc_status fc_phase_correlate(fc_ctx *ctx, const float *frames_prev, const float 
 fc_status fc_phase_correlate_rotation(fc_ctx *ctx, const float *frames_prev,
                                       const float *frames_cur, int32_t B, int32_t H, int32_t W,
                                       double *angle, double *shift_px, void *stream);
+
+/* New rows into the 8-bit token cache: queries and keys rotated by their positions, keys and
+ * values quantised, for item b the rows len[b] .. len[b] + n_new[b] - 1.
+ *   pos:   [axes][B][n] int32 positions (axes: 3, or 1 when every section is 0);
+ *   len:   [B] int32 rows held before this call, the same for every layer's cache of a step
+ *          (no call advances it: the caller adds n_new after the step's last layer);
+ *   n_new: [B] int32 rows that item b brings, its first n_new[b] of the n; NULL: all n;
+ *   q_out: [B][n][n_heads][head_dim] bf16 rotated queries (NULL with q NULL); it may be q
+ *          itself in that layout, and overlaps no other input.  Rows from n_new[b] on are
+ *          left as they are.
+ * A block's scale is the smallest power of two s >= 2^-100 with all its new numbers within
+ * 448 s, and at least what it was if it held rows before (these are rounded again where it
+ * grows).  Numbers are rounded to nearest even from float32; an infinity is held as
+ * +-448 s, a NaN as a NaN, and neither sets the scale.  The new rows' weights are set to 0.
+ * Rows past the capacity are dropped.  Counts outside their ranges are clamped. */
+fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_axes *rope,
+                           const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
+                           const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
+                           void *stream);
+
+/* Attention of n tokens per item over the cache, their own rows (appended before) among it:
+ * token i of item b, i < n_new[b], attends to the rows j <= len[b] + i with key_mask[b][j]
+ * not 0.  One token or a whole prompt; the work is split over the keys where there are few
+ * rows.
+ *   q:        [B][n][n_heads][head_dim] bf16, rotated (q_out of the append);
+ *   len, n_new: as given to the append;
+ *   key_mask: [B][capacity] uint8 (16-byte aligned), or NULL: every row is seen;
+ *   out:      [B][n][n_heads][head_dim] bf16: softmax(scale q k) v; a token that sees no
+ *             row gets 0; tokens from n_new[b] on are left as they are;
+ *   scale:    usually 1 / sqrt(head_dim);
+ *   accumulate: 1: weight[b][h][j] += the sum of the probabilities that row j has received
+ *             from the tokens and the query heads of its group (cache->weight is needed).
+ * What is hidden from a token has no effect on it, whatever its bytes.  The partial results
+ * use the context's partial-sum workspace: fewer splits where it is small, and
+ * FC_ERR_CAPACITY when accumulate needs more rows than it holds (3 floats for each of the
+ * B n n_heads rows). */
+fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_t *q,
+                              const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
+                              uint16_t *out, int32_t n_heads, float scale, int32_t accumulate,
+                              int32_t B, int32_t n, void *stream);
+
+/* Eviction by the attention weight received: of each item's len[b] rows, head by head, the
+ * first n_sink, the last n_recent and, of those between, the keep - n_sink - n_recent of
+ * largest weight (equal weights: the lower row; -0 equals 0, a NaN counts as the lowest
+ * finite number) go into dst in their order, with their weights; every row when
+ * len[b] <= keep.  dst's blocks get the smallest scale for their rows.
+ *   src, dst: caches of the same heads and head_dim that share no memory (callers alternate
+ *             two caches, or pass one spare on from layer to layer); src->weight is needed,
+ *             dst->weight may be NULL; dst->capacity >= keep;
+ *   keep:     rows kept, >= n_sink + n_recent;
+ *   kept:     [B][n_kv][keep] int32 source rows, ascending, -1 behind the last;
+ *   len_out:  [B] int32 min(len[b], keep), or NULL; not len itself. */
+fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *dst,
+                          const int32_t *len, int32_t keep, int32_t n_sink, int32_t n_recent,
+                          int32_t *kept, int32_t *len_out, int32_t B, void *stream);
 
 /* Debug mode (process-wide): after every kernel launch the library waits for the
  * launch stream and reports an error raised while the kernel ran as FC_ERR_HIP from

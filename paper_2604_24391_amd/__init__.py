@@ -14,4 +14,5 @@ from .freqcache import (  # noqa: F401
     fc_select_carry, fc_vit_block_forward, fc_vit_cache_update, fc_vit_merger_forward,
     MergerDesc, VitCache, VitDesc,
     select_state_bytes, select_state_alloc, fc_slot_map_init, slot_state_alloc,
-    slot_state_bytes, fc_version, lib, token_grid)
+    slot_state_bytes, fc_version, lib, token_grid,
+    fc_qcache_append, fc_qcache_attention, fc_qcache_evict, QCACHE_BLOCK, QCache, RopeAxes)

@@ -1,6 +1,5 @@
 // C ABI of the FreqCache hot path: argument validation, context and workspace,
-// error reporting and event-based kernel timing.  The kernels live in select.hip
-// and layer.hip.
+// error reporting and event-based kernel timing.  The kernels live in the other files.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,6 +37,12 @@ fc_status fail(fc_status st, const char *fmt, ...) {
 static bool overlap(const void *a, const void *b, size_t n) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && x < y + n && y < x + n;
+}
+
+// The same for ranges of different lengths.
+static bool overlap2(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
 }
 
 // Debug mode: FC_DEBUG set to anything but "" or "0" when the library loads, or fc_debug.
@@ -183,6 +188,19 @@ fc_status use_device(fc_ctx *ctx) {
   if (e != hipSuccess) return fail(FC_ERR_HIP, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
   return FC_OK;
 }
+
+// The context's device for the length of a call, the caller's again after it.
+struct DeviceScope {
+  int prev = -1, dev;
+  fc_status st;
+  explicit DeviceScope(fc_ctx *ctx) : dev(ctx->device) {
+    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+    st = prev == dev ? FC_OK : use_device(ctx);
+  }
+  ~DeviceScope() {
+    if (prev >= 0 && prev != dev) hipSetDevice(prev);
+  }
+};
 
 // The pixel phase-correlation workspace, sized for the context's caps at its first use.
 fc_status ensure_pix(fc_ctx *ctx) {
@@ -710,6 +728,144 @@ fc_status fc_vit_merger_forward(fc_ctx *ctx, const fc_merger_desc *merger, const
   if (st != FC_OK) return st;
   return fc::launch_vit_merger(ctx, M, y, recompute_idx, n_recompute, x_out, n_tokens, B,
                                reinterpret_cast<hipStream_t>(stream));
+}
+
+static fc_status check_qcache(fc_ctx *ctx, const fc_qcache *c, int B, const char *who) {
+  if (!ctx) return fail(FC_ERR_INVALID_ARG, "%s: null context", who);
+  if (!c) return fail(FC_ERR_INVALID_ARG, "%s: null cache descriptor", who);
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale)
+    return fail(FC_ERR_INVALID_ARG, "%s: null cache buffer", who);
+  if (((uintptr_t)c->k | (uintptr_t)c->v) % 16)
+    return fail(FC_ERR_INVALID_ARG, "%s: the cache's k and v must be 16-byte aligned", who);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(FC_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128)", who, c->head_dim);
+  if (c->capacity < FC_QCACHE_BLOCK || c->capacity % FC_QCACHE_BLOCK || c->capacity > (1 << 30))
+    return fail(FC_ERR_SHAPE, "%s: capacity %d (a multiple of %d up to 2^30)", who, c->capacity,
+                FC_QCACHE_BLOCK);
+  if (B < 1 || c->n_kv_heads < 1 || (long)B * c->n_kv_heads > 65535)
+    return fail(FC_ERR_SHAPE, "%s: B=%d items of %d key-value heads (B n_kv from 1 to 65535)", who, B,
+                c->n_kv_heads);
+  return FC_OK;
+}
+
+static fc_status check_qrows(const fc_qcache &c, int n_heads, int B, int n, const char *who) {
+  if (n_heads < 1 || n_heads % c.n_kv_heads)
+    return fail(FC_ERR_SHAPE, "%s: n_kv_heads %d does not divide n_heads %d", who, c.n_kv_heads, n_heads);
+  if (n < 1 || n > c.capacity) return fail(FC_ERR_SHAPE, "%s: n=%d tokens, capacity %d", who, n, c.capacity);
+  if ((long)n * n_heads > (1L << 30))
+    return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens of %d heads (at most 2^30 rows an item)", who, n, n_heads);
+  return FC_OK;
+}
+
+fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_axes *rope,
+                           const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
+                           const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
+                           void *stream) {
+  const char *who = "fc_qcache_append";
+  fc_status st = check_qcache(ctx, cache, B, who);
+  if (st != FC_OK) return st;
+  const fc_qcache &c = *cache;
+  if (!rope || !rows || !rows->k || !rows->v || !pos || !len || (!rows->q) != (!q_out))
+    return fail(FC_ERR_INVALID_ARG, "%s: null rotary description, rows, positions or lengths, or only "
+                "one of q and q_out", who);
+  const fc_qkv_rows &x = *rows;
+  if ((st = check_qrows(c, x.n_heads, B, n, who)) != FC_OK) return st;
+  const int *sec = rope->section;
+  if (!(rope->theta > 1) || !std::isfinite(rope->theta))
+    return fail(FC_ERR_INVALID_ARG, "%s: theta must be above 1", who);
+  if ((sec[0] || sec[1] || sec[2]) &&
+      (sec[0] < 0 || sec[1] < 0 || sec[2] < 0 || (long)sec[0] + sec[1] + sec[2] != c.head_dim / 2))
+    return fail(FC_ERR_INVALID_ARG, "%s: rotary sections %d/%d/%d must sum to head_dim/2 = %d", who,
+                sec[0], sec[1], sec[2], c.head_dim / 2);
+  const uint16_t *in[3] = {x.q, x.k, x.v};
+  const int64_t row[3] = {x.q_row, x.k_row, x.v_row}, item[3] = {x.q_item, x.k_item, x.v_item};
+  const size_t qb = (size_t)B * n * x.n_heads * c.head_dim * 2;
+  if ((uintptr_t)q_out % 16) return fail(FC_ERR_INVALID_ARG, "%s: q_out must be 16-byte aligned", who);
+  for (int i = 0; i < 3; ++i) {
+    if (!in[i]) continue;
+    if ((uintptr_t)in[i] % 16 || row[i] < 0 || item[i] < 0 || row[i] % 8 || item[i] % 8 ||
+        row[i] > (1L << 40) || item[i] > (1L << 40))
+      return fail(FC_ERR_INVALID_ARG, "%s: q, k and v must be 16-byte aligned, with strides that are "
+                  "multiples of 8 elements and not negative", who);
+    const int width = (i ? c.n_kv_heads : x.n_heads) * c.head_dim;
+    const size_t bytes = ((size_t)(B - 1) * item[i] + (size_t)(n - 1) * row[i] + width) * 2;
+    const bool same = i == 0 && x.q == q_out && (n == 1 || row[0] == width) &&
+                      (B == 1 || item[0] == (int64_t)n * width);
+    if (!same && fc::overlap2(in[i], bytes, q_out, qb))
+      return fail(FC_ERR_INVALID_ARG, "%s: q_out overlaps an input (it may be q itself in the same "
+                  "layout)", who);
+  }
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_qcache_append(ctx, c, *rope, x, pos, len, n_new, q_out, B, n,
+                                  reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_t *q,
+                              const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
+                              uint16_t *out, int32_t n_heads, float scale, int32_t accumulate,
+                              int32_t B, int32_t n, void *stream) {
+  const char *who = "fc_qcache_attention";
+  fc_status st = check_qcache(ctx, cache, B, who);
+  if (st != FC_OK) return st;
+  const fc_qcache &c = *cache;
+  if (!q || !len || !out) return fail(FC_ERR_INVALID_ARG, "%s: null queries, lengths or output", who);
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)key_mask) % 16)
+    return fail(FC_ERR_INVALID_ARG, "%s: q, out and key_mask must be 16-byte aligned", who);
+  if ((st = check_qrows(c, n_heads, B, n, who)) != FC_OK) return st;
+  if (!std::isfinite(scale)) return fail(FC_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  if (accumulate != 0 && accumulate != 1)
+    return fail(FC_ERR_INVALID_ARG, "%s: accumulate %d (0 or 1)", who, accumulate);
+  if (accumulate && !c.weight)
+    return fail(FC_ERR_INVALID_ARG, "%s: accumulate needs the cache's weight buffer", who);
+  const size_t qb = (size_t)B * n * n_heads * c.head_dim * 2;
+  if (fc::overlap(q, out, qb)) return fail(FC_ERR_INVALID_ARG, "%s: q and out overlap", who);
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_qcache_attention(ctx, c, q, len, n_new, key_mask, out, n_heads, scale,
+                                     accumulate != 0, B, n, reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *dst,
+                          const int32_t *len, int32_t keep, int32_t n_sink, int32_t n_recent,
+                          int32_t *kept, int32_t *len_out, int32_t B, void *stream) {
+  const char *who = "fc_qcache_evict";
+  fc_status st = check_qcache(ctx, src, B, who);
+  if (st == FC_OK) st = check_qcache(ctx, dst, B, who);
+  if (st != FC_OK) return st;
+  if (!len || !kept || !src->weight)
+    return fail(FC_ERR_INVALID_ARG, "%s: null lengths, kept rows or source weights", who);
+  if (src->n_kv_heads != dst->n_kv_heads || src->head_dim != dst->head_dim)
+    return fail(FC_ERR_SHAPE, "%s: the caches' heads differ (%d x %d, %d x %d)", who, src->n_kv_heads,
+                src->head_dim, dst->n_kv_heads, dst->head_dim);
+  if (keep < 1 || n_sink < 0 || n_recent < 0 || (long)n_sink + n_recent > keep)
+    return fail(FC_ERR_INVALID_ARG, "%s: keep %d, n_sink %d, n_recent %d (keep >= 1 and >= their sum)",
+                who, keep, n_sink, n_recent);
+  if (keep > dst->capacity)
+    return fail(FC_ERR_SHAPE, "%s: keep %d above the destination's capacity %d", who, keep, dst->capacity);
+  // every buffer that is written against every other one
+  const size_t heads = (size_t)B * src->n_kv_heads;
+  auto parts = [&](const fc_qcache &c, const void **p, size_t *n) {
+    const size_t rows = heads * c.capacity, blocks = rows / FC_QCACHE_BLOCK * sizeof(float);
+    p[0] = c.k, p[1] = c.v, p[2] = c.k_scale, p[3] = c.v_scale, p[4] = c.weight;
+    n[0] = n[1] = rows * c.head_dim, n[2] = n[3] = blocks, n[4] = rows * sizeof(float);
+  };
+  const void *buf[13];
+  size_t bytes[13];
+  parts(*dst, buf, bytes);
+  buf[5] = kept, bytes[5] = heads * keep * sizeof(int32_t);
+  buf[6] = len_out, bytes[6] = B * sizeof(int32_t);
+  parts(*src, buf + 7, bytes + 7);
+  buf[12] = len, bytes[12] = B * sizeof(int32_t);
+  for (int i = 0; i < 7; ++i)
+    for (int j = i + 1; j < 13; ++j)
+      if (fc::overlap2(buf[i], bytes[i], buf[j], bytes[j]))
+        return fail(FC_ERR_INVALID_ARG, "%s: a buffer that is written overlaps another one (the two "
+                    "caches, kept, len and len_out must share no memory)", who);
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_qcache_evict(ctx, *src, *dst, len, keep, n_sink, n_recent, kept, len_out, B,
+                                 reinterpret_cast<hipStream_t>(stream));
 }
 
 size_t fc_slot_state_bytes(int32_t B, int32_t S) { return fc::slot_state_bytes(B, S); }

@@ -244,6 +244,18 @@ fc_status launch_cache_update_layers(fc_ctx *ctx, const fc_layer_desc &L, int n_
                                      uint16_t *const *y_cur, const int32_t *shift,
                                      const uint8_t *reuse, int grid_w, int B, hipStream_t st);
 
+// The 8-bit token cache (qcache.hip, qattn.hip).
+fc_status launch_qcache_append(fc_ctx *ctx, const fc_qcache &c, const fc_rope_axes &rope,
+                               const fc_qkv_rows &x, const int32_t *pos, const int32_t *len,
+                               const int32_t *n_new, uint16_t *q_out, int B, int n, hipStream_t st);
+fc_status launch_qcache_attention(fc_ctx *ctx, const fc_qcache &c, const uint16_t *q,
+                                  const int32_t *len, const int32_t *n_new,
+                                  const uint8_t *key_mask, uint16_t *out, int n_heads, float scale,
+                                  bool accumulate, int B, int n, hipStream_t st);
+fc_status launch_qcache_evict(fc_ctx *ctx, const fc_qcache &s, const fc_qcache &d, const int32_t *len,
+                              int keep, int sink, int recent, int32_t *kept, int32_t *len_out, int B,
+                              hipStream_t st);
+
 fc_status upload_select_tables();
 
 }  // namespace fc

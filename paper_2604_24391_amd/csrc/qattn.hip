@@ -1,0 +1,458 @@
+// Attention of new rows over the 8-bit token cache.
+//
+//   S_ij = c q_i . k_j over the rows j <= held + i that the key mask shows,
+//   P = softmax_j(S), out_i = sum_j P_ij v_j (a row that sees no key: 0),
+//   weight_j += sum over the rows i and the query heads of j's group of P_ij (on request).
+//
+// The G query heads of a group share their keys, so the n tokens of an item make R = n G rows
+// of a matrix product per key-value head: row r is head r % G of the group at token r / G.
+// S^T = K Q^T and O^T = V^T P^T: a lane then holds one query row, so the softmax's running
+// maximum and sum, and the rescaling of O, are per-lane scalars.  Both A operands are read as
+// the cache stores them (K by rows, V by columns of a block), each with 16-byte loads that
+// cover whole 64-byte pieces, and P is already in the layout of the second product's B operand:
+// the rows of an S^T tile are permuted so that a lane's 16 probabilities of a block belong to
+// 16 neighbouring keys.  e4m3 numbers are dequantised to bfloat16, which is exact, and the
+// products run on the bfloat16 matrix instructions: those of 8 bits align the products to the
+// largest before they add them (7e-6 of sum |q k| at worst on normal data; bfloat16 2e-8), which
+// the added-up weights, float32 numbers, would show.  P is rounded to bfloat16 for the second
+// product (half a step, 2^-8 of each term of a float32 sum whose terms err apart).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "fc_internal.h"
+#include "qcache.h"
+
+namespace fc {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNegInf = -__builtin_inff();
+
+struct QAttnArgs {
+  const uint8_t *k, *v;
+  const float *ks, *vs;
+  float *weight;
+  const uint16_t *q;
+  uint16_t *out;
+  const int32_t *len, *n_new;
+  const uint8_t *mask;               // [B][cap], or null
+  float2 *ml;                        // [splits][B KV][R] running maximum (log2) and sum
+  float *part;                       // [splits][B KV][R][hd] unnormalised outputs
+  float c;                           // scale log2(e)
+  int B, n, H, KV, G, cap, splits;
+};
+
+// Eight e4m3 codes (two words) times a power of two, as bfloat16 (exact).
+__device__ __forceinline__ bf16x8 dequant8(uint32_t w0, uint32_t w1, float s) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// Bytes of w that hold a NaN (0x7f or 0xff), as 0x01 each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
+}
+// Bytes of w that are not zero, as 0xff each.
+__device__ __forceinline__ uint32_t set_bytes(uint32_t w) {
+  return ((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) >> 7 & 0x01010101u) * 255u;
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// First and one-past-last key block of a split: the blocks of the rows' visible keys in equal parts.
+__device__ __forceinline__ void split_range(int blocks, int split, int splits, int &lo, int &hi) {
+  lo = (int)((long)blocks * split / splits);
+  hi = (int)((long)blocks * (split + 1) / splits);
+}
+
+// MT tiles of 16 rows against a run of key blocks; the 4 waves of a workgroup take blocks in
+// turn and their results are joined in LDS.  One split writes the outputs, several their parts.
+template <int HD, int MT>
+__global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
+  constexpr int KC = HD / 64;                   // 16-byte pieces of a key row that a lane holds
+  constexpr int DT = HD / 16;                   // output tiles of 16 dims
+  constexpr int OS = HD + 4;
+  __shared__ float sm_o[4][16][OS];
+  __shared__ float2 sm_ml[4][16 * MT];
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, split = blockIdx.x % a.splits;
+  const int r0 = blockIdx.x / a.splits * (16 * MT);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int rows = m * a.G, R = a.n * a.G;
+  if (r0 >= rows) return;
+  const int last = min(r0 + 16 * MT, rows) - 1;
+  const int kmax = held + last / a.G + 1;       // keys that any row sees
+  const int kall = held + r0 / a.G + 1;         // keys that every row sees, but for the mask
+  int blo, bhi;
+  split_range((kmax + kQBlock - 1) / kQBlock, split, a.splits, blo, bhi);
+
+  bf16x8 q[MT][2 * KC];
+  int seen[MT];                                 // keys that the lane's row sees
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int r = r0 + 16 * t + l16;
+    seen[t] = r < rows ? held + r / a.G + 1 : 0;
+    const int rc = min(r, rows - 1);
+    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+      q[t][2 * i] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16);
+      q[t][2 * i + 1] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16 + 8);
+    }
+  }
+  f32x4 o[MT][DT];
+  float mx[MT], sum[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    mx[t] = kNegInf, sum[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0, 0, 0, 0};
+  }
+  const long nblk = a.cap / kQBlock;
+  const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
+  const float *ksb = a.ks + hb * nblk, *vsb = a.vs + hb * nblk;
+
+  for (int blk = blo + wave; blk < bhi; blk += 4) {
+    const int j0 = blk * kQBlock;
+    u32x4 kw[4][KC], vw[DT];
+    // S^T row m of tile t is key (m / 4) 16 + 4 t + m % 4
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+        kw[t][i] = *reinterpret_cast<const u32x4 *>(
+            kbase + (long)(j0 + (l16 >> 2) * 16 + 4 * t + (l16 & 3)) * HD + 64 * i + g * 16);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      vw[d] = *reinterpret_cast<const u32x4 *>(vbase + (long)blk * (HD * kQBlock) + (16 * d + l16) * kQBlock + g * 16);
+    const float ks = ksb[blk], vs = vsb[blk];
+    const bool full = !a.mask && j0 + kQBlock <= kall;
+    uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};      // the lane's 16 keys that some row may see, by bytes
+    if (!full) {
+      if (a.mask) {
+        const u32x4 mw = *reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + g * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vis[i] = set_bytes(mw[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = kmax - (j0 + g * 16 + 4 * i);   // keys from this word on
+        vis[i] &= left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+      }
+    }
+    // what no row sees may hold anything, NaN among it, and 0 x NaN is NaN; a NaN that only later
+    // rows see is taken out too and added for them apart
+    bool odd = false;
+    if (!full) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vw[d][i] &= vis[i];
+          any |= nan_bytes(vw[d][i]);
+        }
+      odd = __any(any != 0);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      f32x4 s[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(kw[x][i][0], kw[x][i][1], ks), q[t][2 * i], s[x], 0, 0, 0);
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(kw[x][i][2], kw[x][i][3], ks), q[t][2 * i + 1], s[x], 0, 0, 0);
+        }
+      }
+      float top = kNegInf;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float y = s[x][e] * a.c;
+          if (!full) {
+            const int j = j0 + g * 16 + 4 * x + e;
+            y = (j < seen[t] && (vis[x] >> (8 * e) & 1u)) ? y : kNegInf;
+          }
+          s[x][e] = y;
+          top = fmaxf(top, y);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(mx[t], top);
+      const float ref = mn == kNegInf ? 0.f : mn;
+      const float corr = exp2_fast(mx[t] - ref);
+      mx[t] = mn;
+      float add = 0.f;
+      bf16x8 p[2];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = exp2_fast(s[x][e] - ref);
+          add += y;
+          p[x >> 1][(x & 1) * 4 + e] = (__bf16)y;
+        }
+      sum[t] = sum[t] * corr + add;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        o[t][d] *= corr;
+        if (!odd) {
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][0], vw[d][1], vs), p[0], o[t][d], 0, 0, 0);
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][2], vw[d][3], vs), p[1], o[t][d], 0, 0, 0);
+        } else {
+          // finite values as ever; a second product counts the NaN among the keys each row sees
+          uint32_t fin[4], bad[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t nb = nan_bytes(vw[d][i]);
+            fin[i] = vw[d][i] & ~(nb * 255u);
+            bad[i] = nb * 0x38u;                 // e4m3 1.0
+          }
+          bf16x8 one[2];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              one[x >> 1][(x & 1) * 4 + e] = (__bf16)(s[x][e] == kNegInf ? 0.f : 1.f);
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(fin[0], fin[1], vs), p[0], o[t][d], 0, 0, 0);
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(fin[2], fin[3], vs), p[1], o[t][d], 0, 0, 0);
+          f32x4 cn = {0, 0, 0, 0};
+          cn = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(bad[0], bad[1], 1.f), one[0], cn, 0, 0, 0);
+          cn = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(bad[2], bad[3], 1.f), one[1], cn, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][d][e] = cn[e] > 0.f ? __builtin_nanf("") : o[t][d][e];
+        }
+      }
+    }
+  }
+
+  // the four waves' parts of each row, joined; a lane's group g holds the sum over its own keys
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    float s = sum[t];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (g == 0) sm_ml[wave][16 * t + l16] = make_float2(mx[t], s);
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    __syncthreads();
+    const float2 w0 = sm_ml[0][16 * t + l16], w1 = sm_ml[1][16 * t + l16], w2 = sm_ml[2][16 * t + l16],
+                 w3 = sm_ml[3][16 * t + l16];
+    const float mt = fmaxf(fmaxf(w0.x, w1.x), fmaxf(w2.x, w3.x)), ref = mt == kNegInf ? 0.f : mt;
+    const float f = exp2_fast(mx[t] - ref);
+    const float l = w0.y * exp2_fast(w0.x - ref) + w1.y * exp2_fast(w1.x - ref) +
+                    w2.y * exp2_fast(w2.x - ref) + w3.y * exp2_fast(w3.x - ref);
+    // O^T: lane (g, l16) holds dims 16 d + 4 g + e of row l16
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sm_o[wave][l16][16 * d + 4 * g + e] = o[t][d][e] * f;
+    const int rt = r0 + 16 * t;
+    if (a.ml && wave == 0 && g == 0 && rt + l16 < rows)
+      a.ml[((long)split * a.B * a.KV + hb) * R + rt + l16] = make_float2(mt, l);
+    __syncthreads();
+    for (int x = tid; x < 16 * HD / 4; x += 256) {
+      const int row = x / (HD / 4), d = x % (HD / 4) * 4, r = rt + row;
+      if (r >= rows) continue;
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        y[e] = sm_o[0][row][d + e] + sm_o[1][row][d + e] + sm_o[2][row][d + e] + sm_o[3][row][d + e];
+      if (a.splits > 1) {
+        *reinterpret_cast<float4 *>(a.part + (((long)split * a.B * a.KV + hb) * R + r) * HD + d) =
+            make_float4(y[0], y[1], y[2], y[3]);
+      } else {
+        // row's own sum: recomputed from the shared parts
+        const float2 z0 = sm_ml[0][16 * t + row], z1 = sm_ml[1][16 * t + row], z2 = sm_ml[2][16 * t + row],
+                     z3 = sm_ml[3][16 * t + row];
+        const float zm = fmaxf(fmaxf(z0.x, z1.x), fmaxf(z2.x, z3.x)), zr = zm == kNegInf ? 0.f : zm;
+        const float zl = z0.y * exp2_fast(z0.x - zr) + z1.y * exp2_fast(z1.x - zr) +
+                         z2.y * exp2_fast(z2.x - zr) + z3.y * exp2_fast(z3.x - zr);
+        const float inv = zl == 0.f ? 0.f : 1.f / zl;
+        const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
+        *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
+      }
+    }
+  }
+}
+
+// The parts of one row joined: its splits' outputs weighted by 2^(m_s - m) and divided by the sum.
+template <int HD>
+__global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a) {
+  constexpr int TPR = HD / 4, RPW = 256 / TPR;
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int R = a.n * a.G, r = blockIdx.x * RPW + threadIdx.x / TPR, d = threadIdx.x % TPR * 4;
+  if (r >= m * a.G) return;
+  const long at = (long)hb * R + r, step = (long)a.B * a.KV * R;
+  float mt = kNegInf;
+  for (int s = 0; s < a.splits; ++s) mt = fmaxf(mt, a.ml[s * step + at].x);
+  const float ref = mt == kNegInf ? 0.f : mt;
+  float l = 0.f, y[4] = {0, 0, 0, 0};
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 z = a.ml[s * step + at];
+    if (z.x == kNegInf && z.y == 0.f) continue;  // saw no key: its part need not be written
+    const float f = exp2_fast(z.x - ref);
+    const float4 x = *reinterpret_cast<const float4 *>(a.part + (s * step + at) * HD + d);
+    l += z.y * f;
+    y[0] += x.x * f, y[1] += x.y * f, y[2] += x.z * f, y[3] += x.w * f;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
+  *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
+}
+
+// Each row's maximum and sum over its splits as one number, log2 of the sum of 2^S: the
+// probability of key j is 2^(S_j - L).  A row that sees no key gets +inf (every weight 0).
+__global__ __launch_bounds__(256) void k_qattn_lse(QAttnArgs a, float *lse) {
+  const int hb = blockIdx.y, R = a.n * a.G, r = blockIdx.x * 256 + threadIdx.x;
+  if (r >= R) return;
+  const int b = hb / a.KV, held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const long at = (long)hb * R + r, step = (long)a.B * a.KV * R;
+  float mt = kNegInf, l = 0.f;
+  if (r < m * a.G) {
+    for (int s = 0; s < a.splits; ++s) mt = fmaxf(mt, a.ml[s * step + at].x);
+    const float ref = mt == kNegInf ? 0.f : mt;
+    for (int s = 0; s < a.splits; ++s) {
+      const float2 z = a.ml[s * step + at];
+      l += z.y * exp2_fast(z.x - ref);
+    }
+    mt = ref;
+  }
+  lse[at] = l == 0.f ? __builtin_inff() : mt + __log2f(l);
+}
+
+// The weight that each key of one block receives: S^T again, rows in tiles of 16 over the waves.
+template <int HD>
+__global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a, const float *lse) {
+  constexpr int KC = HD / 64;
+  __shared__ float red[4][kQBlock];
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, blk = blockIdx.x, j0 = blk * kQBlock;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  if (m == 0 || j0 >= held + m) return;
+  const int rows = m * a.G, R = a.n * a.G;
+  const long nblk = a.cap / kQBlock;
+  const float ks = a.ks[hb * nblk + blk];
+  bf16x8 k[4][2 * KC];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+      const u32x4 w = *reinterpret_cast<const u32x4 *>(
+          a.k + ((long)hb * a.cap + j0 + (l16 >> 2) * 16 + 4 * t + (l16 & 3)) * HD + 64 * i + g * 16);
+      k[t][2 * i] = dequant8(w[0], w[1], ks);
+      k[t][2 * i + 1] = dequant8(w[2], w[3], ks);
+    }
+  uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
+  if (a.mask) {
+    const u32x4 mw = *reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + g * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vis[i] = set_bytes(mw[i]);
+  }
+  float acc[4][4] = {};
+  const int first = max(0, j0 - held) * a.G / 16 * 16;    // rows before see no key of the block
+  for (int rt = first + 16 * wave; rt < rows; rt += 64) {
+    const int r = rt + l16, rc = min(r, rows - 1);
+    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
+    bf16x8 q[2 * KC];
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+      q[2 * i] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16);
+      q[2 * i + 1] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16 + 8);
+    }
+    const float L = lse[(long)hb * R + rc];
+    const int seen = r < rows ? held + r / a.G + 1 : 0;
+    f32x4 s[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 2 * KC; ++i) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[x][i], q[i], s[x], 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = j0 + g * 16 + 4 * x + e;
+        const float p = exp2_fast(s[x][e] * a.c - L);
+        acc[x][e] += (j < seen && (vis[x] >> (8 * e) & 1u)) ? p : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float w = acc[x][e];
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) w += __shfl_xor(w, o);
+      if (l16 == 0) red[wave][g * 16 + 4 * x + e] = w;
+    }
+  __syncthreads();
+  if (tid < kQBlock && j0 + tid < held + m)
+    a.weight[(long)hb * a.cap + j0 + tid] += red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
+}
+
+template <int HD>
+fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
+  const long R = (long)a.n * a.G, pairs = (long)a.B * a.KV;
+  const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
+  const long tiles = (R + 16 * MT - 1) / (16 * MT);
+  // workgroups for four on every CU, as long as each split keeps four blocks (one per wave)
+  long splits = std::max<long>(1, (4L * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
+  splits = std::min<long>(splits, std::max(1, a.cap / kQBlock / 4));
+  const long per = pairs * R, lse_floats = weigh ? (per + 3) / 4 * 4 : 0;
+  const long ws = (long)ctx->part_elems - lse_floats;
+  splits = std::min<long>(splits, std::max<long>(1, ws / (per * (2 + HD))));
+  if (weigh && ws < 2 * per)
+    return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the row sums of %ld rows exceed the context's workspace", per);
+  a.splits = (int)splits;
+  float *lse = ctx->part;
+  float *base = ctx->part + lse_floats;
+  a.part = base;
+  a.ml = splits > 1 || weigh ? reinterpret_cast<float2 *>(base + (splits > 1 ? splits * per * HD : 0)) : nullptr;
+  const dim3 grid((unsigned)(tiles * splits), (unsigned)pairs);
+  {
+    ProfScope ps(ctx, st, "fc_qattn");
+    if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1>), grid, dim3(256), 0, st, a);
+    else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_qattn<HD, 4>), grid, dim3(256), 0, st, a);
+    FC_LAUNCH_OK(st, "k_qattn");
+  }
+  if (splits > 1) {
+    ProfScope ps(ctx, st, "fc_qattn_join");
+    hipLaunchKernelGGL(k_qattn_join<HD>, dim3((unsigned)((R + 1024 / HD - 1) / (1024 / HD)), (unsigned)pairs), dim3(256), 0, st, a);
+    FC_LAUNCH_OK(st, "k_qattn_join");
+  }
+  if (weigh) {
+    {
+      ProfScope ps(ctx, st, "fc_qattn_lse");
+      hipLaunchKernelGGL(k_qattn_lse, dim3((unsigned)((R + 255) / 256), (unsigned)pairs), dim3(256), 0, st, a, lse);
+      FC_LAUNCH_OK(st, "k_qattn_lse");
+    }
+    ProfScope ps(ctx, st, "fc_qattn_weight");
+    hipLaunchKernelGGL(k_qattn_weight<HD>, dim3((unsigned)(a.cap / kQBlock), (unsigned)pairs), dim3(256), 0, st, a, lse);
+    FC_LAUNCH_OK(st, "k_qattn_weight");
+  }
+  return FC_OK;
+}
+
+}  // namespace
+
+fc_status launch_qcache_attention(fc_ctx *ctx, const fc_qcache &c, const uint16_t *q,
+                                  const int32_t *len, const int32_t *n_new,
+                                  const uint8_t *key_mask, uint16_t *out, int n_heads, float scale,
+                                  bool accumulate, int B, int n, hipStream_t st) {
+  QAttnArgs a{};
+  a.k = c.k, a.v = c.v, a.ks = c.k_scale, a.vs = c.v_scale, a.weight = c.weight;
+  a.q = q, a.out = out, a.len = len, a.n_new = n_new, a.mask = key_mask;
+  a.c = scale * kLog2e;
+  a.B = B, a.n = n, a.H = n_heads, a.KV = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.cap = c.capacity;
+  return c.head_dim == 128 ? run_qattn<128>(ctx, a, accumulate, st) : run_qattn<64>(ctx, a, accumulate, st);
+}
+
+}  // namespace fc

@@ -36,7 +36,7 @@ EXPORTS = ("fc_version", "fc_last_error", "fc_create", "fc_destroy", "fc_select"
            "fc_cache_update_layers", "fc_cache_step", "fc_layer_forward", "fc_layer_forward_trail", "fc_debug",
            "fc_phase_correlate", "fc_phase_correlate_rotation", "fc_vit_block_forward",
            "fc_vit_cache_update", "fc_vit_merger_forward", "fc_slot_state_bytes",
-           "fc_slot_map_init",
+           "fc_slot_map_init", "fc_qcache_append", "fc_qcache_attention", "fc_qcache_evict",
            "fc_profile_enable", "fc_profile_only", "fc_profile_read")
 
 
@@ -101,6 +101,21 @@ class fc_vit_cache(ctypes.Structure):
                 ("v_prev", c_void_p)]
 
 
+class fc_qcache(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale", "weight")] + \
+        [("n_kv_heads", c_int32), ("head_dim", c_int32), ("capacity", c_int32)]
+
+
+class fc_rope_axes(ctypes.Structure):
+    _fields_ = [("theta", c_double), ("section", c_int32 * 3)]
+
+
+class fc_qkv_rows(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v")] + \
+        [(n, c_int64) for n in ("q_row", "k_row", "v_row", "q_item", "k_item", "v_item")] + \
+        [("n_heads", c_int32)]
+
+
 def lib() -> ctypes.CDLL:
     """Load libfreqcache.so (fails loudly when it has not been built)."""
     global _lib
@@ -157,6 +172,16 @@ def lib() -> ctypes.CDLL:
         L.fc_slot_state_bytes.restype = ctypes.c_size_t
         L.fc_slot_map_init.argtypes = [c_void_p, ctypes.POINTER(fc_layer_desc),
                                        ctypes.POINTER(fc_kv_cache), c_int32, c_void_p]
+        L.fc_qcache_append.argtypes = [c_void_p, ctypes.POINTER(fc_qcache),
+                                       ctypes.POINTER(fc_rope_axes), ctypes.POINTER(fc_qkv_rows),
+                                       c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                       c_void_p]
+        L.fc_qcache_attention.argtypes = [c_void_p, ctypes.POINTER(fc_qcache), c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_void_p, c_int32, c_float, c_int32,
+                                          c_int32, c_int32, c_void_p]
+        L.fc_qcache_evict.argtypes = [c_void_p, ctypes.POINTER(fc_qcache), ctypes.POINTER(fc_qcache),
+                                      c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                                      c_int32, c_void_p]
         L.fc_debug.argtypes = [c_int32]
         L.fc_debug.restype = c_int32
         L.fc_profile_enable.argtypes = [c_void_p, c_int32]
@@ -167,8 +192,8 @@ def lib() -> ctypes.CDLL:
                   "fc_cache_update", "fc_cache_update_layers", "fc_layer_forward",
                   "fc_layer_forward_trail", "fc_phase_correlate", "fc_phase_correlate_rotation",
                   "fc_vit_block_forward", "fc_vit_cache_update",
-                  "fc_slot_map_init",
-                  "fc_profile_enable",
+                  "fc_slot_map_init", "fc_qcache_append", "fc_qcache_attention",
+                  "fc_qcache_evict", "fc_profile_enable",
                   "fc_profile_only", "fc_profile_read"):
             getattr(L, n).restype = c_int32
         _lib = L
@@ -790,6 +815,199 @@ def fc_slot_map_init(ctx: Context, layer: LayerDesc, kv: KVCache, B: int, stream
     ck = kv.c(B, layer.n_kv_heads * layer.head_dim)
     _check(lib().fc_slot_map_init(ctx.handle, ctypes.byref(cl), ctypes.byref(ck), B,
                                   _stream(stream)))
+
+
+# ------------------------------------------------------------------------------ 8-bit token cache
+QCACHE_BLOCK = 64   # rows that share a scale
+
+
+@dataclass(frozen=True)
+class QCache:
+    """A token cache in 8 bits: e4m3 codes (uint8) and a power-of-two float32 scale for each
+    block of 64 rows and key-value head.
+
+    k [B, n_kv, capacity, head_dim]; v [B, n_kv, capacity / 64, head_dim, 64], each block by
+    columns; k_scale, v_scale [B, n_kv, capacity / 64]; weight [B, n_kv, capacity] float32
+    attention weight received, or None.  Keys are held rotated.  The number of rows held is
+    not part of it: one int32 tensor of lengths serves every layer's cache."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    weight: torch.Tensor | None = None
+
+    def __post_init__(self):
+        if self.k.dim() != 4:
+            raise ValueError("QCache: k must be [B, n_kv, capacity, head_dim]")
+        B, kv, cap, hd = self.k.shape
+        nb = cap // QCACHE_BLOCK
+        if cap % QCACHE_BLOCK or cap == 0:
+            raise ValueError(f"QCache: capacity {cap} must be a positive multiple of {QCACHE_BLOCK}")
+        for name, t, shape in (("v", self.v, (B, kv, nb, hd, QCACHE_BLOCK)),
+                               ("k_scale", self.k_scale, (B, kv, nb)),
+                               ("v_scale", self.v_scale, (B, kv, nb)),
+                               ("weight", self.weight, (B, kv, cap))):
+            if t is None and name == "weight":
+                continue
+            if tuple(t.shape) != shape:
+                raise ValueError(f"QCache: {name} is {tuple(t.shape)}, not {shape}")
+            if t.device != self.k.device:
+                raise ValueError(f"QCache: {name} is on {t.device}, k on {self.k.device}")
+        object.__setattr__(self, "_c", None)
+        self.c()
+
+    @staticmethod
+    def alloc(B: int, n_kv_heads: int, head_dim: int, capacity: int, device="cuda",
+              weight: bool = True) -> "QCache":
+        """An empty cache (capacity rounded up to whole blocks)."""
+        nb = -(-capacity // QCACHE_BLOCK)
+        kw = dict(device=device)
+        return QCache(torch.zeros(B, n_kv_heads, nb * QCACHE_BLOCK, head_dim, dtype=torch.uint8, **kw),
+                      torch.zeros(B, n_kv_heads, nb, head_dim, QCACHE_BLOCK, dtype=torch.uint8, **kw),
+                      torch.zeros(B, n_kv_heads, nb, **kw), torch.zeros(B, n_kv_heads, nb, **kw),
+                      torch.zeros(B, n_kv_heads, nb * QCACHE_BLOCK, **kw) if weight else None)
+
+    @property
+    def capacity(self) -> int:
+        return self.k.shape[2]
+
+    def c(self) -> fc_qcache:
+        """The C descriptor, made once and again if a tensor has got other memory."""
+        w = self.weight
+        p = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+             0 if w is None else w.data_ptr())
+        if self._c is None or self._c[0] != p:
+            B, kv, cap, hd = self.k.shape
+            n, blocks = B * kv * cap, B * kv * (cap // QCACHE_BLOCK)
+            for t, dtype, size, name in ((self.k, torch.uint8, n * hd, "k"), (self.v, torch.uint8, n * hd, "v"),
+                                         (self.k_scale, torch.float32, blocks, "k_scale"),
+                                         (self.v_scale, torch.float32, blocks, "v_scale"),
+                                         (w, torch.float32, n, "weight")):
+                if t is not None:
+                    _ptr(t, dtype, size, name)
+            object.__setattr__(self, "_c", (p, fc_qcache(*p, kv, hd, cap)))
+        return self._c[1]
+
+    def rows(self, values: bool = False) -> torch.Tensor:
+        """The keys (or values) that the codes stand for: [B, n_kv, capacity, head_dim] float32."""
+        t, s = (self.v.transpose(-1, -2), self.v_scale) if values else (self.k, self.k_scale)
+        x = t.contiguous().view(torch.float8_e4m3fn).float().view(*s.shape, QCACHE_BLOCK, -1)
+        return (x * s[..., None, None]).view(self.k.shape)
+
+
+@dataclass(frozen=True)
+class RopeAxes:
+    """Rotary positions: theta and the rotary pairs of each axis (time, row, column), which sum
+    to head_dim / 2; (0, 0, 0): one axis."""
+    theta: float = 1e6
+    section: tuple = (0, 0, 0)
+
+    def c(self) -> fc_rope_axes:
+        return fc_rope_axes(self.theta, (c_int32 * 3)(*self.section))
+
+    @property
+    def axes(self) -> int:
+        return 3 if any(self.section) else 1
+
+
+def _on(ctx: Context, *ts):
+    for t in ts:
+        if t is not None and t.get_device() != ctx.device:
+            raise ValueError(f"a tensor is on {t.device}, the context on GPU {ctx.device}")
+
+
+def _ctx_stream(ctx: Context, stream):
+    return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
+
+
+def _qrows(t: torch.Tensor, B: int, n: int, heads: int, hd: int, name: str):
+    """Pointer and strides of [B, n, heads, hd] rows whose heads lie side by side."""
+    if tuple(t.shape) != (B, n, heads, hd):
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {(B, n, heads, hd)}")
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a bfloat16 GPU tensor")
+    item, row, head, one = t.stride()
+    if (one != 1 and hd > 1) or (head != hd and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    # strides of axes of length 1 say nothing
+    return t.data_ptr(), (row if n > 1 else 0), (item if B > 1 else 0)
+
+
+def fc_qcache_append(ctx: Context, cache: QCache, rope: RopeAxes, q: torch.Tensor | None,
+                     k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, lens: torch.Tensor,
+                     n_new: torch.Tensor | None, q_out: torch.Tensor | None, stream=None):
+    """New rows into the cache behind the lens[b] held: k, v [B, n, n_kv, hd] and q
+    [B, n, n_heads, hd] bfloat16 (views of one projection's rows will do), pos int32 [3, B, n],
+    or [B, n] with one axis; item b brings its first n_new[b] tokens (None: all).  Rotated
+    queries go to q_out [B, n, n_heads, hd]; q and q_out may both be None.  lens is not
+    advanced: it serves every layer of the step."""
+    B, n = k.shape[:2]
+    Bc, kv, _, hd = cache.k.shape
+    if B != Bc:
+        raise ValueError(f"k has {B} items, the cache {Bc}")
+    if (q is None) != (q_out is None):
+        raise ValueError("give both q and q_out or neither")
+    heads = kv if q is None else q.shape[2]
+    pk, k_row, k_item = _qrows(k, B, n, kv, hd, "k")
+    pv, v_row, v_item = _qrows(v, B, n, kv, hd, "v")
+    pq, q_row, q_item = (0, 0, 0) if q is None else _qrows(q, B, n, heads, hd, "q")
+    _on(ctx, cache.k, q, k, v, pos, lens, n_new, q_out)
+    rows = fc_qkv_rows(pq, pk, pv, q_row, k_row, v_row, q_item, k_item, v_item, heads)
+    if pos.numel() != rope.axes * B * n:
+        raise ValueError(f"pos has {pos.numel()} positions, {rope.axes} axes of {B} x {n} tokens need {rope.axes * B * n}")
+    _check(lib().fc_qcache_append(
+        ctx.handle, ctypes.byref(cache.c()), ctypes.byref(rope.c()), ctypes.byref(rows),
+        _int32(pos, rope.axes * B * n, "pos"), _int32(lens, B, "lens"),
+        None if n_new is None else _int32(n_new, B, "n_new"),
+        None if q_out is None else _ptr(q_out, torch.bfloat16, B * n * heads * hd, "q_out"), B, n,
+        _ctx_stream(ctx, stream)))
+
+
+def _int32(t: torch.Tensor, numel: int, name: str):
+    """_ptr of int32 numbers, which need no more than their own alignment."""
+    if t is None or not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name} must be a contiguous int32 GPU tensor of at least {numel} elements")
+    return t.data_ptr()
+
+
+def fc_qcache_attention(ctx: Context, cache: QCache, q: torch.Tensor, lens: torch.Tensor,
+                        n_new: torch.Tensor | None, out: torch.Tensor,
+                        key_mask: torch.Tensor | None = None, scale: float | None = None,
+                        accumulate: bool = False, stream=None):
+    """Causal attention of the tokens just appended (q, out [B, n, n_heads, hd] bfloat16; lens and
+    n_new as given to fc_qcache_append) over the cache.  key_mask [B, capacity] uint8 or bool:
+    0 hides a row.  scale: 1 / sqrt(hd) by default.  accumulate adds the weight that each row
+    receives to cache.weight."""
+    Bc, kv, cap, hd = cache.k.shape
+    if q.dim() != 4 or q.shape[0] != Bc or q.shape[3] != hd:
+        raise ValueError(f"q is {tuple(q.shape)}, the cache has {Bc} items of head_dim {hd}")
+    B, n, heads, _ = q.shape
+    size = B * n * heads * hd
+    if key_mask is not None and key_mask.dtype == torch.bool:
+        key_mask = key_mask.view(torch.uint8)
+    _on(ctx, cache.k, q, lens, n_new, out, key_mask)
+    _check(lib().fc_qcache_attention(
+        ctx.handle, ctypes.byref(cache.c()), _ptr(q, torch.bfloat16, size, "q"), _int32(lens, B, "lens"),
+        None if n_new is None else _int32(n_new, B, "n_new"),
+        None if key_mask is None else _ptr(key_mask, torch.uint8, B * cap, "key_mask"),
+        _ptr(out, torch.bfloat16, size, "out"), heads, hd ** -0.5 if scale is None else scale,
+        int(accumulate), B, n, _ctx_stream(ctx, stream)))
+
+
+def fc_qcache_evict(ctx: Context, src: QCache, dst: QCache, lens: torch.Tensor, keep: int,
+                    sink: int, recent: int, kept: torch.Tensor, lens_out: torch.Tensor | None = None,
+                    stream=None):
+    """Of each item's lens[b] rows, head by head, the first `sink`, the last `recent` and those of
+    largest weight between, `keep` in all, into dst in their order; their numbers go to kept
+    [B, n_kv, keep] int32 (-1 behind the last), min(lens, keep) to lens_out."""
+    B, kv = src.k.shape[:2]
+    if dst.k.shape[0] != B:
+        raise ValueError(f"dst has {dst.k.shape[0]} items, src {B}")
+    _on(ctx, src.k, dst.k, lens, kept, lens_out)
+    _check(lib().fc_qcache_evict(
+        ctx.handle, ctypes.byref(src.c()), ctypes.byref(dst.c()), _int32(lens, B, "lens"), keep, sink,
+        recent, _int32(kept, B * kv * max(keep, 0), "kept"),
+        None if lens_out is None else _int32(lens_out, B, "lens_out"), B, _ctx_stream(ctx, stream)))
 
 
 # ------------------------------------------------------------------------------ timing
