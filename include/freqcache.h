@@ -523,7 +523,7 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  *             from the tokens and the query heads of its group (cache->weight is needed).
  * What is hidden from a token has no effect on it, whatever its bytes.  The partial results
  * use the context's partial-sum workspace: fewer splits where it is small, and
- * FC_ERR_CAPACITY when accumulate needs more rows than it holds (3 floats for each of the
+ * FC_ERR_CAPACITY when accumulate needs more rows than it holds (one float for each of the
  * B n n_heads rows). */
 fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_t *q,
                               const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,

@@ -39,8 +39,10 @@ struct QAttnArgs {
   const uint8_t *mask;               // [B][cap], or null
   float2 *ml;                        // [splits][B KV][R] running maximum (log2) and sum
   float *part;                       // [splits][B KV][R][hd] unnormalised outputs
+  float *lse;                        // [B KV][R] log2 of each row's sum, or null
+  float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
-  int B, n, H, KV, G, cap, splits;
+  int B, n, H, KV, G, cap, splits, tile_rows;
 };
 
 // Eight e4m3 codes (two words) times a power of two, as bfloat16 (exact).
@@ -61,11 +63,18 @@ __device__ __forceinline__ uint32_t set_bytes(uint32_t w) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// First and one-past-last key block of a split: the blocks of the rows' visible keys in equal parts.
-__device__ __forceinline__ void split_range(int blocks, int split, int splits, int &lo, int &hi) {
-  lo = (int)((long)blocks * split / splits);
-  hi = (int)((long)blocks * (split + 1) / splits);
+// Splits that the key blocks of one tile of rows are dealt over: lengths are known on the device
+// only, so the grid has room for `splits`, and a short item uses no more than leaves each of
+// them four blocks (one per wave).
+__device__ __forceinline__ int splits_used(int kmax, int splits) {
+  return max(1, min(splits, (kmax + 4 * kQBlock - 1) / (4 * kQBlock)));
 }
+// log2 of the sum of 2^S of a row from its maximum and sum: the probability of key j is 2^(S_j - L).
+// A row that sees no key gets +inf (every weight 0).
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.f ? __builtin_inff() : (m == kNegInf ? 0.f : m) + __log2f(l);
+}
+__device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 0.f : exp2_fast(y - L); }
 
 // MT tiles of 16 rows against a run of key blocks; the 4 waves of a workgroup take blocks in
 // turn and their results are joined in LDS.  One split writes the outputs, several their parts.
@@ -76,6 +85,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   constexpr int OS = HD + 4;
   __shared__ float sm_o[4][16][OS];
   __shared__ float2 sm_ml[4][16 * MT];
+  __shared__ float sm_l[16], sm_lse[16];
   const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, split = blockIdx.x % a.splits;
   const int r0 = blockIdx.x / a.splits * (16 * MT);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
@@ -85,8 +95,9 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   const int last = min(r0 + 16 * MT, rows) - 1;
   const int kmax = held + last / a.G + 1;       // keys that any row sees
   const int kall = held + r0 / a.G + 1;         // keys that every row sees, but for the mask
-  int blo, bhi;
-  split_range((kmax + kQBlock - 1) / kQBlock, split, a.splits, blo, bhi);
+  const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
+  if (split >= used) return;
+  const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
   bf16x8 q[MT][2 * KC];
   int seen[MT];                                 // keys that the lane's row sees
@@ -181,6 +192,11 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
           s[x][e] = y;
           top = fmaxf(top, y);
         }
+      if (MT == 1 && a.logit && seen[t]) {
+        float *to = a.logit + ((long)hb * R + r0 + 16 * t + l16) * a.cap + j0 + g * 16;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(to + 4 * x) = s[x];
+      }
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float mn = fmaxf(mx[t], top);
@@ -254,8 +270,12 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) sm_o[wave][l16][16 * d + 4 * g + e] = o[t][d][e] * f;
     const int rt = r0 + 16 * t;
-    if (a.ml && wave == 0 && g == 0 && rt + l16 < rows)
-      a.ml[((long)split * a.B * a.KV + hb) * R + rt + l16] = make_float2(mt, l);
+    if (wave == 0 && g == 0) {
+      if (a.ml && rt + l16 < rows) a.ml[((long)split * a.B * a.KV + hb) * R + rt + l16] = make_float2(mt, l);
+      if (a.lse && rt + l16 < rows) a.lse[(long)hb * R + rt + l16] = log_sum(mt, l);
+      sm_l[l16] = l;
+      sm_lse[l16] = log_sum(mt, l);
+    }
     __syncthreads();
     for (int x = tid; x < 16 * HD / 4; x += 256) {
       const int row = x / (HD / 4), d = x % (HD / 4) * 4, r = rt + row;
@@ -268,69 +288,122 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
         *reinterpret_cast<float4 *>(a.part + (((long)split * a.B * a.KV + hb) * R + r) * HD + d) =
             make_float4(y[0], y[1], y[2], y[3]);
       } else {
-        // row's own sum: recomputed from the shared parts
-        const float2 z0 = sm_ml[0][16 * t + row], z1 = sm_ml[1][16 * t + row], z2 = sm_ml[2][16 * t + row],
-                     z3 = sm_ml[3][16 * t + row];
-        const float zm = fmaxf(fmaxf(z0.x, z1.x), fmaxf(z2.x, z3.x)), zr = zm == kNegInf ? 0.f : zm;
-        const float zl = z0.y * exp2_fast(z0.x - zr) + z1.y * exp2_fast(z1.x - zr) +
-                         z2.y * exp2_fast(z2.x - zr) + z3.y * exp2_fast(z3.x - zr);
-        const float inv = zl == 0.f ? 0.f : 1.f / zl;
+        const float inv = sm_l[row] == 0.f ? 0.f : 1.f / sm_l[row];
         const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
         *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
       }
     }
   }
-}
-
-// The parts of one row joined: its splits' outputs weighted by 2^(m_s - m) and divided by the sum.
-template <int HD>
-__global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a) {
-  constexpr int TPR = HD / 4, RPW = 256 / TPR;
-  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV;
-  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  const int R = a.n * a.G, r = blockIdx.x * RPW + threadIdx.x / TPR, d = threadIdx.x % TPR * 4;
-  if (r >= m * a.G) return;
-  const long at = (long)hb * R + r, step = (long)a.B * a.KV * R;
-  float mt = kNegInf;
-  for (int s = 0; s < a.splits; ++s) mt = fmaxf(mt, a.ml[s * step + at].x);
-  const float ref = mt == kNegInf ? 0.f : mt;
-  float l = 0.f, y[4] = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 z = a.ml[s * step + at];
-    if (z.x == kNegInf && z.y == 0.f) continue;  // saw no key: its part need not be written
-    const float f = exp2_fast(z.x - ref);
-    const float4 x = *reinterpret_cast<const float4 *>(a.part + (s * step + at) * HD + d);
-    l += z.y * f;
-    y[0] += x.x * f, y[1] += x.y * f, y[2] += x.z * f, y[3] += x.w * f;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
-  *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
-}
-
-// Each row's maximum and sum over its splits as one number, log2 of the sum of 2^S: the
-// probability of key j is 2^(S_j - L).  A row that sees no key gets +inf (every weight 0).
-__global__ __launch_bounds__(256) void k_qattn_lse(QAttnArgs a, float *lse) {
-  const int hb = blockIdx.y, R = a.n * a.G, r = blockIdx.x * 256 + threadIdx.x;
-  if (r >= R) return;
-  const int b = hb / a.KV, held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  const long at = (long)hb * R + r, step = (long)a.B * a.KV * R;
-  float mt = kNegInf, l = 0.f;
-  if (r < m * a.G) {
-    for (int s = 0; s < a.splits; ++s) mt = fmaxf(mt, a.ml[s * step + at].x);
-    const float ref = mt == kNegInf ? 0.f : mt;
-    for (int s = 0; s < a.splits; ++s) {
-      const float2 z = a.ml[s * step + at];
-      l += z.y * exp2_fast(z.x - ref);
+  // one workgroup saw every key of these rows: their weights too (the scores it wrote above)
+  if (MT == 1 && a.logit && a.splits == 1) {
+    __threadfence();
+    __syncthreads();
+    for (int j = tid; j < kmax; j += 256) {
+      float w = 0.f;
+      for (int r = 0; r < rows; ++r) w += prob(a.logit[((long)hb * R + r) * a.cap + j], sm_lse[r]);
+      a.weight[(long)hb * a.cap + j] += w;
     }
-    mt = ref;
   }
-  lse[at] = l == 0.f ? __builtin_inff() : mt + __log2f(l);
+}
+
+// The splits of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
+// by the sum.  With scores written down (R <= 16 rows), further workgroups turn them into the
+// weight that each key receives: 4 R bytes a key written and read, against the 2 R hd multiplications
+// and the hd bytes of the keys that computing them again costs.
+constexpr int kWeightKeys = 1024;
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) {
+  constexpr int TPR = HD / 4, SG = 256 / TPR;
+  __shared__ float sm_y[SG][HD];
+  __shared__ float2 sm_ml[SG];
+  __shared__ float sm_lse[16];
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tid = threadIdx.x;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x;
+  const long step = (long)a.B * a.KV * R;
+  if (r < join_rows) {
+    if (r >= rows) return;
+    const int rt = r / a.tile_rows * a.tile_rows, last = min(rt + a.tile_rows, rows) - 1;
+    const int used = splits_used(held + last / a.G + 1, a.splits);
+    const int sg = tid / TPR, d = tid % TPR * 4;
+    const long at = (long)hb * R + r;
+    float mt = kNegInf, l = 0.f;
+    f32x4 y = {0, 0, 0, 0};
+    for (int s = sg; s < used; s += SG) {
+      const float2 z = a.ml[s * step + at];
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + (s * step + at) * HD + d);
+      const float mn = fmaxf(mt, z.x), ref = mn == kNegInf ? 0.f : mn;
+      const float f = exp2_fast(mt - ref), h = exp2_fast(z.x - ref);
+      mt = mn;
+      l = l * f + z.y * h;
+      y = y * f + x * h;
+    }
+    if (tid % TPR == 0) sm_ml[sg] = make_float2(mt, l);
+    __syncthreads();
+    float top = kNegInf;
+#pragma unroll
+    for (int i = 0; i < SG; ++i) top = fmaxf(top, sm_ml[i].x);
+    const float ref = top == kNegInf ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < SG; ++i) sum += sm_ml[i].y * exp2_fast(sm_ml[i].x - ref);
+    *reinterpret_cast<f32x4 *>(&sm_y[sg][d]) = y * exp2_fast(mt - ref);
+    __syncthreads();
+    if (tid < TPR) {
+      f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < SG; ++i) t += *reinterpret_cast<const f32x4 *>(&sm_y[i][d]);
+      t *= sum == 0.f ? 0.f : 1.f / sum;
+      const bf16x4 w = {(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
+      *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
+      if (a.lse && tid == 0) a.lse[at] = log_sum(top, sum);
+    }
+    return;
+  }
+  const int j0 = (r - join_rows) * kWeightKeys, seen = held + m;
+  if (m == 0 || j0 >= seen) return;
+  {
+    // 16 threads to a row
+    const int row = tid / 16, used = splits_used(seen, a.splits);
+    float mt = kNegInf, l = 0.f;
+    if (row < rows)
+      for (int s = tid % 16; s < used; s += 16) {
+        const float2 z = a.ml[s * step + (long)hb * R + row];
+        const float mn = fmaxf(mt, z.x), ref = mn == kNegInf ? 0.f : mn;
+        l = l * exp2_fast(mt - ref) + z.y * exp2_fast(z.x - ref);
+        mt = mn;
+      }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const float m2 = __shfl_xor(mt, o), l2 = __shfl_xor(l, o);
+      const float mn = fmaxf(mt, m2), ref = mn == kNegInf ? 0.f : mn;
+      l = l * exp2_fast(mt - ref) + l2 * exp2_fast(m2 - ref);
+      mt = mn;
+    }
+    if (tid % 16 == 0) sm_lse[row] = log_sum(mt, l);
+  }
+  __syncthreads();
+  const int j = j0 + 4 * tid;
+  if (j >= seen) return;
+  f32x4 w = {0, 0, 0, 0};
+  for (int i = 0; i < rows; ++i) {
+    const f32x4 y = *reinterpret_cast<const f32x4 *>(a.logit + ((long)hb * R + i) * a.cap + j);
+    const float L = sm_lse[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] += prob(y[e], L);
+  }
+  float *to = a.weight + (long)hb * a.cap + j;
+  if (j + 4 <= seen) {
+    *reinterpret_cast<f32x4 *>(to) += w;
+  } else {
+    for (int e = 0; e < seen - j; ++e) to[e] += w[e];
+  }
 }
 
 // The weight that each key of one block receives: S^T again, rows in tiles of 16 over the waves.
 template <int HD>
-__global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a, const float *lse) {
+__global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a) {
   constexpr int KC = HD / 64;
   __shared__ float red[4][kQBlock];
   const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, blk = blockIdx.x, j0 = blk * kQBlock;
@@ -367,7 +440,7 @@ __global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a, const float *
       q[2 * i] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16);
       q[2 * i + 1] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16 + 8);
     }
-    const float L = lse[(long)hb * R + rc];
+    const float L = a.lse[(long)hb * R + rc];
     const int seen = r < rows ? held + r / a.G + 1 : 0;
     f32x4 s[4];
 #pragma unroll
@@ -405,16 +478,25 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   // workgroups for four on every CU, as long as each split keeps four blocks (one per wave)
   long splits = std::max<long>(1, (4L * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
   splits = std::min<long>(splits, std::max(1, a.cap / kQBlock / 4));
-  const long per = pairs * R, lse_floats = weigh ? (per + 3) / 4 * 4 : 0;
-  const long ws = (long)ctx->part_elems - lse_floats;
-  splits = std::min<long>(splits, std::max<long>(1, ws / (per * (2 + HD))));
-  if (weigh && ws < 2 * per)
-    return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the row sums of %ld rows exceed the context's workspace", per);
+  const long per = pairs * R, ws = (long)ctx->part_elems;
+  auto up4 = [](long x) { return (x + 3) / 4 * 4; };
+  // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
+  // of at least two splits; else the weights compute them again from each row's sum
+  const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD <= ws;
+  const long side = !weigh ? 0 : logit ? per * a.cap : up4(per);
+  splits = std::max<long>(1, std::min<long>(splits, (ws - side) / (up4(2 * per) + per * HD)));
+  if (side > ws)
+    return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   a.splits = (int)splits;
-  float *lse = ctx->part;
-  float *base = ctx->part + lse_floats;
-  a.part = base;
-  a.ml = splits > 1 || weigh ? reinterpret_cast<float2 *>(base + (splits > 1 ? splits * per * HD : 0)) : nullptr;
+  a.tile_rows = 16 * MT;
+  float *at = ctx->part;
+  if (logit) a.logit = at;
+  else if (weigh) a.lse = at;
+  at += side;
+  if (splits > 1) {
+    a.part = at;
+    a.ml = reinterpret_cast<float2 *>(at + splits * per * HD);
+  }
   const dim3 grid((unsigned)(tiles * splits), (unsigned)pairs);
   {
     ProfScope ps(ctx, st, "fc_qattn");
@@ -425,17 +507,13 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   }
   if (splits > 1) {
     ProfScope ps(ctx, st, "fc_qattn_join");
-    hipLaunchKernelGGL(k_qattn_join<HD>, dim3((unsigned)((R + 1024 / HD - 1) / (1024 / HD)), (unsigned)pairs), dim3(256), 0, st, a);
+    const long more = logit ? (a.cap + kWeightKeys - 1) / kWeightKeys : 0;
+    hipLaunchKernelGGL(k_qattn_join<HD>, dim3((unsigned)(R + more), (unsigned)pairs), dim3(256), 0, st, a, (int)R);
     FC_LAUNCH_OK(st, "k_qattn_join");
   }
-  if (weigh) {
-    {
-      ProfScope ps(ctx, st, "fc_qattn_lse");
-      hipLaunchKernelGGL(k_qattn_lse, dim3((unsigned)((R + 255) / 256), (unsigned)pairs), dim3(256), 0, st, a, lse);
-      FC_LAUNCH_OK(st, "k_qattn_lse");
-    }
+  if (weigh && !logit) {
     ProfScope ps(ctx, st, "fc_qattn_weight");
-    hipLaunchKernelGGL(k_qattn_weight<HD>, dim3((unsigned)(a.cap / kQBlock), (unsigned)pairs), dim3(256), 0, st, a, lse);
+    hipLaunchKernelGGL(k_qattn_weight<HD>, dim3((unsigned)(a.cap / kQBlock), (unsigned)pairs), dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn_weight");
   }
   return FC_OK;

@@ -28,7 +28,7 @@ struct AppendArgs {
   uint8_t *kc, *vc;
   float *ks, *vs, *weight;
   int n, H, KV, cap, sec0, sec1;              // pairs below sec0 take axis 0, below sec1 axis 1
-  double turns[64];                           // theta^(-2 i / hd) / (2 pi): turns per position
+  double lo[8], hi[8];                        // lo[i % 8] hi[i / 8] = theta^(-2 i / hd) / (2 pi) turns
 };
 
 __device__ __forceinline__ float wave_max(float x) {
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kQThreads) void k_qappend(AppendArgs a) {
   for (int x = tid; x < cnt * HALF; x += kQThreads) {
     const int t = x / HALF, p = x % HALF;
     const long ax = p < a.sec0 ? 0 : (p < a.sec1 ? 1 : 2);
-    const double turn = (double)a.pos[ax * a.pos_axis + (long)b * a.n + i0 + t] * a.turns[p];
+    const double turn = (double)a.pos[ax * a.pos_axis + (long)b * a.n + i0 + t] * (a.lo[p & 7] * a.hi[p >> 3]);
     float s, c;
     sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
     cs[t][p] = make_float2(c, s);
@@ -409,8 +409,10 @@ fc_status launch_qcache_append(fc_ctx *ctx, const fc_qcache &c, const fc_rope_ax
   const bool one = !(rope.section[0] || rope.section[1] || rope.section[2]);
   a.sec0 = one ? half : rope.section[0];
   a.sec1 = one ? half : rope.section[0] + rope.section[1];
-  for (int i = 0; i < half; ++i)
-    a.turns[i] = std::pow(rope.theta, -2.0 * i / c.head_dim) / (2.0 * M_PI);
+  for (int i = 0; i < 8; ++i) {
+    a.lo[i] = std::pow(rope.theta, -2.0 * i / c.head_dim) / (2.0 * M_PI);
+    a.hi[i] = std::pow(rope.theta, -16.0 * i / c.head_dim);
+  }
   // the new rows start inside a block, so one more may be touched than they fill
   const dim3 grid((unsigned)((n + 2 * kQBlock - 2) / kQBlock), (unsigned)(B * c.n_kv_heads));
   ProfScope ps(ctx, st, "fc_qappend");

@@ -902,32 +902,52 @@ class RopeAxes:
     theta: float = 1e6
     section: tuple = (0, 0, 0)
 
+    def __post_init__(self):
+        object.__setattr__(self, "_c", fc_rope_axes(self.theta, (c_int32 * 3)(*self.section)))
+
     def c(self) -> fc_rope_axes:
-        return fc_rope_axes(self.theta, (c_int32 * 3)(*self.section))
+        return self._c
 
     @property
     def axes(self) -> int:
         return 3 if any(self.section) else 1
 
 
-def _on(ctx: Context, *ts):
-    for t in ts:
-        if t is not None and t.get_device() != ctx.device:
-            raise ValueError(f"a tensor is on {t.device}, the context on GPU {ctx.device}")
+def _arg(dev: int, t: torch.Tensor, dtype, numel: int, name: str, align: int = 16):
+    """Pointer of a contiguous tensor of at least numel elements on GPU `dev`."""
+    p = t.data_ptr()
+    if (t.get_device() == dev and t.dtype is dtype and t.is_contiguous() and t.numel() >= numel
+            and not p % align):
+        return p
+    if t.is_cuda and t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the context on GPU {dev}")
+    return _ptr(t, dtype, numel, name)
 
 
-def _ctx_stream(ctx: Context, stream):
-    return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
+def _ints(dev: int, t: torch.Tensor | None, numel: int, name: str):
+    """The same of int32 numbers, which need no more than their own alignment; None: null."""
+    if t is None:
+        return None
+    return _arg(dev, t, torch.int32, numel, name, 4)
 
 
-def _qrows(t: torch.Tensor, B: int, n: int, heads: int, hd: int, name: str):
+# torch's current stream as a number without a Stream object around it (1.2 us of a 3 us launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _dev_stream(dev: int, stream):
+    return _raw_stream(dev) if stream is None else _stream(stream)
+
+
+def _qrows(dev: int, t: torch.Tensor, B: int, n: int, heads: int, hd: int, name: str):
     """Pointer and strides of [B, n, heads, hd] rows whose heads lie side by side."""
-    if tuple(t.shape) != (B, n, heads, hd):
+    if t.shape != (B, n, heads, hd):
         raise ValueError(f"{name} is {tuple(t.shape)}, not {(B, n, heads, hd)}")
-    if not t.is_cuda or t.dtype != torch.bfloat16:
-        raise ValueError(f"{name} must be a bfloat16 GPU tensor")
+    if t.get_device() != dev or t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be a bfloat16 tensor on GPU {dev}")
     item, row, head, one = t.stride()
-    if (one != 1 and hd > 1) or (head != hd and heads > 1):
+    if one != 1 or (head != hd and heads > 1):
         raise ValueError(f"{name}: the heads of a token must lie side by side")
     # strides of axes of length 1 say nothing
     return t.data_ptr(), (row if n > 1 else 0), (item if B > 1 else 0)
@@ -941,33 +961,28 @@ def fc_qcache_append(ctx: Context, cache: QCache, rope: RopeAxes, q: torch.Tenso
     or [B, n] with one axis; item b brings its first n_new[b] tokens (None: all).  Rotated
     queries go to q_out [B, n, n_heads, hd]; q and q_out may both be None.  lens is not
     advanced: it serves every layer of the step."""
+    dev = ctx.device
     B, n = k.shape[:2]
     Bc, kv, _, hd = cache.k.shape
-    if B != Bc:
-        raise ValueError(f"k has {B} items, the cache {Bc}")
+    if B != Bc or cache.k.get_device() != dev:
+        raise ValueError(f"k has {B} items, the cache {Bc} on {cache.k.device}, the context is on GPU {dev}")
     if (q is None) != (q_out is None):
         raise ValueError("give both q and q_out or neither")
     heads = kv if q is None else q.shape[2]
-    pk, k_row, k_item = _qrows(k, B, n, kv, hd, "k")
-    pv, v_row, v_item = _qrows(v, B, n, kv, hd, "v")
-    pq, q_row, q_item = (0, 0, 0) if q is None else _qrows(q, B, n, heads, hd, "q")
-    _on(ctx, cache.k, q, k, v, pos, lens, n_new, q_out)
-    rows = fc_qkv_rows(pq, pk, pv, q_row, k_row, v_row, q_item, k_item, v_item, heads)
+    pk, k_row, k_item = _qrows(dev, k, B, n, kv, hd, "k")
+    pv, v_row, v_item = _qrows(dev, v, B, n, kv, hd, "v")
+    if q is None:
+        pq, q_row, q_item, po = None, 0, 0, None
+    else:
+        pq, q_row, q_item = _qrows(dev, q, B, n, heads, hd, "q")
+        po = _arg(dev, q_out, torch.bfloat16, B * n * heads * hd, "q_out")
     if pos.numel() != rope.axes * B * n:
         raise ValueError(f"pos has {pos.numel()} positions, {rope.axes} axes of {B} x {n} tokens need {rope.axes * B * n}")
     _check(lib().fc_qcache_append(
-        ctx.handle, ctypes.byref(cache.c()), ctypes.byref(rope.c()), ctypes.byref(rows),
-        _int32(pos, rope.axes * B * n, "pos"), _int32(lens, B, "lens"),
-        None if n_new is None else _int32(n_new, B, "n_new"),
-        None if q_out is None else _ptr(q_out, torch.bfloat16, B * n * heads * hd, "q_out"), B, n,
-        _ctx_stream(ctx, stream)))
-
-
-def _int32(t: torch.Tensor, numel: int, name: str):
-    """_ptr of int32 numbers, which need no more than their own alignment."""
-    if t is None or not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"{name} must be a contiguous int32 GPU tensor of at least {numel} elements")
-    return t.data_ptr()
+        ctx.handle, ctypes.byref(cache.c()), ctypes.byref(rope._c),
+        ctypes.byref(fc_qkv_rows(pq, pk, pv, q_row, k_row, v_row, q_item, k_item, v_item, heads)),
+        _ints(dev, pos, 1, "pos"), _ints(dev, lens, B, "lens"), _ints(dev, n_new, B, "n_new"), po, B, n,
+        _dev_stream(dev, stream)))
 
 
 def fc_qcache_attention(ctx: Context, cache: QCache, q: torch.Tensor, lens: torch.Tensor,
@@ -978,20 +993,22 @@ def fc_qcache_attention(ctx: Context, cache: QCache, q: torch.Tensor, lens: torc
     n_new as given to fc_qcache_append) over the cache.  key_mask [B, capacity] uint8 or bool:
     0 hides a row.  scale: 1 / sqrt(hd) by default.  accumulate adds the weight that each row
     receives to cache.weight."""
+    dev = ctx.device
     Bc, kv, cap, hd = cache.k.shape
     if q.dim() != 4 or q.shape[0] != Bc or q.shape[3] != hd:
         raise ValueError(f"q is {tuple(q.shape)}, the cache has {Bc} items of head_dim {hd}")
+    if cache.k.get_device() != dev:
+        raise ValueError(f"the cache is on {cache.k.device}, the context on GPU {dev}")
     B, n, heads, _ = q.shape
     size = B * n * heads * hd
-    if key_mask is not None and key_mask.dtype == torch.bool:
-        key_mask = key_mask.view(torch.uint8)
-    _on(ctx, cache.k, q, lens, n_new, out, key_mask)
+    if key_mask is not None:
+        if key_mask.dtype is torch.bool:
+            key_mask = key_mask.view(torch.uint8)
+        key_mask = _arg(dev, key_mask, torch.uint8, B * cap, "key_mask")
     _check(lib().fc_qcache_attention(
-        ctx.handle, ctypes.byref(cache.c()), _ptr(q, torch.bfloat16, size, "q"), _int32(lens, B, "lens"),
-        None if n_new is None else _int32(n_new, B, "n_new"),
-        None if key_mask is None else _ptr(key_mask, torch.uint8, B * cap, "key_mask"),
-        _ptr(out, torch.bfloat16, size, "out"), heads, hd ** -0.5 if scale is None else scale,
-        int(accumulate), B, n, _ctx_stream(ctx, stream)))
+        ctx.handle, ctypes.byref(cache.c()), _arg(dev, q, torch.bfloat16, size, "q"), _ints(dev, lens, B, "lens"),
+        _ints(dev, n_new, B, "n_new"), key_mask, _arg(dev, out, torch.bfloat16, size, "out"), heads,
+        hd ** -0.5 if scale is None else scale, 1 if accumulate else 0, B, n, _dev_stream(dev, stream)))
 
 
 def fc_qcache_evict(ctx: Context, src: QCache, dst: QCache, lens: torch.Tensor, keep: int,
@@ -1000,14 +1017,16 @@ def fc_qcache_evict(ctx: Context, src: QCache, dst: QCache, lens: torch.Tensor, 
     """Of each item's lens[b] rows, head by head, the first `sink`, the last `recent` and those of
     largest weight between, `keep` in all, into dst in their order; their numbers go to kept
     [B, n_kv, keep] int32 (-1 behind the last), min(lens, keep) to lens_out."""
+    dev = ctx.device
     B, kv = src.k.shape[:2]
     if dst.k.shape[0] != B:
         raise ValueError(f"dst has {dst.k.shape[0]} items, src {B}")
-    _on(ctx, src.k, dst.k, lens, kept, lens_out)
+    if src.k.get_device() != dev or dst.k.get_device() != dev:
+        raise ValueError(f"the caches are on {src.k.device} and {dst.k.device}, the context on GPU {dev}")
     _check(lib().fc_qcache_evict(
-        ctx.handle, ctypes.byref(src.c()), ctypes.byref(dst.c()), _int32(lens, B, "lens"), keep, sink,
-        recent, _int32(kept, B * kv * max(keep, 0), "kept"),
-        None if lens_out is None else _int32(lens_out, B, "lens_out"), B, _ctx_stream(ctx, stream)))
+        ctx.handle, ctypes.byref(src.c()), ctypes.byref(dst.c()), _ints(dev, lens, B, "lens"), keep, sink,
+        recent, _ints(dev, kept, B * kv * max(keep, 0), "kept"), _ints(dev, lens_out, B, "lens_out"), B,
+        _dev_stream(dev, stream)))
 
 
 # ------------------------------------------------------------------------------ timing

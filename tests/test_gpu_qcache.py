@@ -250,8 +250,9 @@ def test_attention_few_heads_in_a_small_workspace(fc):
     with fc.Context(fc.Caps(max_batch=1, max_height=28, max_width=28, max_tokens=4, max_seq=8, max_d_model=64, max_ffn=64, max_qkv=192)) as small:
         run_attention(fc, small, g, "toy", 1, 1, 2048, [1500], None)
         run_attention(fc, small, g, "toy", 1, 300, 512, [100], None, weight=False)
+        run_attention(fc, small, g, "qwen", 1, 300, 512, [100], None)      # the rows' sums fit
         with pytest.raises(fc.FcError) as e:
-            run_attention(fc, small, g, "qwen", 1, 300, 512, [100], None)
+            run_attention(fc, small, g, "qwen", 1, 600, 1024, [100], None)   # 16800 of them do not
         assert e.value.status == 3
 
 
