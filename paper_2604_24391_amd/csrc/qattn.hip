@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "fc_internal.h"
 #include "qcache.h"
@@ -43,6 +45,7 @@ struct QAttnArgs {
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, tile_rows;
+  uint32_t flip;                     // sign bits of a query pair to turn
 };
 
 // Eight e4m3 codes (two words) times a power of two, as bfloat16 (exact).
@@ -60,6 +63,13 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 // Bytes of w that are not zero, as 0xff each.
 __device__ __forceinline__ uint32_t set_bytes(uint32_t w) {
   return ((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) >> 7 & 0x01010101u) * 255u;
+}
+// Eight query elements, their signs turned where the scale is negative.
+__device__ __forceinline__ bf16x8 load_q(const uint16_t *src, uint32_t flip) {
+  u32x4 w = *reinterpret_cast<const u32x4 *>(src);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] ^= flip;
+  return __builtin_bit_cast(bf16x8, w);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -109,8 +119,8 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
-      q[t][2 * i] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16);
-      q[t][2 * i + 1] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16 + 8);
+      q[t][2 * i] = load_q(src + 64 * i + g * 16, a.flip);
+      q[t][2 * i + 1] = load_q(src + 64 * i + g * 16 + 8, a.flip);
     }
   }
   f32x4 o[MT][DT];
@@ -306,6 +316,238 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   }
 }
 
+// Many rows: 4 waves of 32 rows each share the key blocks, which the DMA brings into LDS three
+// deep (16 KB a block at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
+// back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
+// a lane holds one row and, of a block's keys, the 32 of its half wave.
+//
+// LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the lanes of a read fall on
+// different banks.
+template <int HD>
+__device__ __forceinline__ int key_swz(int row) {
+  return HD == 128 ? ((row >> 1) & 3) | ((row >> 5) << 2) : ((row >> 1) & 1) | ((row >> 5) << 1);
+}
+__device__ __forceinline__ int val_swz(int dim) { return (dim >> 1) & 3; }
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
+  constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
+  constexpr int DT = HD / 32;                   // output tiles of 32 dims
+  constexpr int TILE = kQBlock * HD;            // bytes of a block's keys, and of its values
+  constexpr int DMAS = TILE / 16 / 256;         // DMA instructions of a wave for either
+  constexpr int STAGES = 3;
+  __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
+  // pairs fastest: an XCD (workgroups go round the 8 in turn) keeps to few pairs' keys; the
+  // longest rows first
+  const int P = a.B * a.KV, R = a.n * a.G;
+  const int hb = blockIdx.x % P, rest = blockIdx.x / P, split = rest % a.splits;
+  const int r0 = ((R + 127) / 128 - 1 - rest / a.splits) * 128;
+  const int b = hb / a.KV, kv = hb % a.KV;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int rows = m * a.G;
+  if (r0 >= rows) return;
+  const int kmax = held + (min(r0 + 128, rows) - 1) / a.G + 1;
+  const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
+  if (split >= used) return;
+  const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
+
+  const long nblk = a.cap / kQBlock;
+  const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
+  const float *ksb = a.ks + hb * nblk, *vsb = a.vs + hb * nblk;
+  int ksrc[DMAS], vsrc[DMAS];
+#pragma unroll
+  for (int i = 0; i < DMAS; ++i) {
+    const int p = (wave * DMAS + i) * 64 + lane, kr = p / PC, vr = p / 4;
+    ksrc[i] = kr * HD + ((p % PC) ^ key_swz<HD>(kr)) * 16;
+    vsrc[i] = vr * kQBlock + ((p & 3) ^ val_swz(vr)) * 16;
+  }
+  auto fetch = [&](int blk, int stage) {
+    const long at = (long)blk * TILE;
+#pragma unroll
+    for (int i = 0; i < DMAS; ++i) dma16(kbase + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
+#pragma unroll
+    for (int i = 0; i < DMAS; ++i) dma16(vbase + at + vsrc[i], lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
+  };
+
+  const int w0 = r0 + 32 * wave, r = w0 + l32, rc = min(r, rows - 1);
+  const int seen = r < rows ? held + r / a.G + 1 : 0;                       // keys that the lane's row sees
+  const int wmax = w0 < rows ? held + (min(w0 + 32, rows) - 1) / a.G + 1 : 0;   // that any row of the wave sees
+  const int wall = held + w0 / a.G + 1;                                     // that every one does
+  bf16x8 q[HD / 16];
+  {
+    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) {
+      q[2 * i] = load_q(src + (2 * i + h) * 16, a.flip);
+      q[2 * i + 1] = load_q(src + (2 * i + h) * 16 + 8, a.flip);
+    }
+  }
+  loads_done();
+  fetch(blo, 0);
+  if (blo + 1 < bhi) fetch(blo + 1, 1);
+
+  // S^T row x of tile t is key ((x / 4) % 2) 32 + 16 t + x / 8 4 + x % 4
+  const int kr = ((l32 >> 2) & 1) * 32 + (l32 >> 3) * 4 + (l32 & 3);
+  const int koff = kr * HD, kx = key_swz<HD>(kr), voff = l32 * kQBlock, vx = val_swz(l32);
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
+
+  auto block = [&](auto full_tag, int blk, const uint8_t *kt, const uint8_t *vt) {
+    constexpr bool FULL = decltype(full_tag)::value;
+    const int j0 = blk * kQBlock;
+    const float ks = ksb[blk], vs = vsb[blk];
+    uint32_t vis[8];                 // the lane's 32 keys that some row may see, by bytes
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int left = wmax - (j0 + h * 32 + 4 * i);
+        vis[i] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+      }
+      if (a.mask) {
+        const u32x4 *mw = reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + h * 32);
+        const u32x4 m0 = mw[0], m1 = mw[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vis[i] &= set_bytes(m0[i]), vis[4 + i] &= set_bytes(m1[i]);
+      }
+    }
+    f32x16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(kt + koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16));
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
+      }
+    }
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + h * 32 + t * 16 + e;
+          if (!(j < seen && (vis[4 * t + e / 4] >> (8 * (e & 3)) & 1u))) s[t][e] = kNegInf;
+        }
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
+    // the reference follows the maximum only where it is 2^8 behind: no sum comes near
+    // float32's limits, and most blocks need not touch O
+    if (__any(top > ref + 8.f)) {
+      const float mn = fmaxf(ref, top), corr = exp2_fast(ref - (mn == kNegInf ? 0.f : mn));
+      ref = mn;
+      sum *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+    }
+    const float sub = ref == kNegInf ? 0.f : ref;
+    bf16x8 p[4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = exp2_fast(fmaf(s[t][e], a.c, -sub));
+        sum += y;
+        p[2 * t + e / 8][e % 8] = (__bf16)y;
+      }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      u32x4 w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
+      bool odd = false;
+      if constexpr (!FULL) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            w[i][x] &= vis[4 * i + x];
+            any |= nan_bytes(w[i][x]);
+          }
+        odd = __any(any != 0);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][0], w[i][1], vs), p[2 * i], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][2], w[i][3], vs), p[2 * i + 1], o[d], 0, 0, 0);
+        }
+      } else {
+        // as in k_qattn: finite values, then NaN for the rows that see one
+        f32x16 cn;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) cn[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t n0 = nan_bytes(w[i][2 * x]), n1 = nan_bytes(w[i][2 * x + 1]);
+            bf16x8 one;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) one[e] = (__bf16)(s[i][8 * x + e] == kNegInf ? 0.f : 1.f);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][2 * x] & ~(n0 * 255u), w[i][2 * x + 1] & ~(n1 * 255u), vs), p[2 * i + x], o[d], 0, 0, 0);
+            cn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(n0 * 0x38u, n1 * 0x38u, 1.f), one, cn, 0, 0, 0);
+          }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = cn[e] > 0.f ? __builtin_nanf("") : o[d][e];
+      }
+    }
+  };
+
+  int stage = 0;
+  for (int blk = blo; blk < bhi; ++blk) {
+    // this block's DMAs are done when at most the next one's are outstanding
+    if (blk + 1 < bhi) wait_vm<2 * DMAS>();
+    else wait_vm<0>();
+    lds_barrier();                   // and the other waves', and everyone has left the oldest stage
+    if (blk + 2 < bhi) fetch(blk + 2, stage == 0 ? 2 : stage - 1);
+    const int j0 = blk * kQBlock;
+    const uint8_t *kt = sm[stage][0], *vt = sm[stage][1];
+    if (j0 < wmax) {
+      if (!a.mask && j0 + kQBlock <= wall) block(std::true_type{}, blk, kt, vt);
+      else block(std::false_type{}, blk, kt, vt);
+    }
+    stage = stage == 2 ? 0 : stage + 1;
+  }
+
+  sum += __shfl_xor(sum, 32);
+  if (r >= rows) return;
+  const long at = (long)hb * R + r;
+  if (a.splits > 1) {
+    const long to = (long)split * P * R + at;
+    if (h == 0) a.ml[to] = make_float2(ref, sum);
+    float *dst = a.part + to * HD;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4 *>(dst + 32 * d + 8 * j + 4 * h) = make_float4(o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]);
+  } else {
+    if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t *dst = a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x4 w = {(__bf16)(o[d][4 * j] * inv), (__bf16)(o[d][4 * j + 1] * inv), (__bf16)(o[d][4 * j + 2] * inv), (__bf16)(o[d][4 * j + 3] * inv)};
+        *reinterpret_cast<bf16x4 *>(dst + 32 * d + 8 * j + 4 * h) = w;
+      }
+  }
+}
+
 // The splits of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
 // by the sum.  With scores written down (R <= 16 rows), further workgroups turn them into the
 // weight that each key receives: 4 R bytes a key written and read, against the 2 R hd multiplications
@@ -437,8 +679,8 @@ __global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a) {
     bf16x8 q[2 * KC];
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
-      q[2 * i] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16);
-      q[2 * i + 1] = *reinterpret_cast<const bf16x8 *>(src + 64 * i + g * 16 + 8);
+      q[2 * i] = load_q(src + 64 * i + g * 16, a.flip);
+      q[2 * i + 1] = load_q(src + 64 * i + g * 16 + 8, a.flip);
     }
     const float L = a.lse[(long)hb * R + rc];
     const int seen = r < rows ? held + r / a.G + 1 : 0;
@@ -473,10 +715,12 @@ __global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a) {
 template <int HD>
 fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const long R = (long)a.n * a.G, pairs = (long)a.B * a.KV;
-  const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
-  const long tiles = (R + 16 * MT - 1) / (16 * MT);
-  // workgroups for four on every CU, as long as each split keeps four blocks (one per wave)
-  long splits = std::max<long>(1, (4L * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
+  const bool many = R > 64;
+  const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4), tile = many ? 128 : 16 * MT;
+  const long tiles = (R + tile - 1) / tile;
+  // workgroups for four on every CU (of the many-row kernel: two), as long as each split keeps
+  // four blocks (one per wave)
+  long splits = std::max<long>(1, ((many ? 2L : 4L) * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
   splits = std::min<long>(splits, std::max(1, a.cap / kQBlock / 4));
   const long per = pairs * R, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
@@ -488,7 +732,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   a.splits = (int)splits;
-  a.tile_rows = 16 * MT;
+  a.tile_rows = tile;
   float *at = ctx->part;
   if (logit) a.logit = at;
   else if (weigh) a.lse = at;
@@ -497,8 +741,14 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     a.part = at;
     a.ml = reinterpret_cast<float2 *>(at + splits * per * HD);
   }
-  const dim3 grid((unsigned)(tiles * splits), (unsigned)pairs);
-  {
+  if (many) {
+    if (pairs * tiles * splits > (1L << 24) - 1)
+      return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
+    ProfScope ps(ctx, st, "fc_qattn_rows");
+    hipLaunchKernelGGL(k_qattn_rows<HD>, dim3((unsigned)(pairs * tiles * splits)), dim3(256), 0, st, a);
+    FC_LAUNCH_OK(st, "k_qattn_rows");
+  } else {
+    const dim3 grid((unsigned)(tiles * splits), (unsigned)pairs);
     ProfScope ps(ctx, st, "fc_qattn");
     if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1>), grid, dim3(256), 0, st, a);
     else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2>), grid, dim3(256), 0, st, a);
@@ -528,7 +778,10 @@ fc_status launch_qcache_attention(fc_ctx *ctx, const fc_qcache &c, const uint16_
   QAttnArgs a{};
   a.k = c.k, a.v = c.v, a.ks = c.k_scale, a.vs = c.v_scale, a.weight = c.weight;
   a.q = q, a.out = out, a.len = len, a.n_new = n_new, a.mask = key_mask;
-  a.c = scale * kLog2e;
+  // a negative scale turns the queries' signs instead; scale 0: a number that leaves scores of any
+  // ordinary size at 0 and hidden ones at -inf
+  a.c = std::max(std::fabs(scale) * kLog2e, 1.2e-38f);
+  a.flip = scale < 0.f ? 0x80008000u : 0u;
   a.B = B, a.n = n, a.H = n_heads, a.KV = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.cap = c.capacity;
   return c.head_dim == 128 ? run_qattn<128>(ctx, a, accumulate, st) : run_qattn<64>(ctx, a, accumulate, st);
 }
