@@ -321,13 +321,13 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 // back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
 // a lane holds one row and, of a block's keys, the 32 of its half wave.
 //
-// LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the lanes of a read fall on
-// different banks.
+// LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
+// together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks.
 template <int HD>
 __device__ __forceinline__ int key_swz(int row) {
-  return HD == 128 ? ((row >> 1) & 3) | ((row >> 5) << 2) : ((row >> 1) & 1) | ((row >> 5) << 1);
+  return HD == 128 ? ((row >> 1) & 3) | ((row >> 5) << 2) : (row >> 2) & 3;
 }
-__device__ __forceinline__ int val_swz(int dim) { return (dim >> 1) & 3; }
+__device__ __forceinline__ int val_swz(int dim) { return (dim >> 2) & 3; }
 
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
@@ -643,73 +643,136 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   }
 }
 
-// The weight that each key of one block receives: S^T again, rows in tiles of 16 over the waves.
+// The weight that each key receives, from scores computed again: 4 waves hold 64 keys each in
+// registers, as bfloat16, and the rows' queries pass by in tiles of 32 through LDS.  S^T puts the
+// keys in a lane's registers, so its sums over rows stay there until the end.  One exponential
+// for every two matrix cycles: the vector unit bounds it.  Row ranges are dealt over
+// `row_splits` workgroups, whose sums the next kernel adds up in order.
+constexpr int kWaveKeys = 64, kGroupKeys = 4 * kWaveKeys;
+
 template <int HD>
-__global__ __launch_bounds__(256) void k_qattn_weight(QAttnArgs a) {
-  constexpr int KC = HD / 64;
-  __shared__ float red[4][kQBlock];
-  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, blk = blockIdx.x, j0 = blk * kQBlock;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+__global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpart, int row_splits) {
+  constexpr int PC = HD / 8;                    // 16-byte pieces of a query row
+  constexpr int TILE = 32 * HD * 2, DMAS = TILE / 16 / 256;
+  __shared__ __align__(1024) uint8_t sm[3][TILE];
+  const int P = a.B * a.KV, R = a.n * a.G;
+  const int hb = blockIdx.x % P, rest = blockIdx.x / P, rs = rest % row_splits, j0 = rest / row_splits * kGroupKeys;
+  const int b = hb / a.KV, kv = hb % a.KV;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  if (m == 0 || j0 >= held + m) return;
-  const int rows = m * a.G, R = a.n * a.G;
-  const long nblk = a.cap / kQBlock;
-  const float ks = a.ks[hb * nblk + blk];
-  bf16x8 k[4][2 * KC];
+  const int rows = m * a.G, seen = held + m;
+  if (m == 0 || j0 >= seen) return;
+  // row tiles that see a key of the group, and this workgroup's part of them
+  const int t0 = (int)((long)max(0, j0 - held) * a.G / 32), t1 = (rows + 31) / 32;
+  const int lo = t0 + (int)((long)(t1 - t0) * rs / row_splits), hi = t0 + (int)((long)(t1 - t0) * (rs + 1) / row_splits);
+
+  const int w0 = j0 + kWaveKeys * wave, blk = min(w0, a.cap - kQBlock) / kQBlock;
+  const float ks = a.ks[hb * (long)(a.cap / kQBlock) + blk];
+  bf16x8 k[2][HD / 16];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < KC; ++i) {
+    for (int i = 0; i < HD / 32; ++i) {
+      // S^T row x of tile t is key 32 t + x
       const u32x4 w = *reinterpret_cast<const u32x4 *>(
-          a.k + ((long)hb * a.cap + j0 + (l16 >> 2) * 16 + 4 * t + (l16 & 3)) * HD + 64 * i + g * 16);
+          a.k + ((long)hb * a.cap + (long)blk * kQBlock + 32 * t + l32) * HD + (2 * i + h) * 16);
       k[t][2 * i] = dequant8(w[0], w[1], ks);
       k[t][2 * i + 1] = dequant8(w[2], w[3], ks);
     }
-  uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
-  if (a.mask) {
-    const u32x4 mw = *reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + g * 16);
+  const uint16_t *qb = a.q + ((long)b * a.n * a.H + kv * a.G) * HD;
+  auto fetch = [&](int tile, int stage) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vis[i] = set_bytes(mw[i]);
-  }
-  float acc[4][4] = {};
-  const int first = max(0, j0 - held) * a.G / 16 * 16;    // rows before see no key of the block
-  for (int rt = first + 16 * wave; rt < rows; rt += 64) {
-    const int r = rt + l16, rc = min(r, rows - 1);
-    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
-    bf16x8 q[2 * KC];
-#pragma unroll
-    for (int i = 0; i < KC; ++i) {
-      q[2 * i] = load_q(src + 64 * i + g * 16, a.flip);
-      q[2 * i + 1] = load_q(src + 64 * i + g * 16 + 8, a.flip);
+    for (int i = 0; i < DMAS; ++i) {
+      const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(tile * 32 + row, rows - 1);
+      const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
+      dma16(qb + ((long)(r / a.G) * a.H + r % a.G) * HD + piece * 8, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
     }
-    const float L = a.lse[(long)hb * R + rc];
-    const int seen = r < rows ? held + r / a.G + 1 : 0;
-    f32x4 s[4];
+  };
+  auto load_l = [&](int tile) {
+    const int r = tile * 32 + l32;
+    return r < rows ? a.lse[(long)hb * R + r] : __builtin_inff();
+  };
+  f32x16 acc[2];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      s[x] = f32x4{0, 0, 0, 0};
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 2 * KC; ++i) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[x][i], q[i], s[x], 0, 0, 0);
+    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+  loads_done();
+  float next = 0.f;
+  if (lo < hi) {
+    next = load_l(lo);
+    fetch(lo, 0);
+    if (lo + 1 < hi) fetch(lo + 1, 1);
+  }
+  const int qx = HD == 128 ? l32 & 15 : (l32 >> 1) & 7;
+  int stage = 0;
+  for (int tile = lo; tile < hi; ++tile) {
+    if (tile + 1 < hi) wait_vm<DMAS>();
+    else wait_vm<0>();
+    lds_barrier();
+    const float L = next;
+    if (tile + 1 < hi) next = load_l(tile + 1);
+    if (tile + 2 < hi) fetch(tile + 2, stage == 0 ? 2 : stage - 1);
+    const uint8_t *qt = sm[stage] + l32 * HD * 2;
+    stage = stage == 2 ? 0 : stage + 1;
+    const int r = tile * 32 + l32;
+    if (w0 >= held + min(tile * 32 + 31, rows - 1) / a.G + 1) continue;      // the last row sees none
+    f32x16 s[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = j0 + g * 16 + 4 * x + e;
-        const float p = exp2_fast(s[x][e] * a.c - L);
-        acc[x][e] += (j < seen && (vis[x] >> (8 * e) & 1u)) ? p : 0.f;
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        // piece of 8 elements: dims (2 i + h) 16 + 8 x
+        const bf16x8 q = load_q(reinterpret_cast<const uint16_t *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16), a.flip);
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][2 * i + x], q, s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][2 * i + x], q, s[1], 0, 0, 0);
+      }
+    if (tile * 32 + 32 <= rows && w0 + kWaveKeys <= held + tile * 32 / a.G + 1) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], a.c, -L));
+    } else {
+      const int see = r < rows ? held + r / a.G + 1 : 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = exp2_fast(fmaf(s[t][e], a.c, -L));
+          acc[t][e] += w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4 < see ? p : 0.f;
+        }
+    }
+  }
+  // over the 32 rows of a half wave: each step halves the registers that a lane still sums
+  const long out = (long)hb * a.cap;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float w = acc[t][e];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) w += __shfl_xor(w, o);
+      const int j = w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4;
+      if (l32 == 0 && j < seen) {
+        if (a.mask && !a.mask[(long)b * a.cap + j]) w = 0.f;
+        if (wpart) wpart[(long)rs * P * a.cap + out + j] = w;
+        else a.weight[out + j] += w;
       }
     }
-  }
-#pragma unroll
-  for (int x = 0; x < 4; ++x)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float w = acc[x][e];
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) w += __shfl_xor(w, o);
-      if (l16 == 0) red[wave][g * 16 + 4 * x + e] = w;
-    }
-  __syncthreads();
-  if (tid < kQBlock && j0 + tid < held + m)
-    a.weight[(long)hb * a.cap + j0 + tid] += red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
+}
+
+__global__ __launch_bounds__(256) void k_qattn_weight_add(QAttnArgs a, const float *wpart, int row_splits) {
+  const int hb = blockIdx.y, b = hb / a.KV, j = blockIdx.x * 256 + threadIdx.x;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  if (m == 0 || j >= held + m) return;
+  const long P = (long)a.B * a.KV;
+  float w = 0.f;
+  for (int i = 0; i < row_splits; ++i) w += wpart[(i * P + hb) * a.cap + j];
+  a.weight[(long)hb * a.cap + j] += w;
 }
 
 template <int HD>
@@ -762,9 +825,23 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     FC_LAUNCH_OK(st, "k_qattn_join");
   }
   if (weigh && !logit) {
-    ProfScope ps(ctx, st, "fc_qattn_weight");
-    hipLaunchKernelGGL(k_qattn_weight<HD>, dim3((unsigned)(a.cap / kQBlock), (unsigned)pairs), dim3(256), 0, st, a);
-    FC_LAUNCH_OK(st, "k_qattn_weight");
+    const long groups = (a.cap + kGroupKeys - 1) / kGroupKeys, all = pairs * groups;
+    // workgroups for four on every CU, each with eight row tiles at least, where their sums fit
+    long rs = std::max<long>(1, std::min(4L * ctx->num_cus / all, (R + 255) / 256));
+    rs = std::max<long>(1, std::min<long>(rs, (ws - up4(per)) / (pairs * a.cap)));
+    if (all * rs > (1L << 24) - 1)
+      return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: weights of %ld heads of %d rows in one call", pairs, a.cap);
+    float *wpart = rs > 1 ? ctx->part + up4(per) : nullptr;   // the splits' parts are joined by now
+    {
+      ProfScope ps(ctx, st, "fc_qattn_weight");
+      hipLaunchKernelGGL(k_qattn_weight<HD>, dim3((unsigned)(all * rs)), dim3(256), 0, st, a, wpart, (int)rs);
+      FC_LAUNCH_OK(st, "k_qattn_weight");
+    }
+    if (rs > 1) {
+      ProfScope ps(ctx, st, "fc_qattn_weight_add");
+      hipLaunchKernelGGL(k_qattn_weight_add, dim3((unsigned)((a.cap + 255) / 256), (unsigned)pairs), dim3(256), 0, st, a, wpart, (int)rs);
+      FC_LAUNCH_OK(st, "k_qattn_weight_add");
+    }
   }
   return FC_OK;
 }
