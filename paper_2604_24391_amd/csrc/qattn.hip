@@ -45,6 +45,7 @@ struct QAttnArgs {
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, tile_rows;
+  Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
 };
 
@@ -56,9 +57,22 @@ __device__ __forceinline__ bf16x8 dequant8(uint32_t w0, uint32_t w1, float s) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// LDS words that lanes of one wave write in parts and read whole, and the order between the two.
+typedef uint16_t __attribute__((may_alias)) part16;
+typedef uint32_t __attribute__((may_alias)) part32;
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 // Bytes of w that hold a NaN (0x7f or 0xff), as 0x01 each.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
+}
+// The four low bits of such bytes, side by side.
+__device__ __forceinline__ uint32_t byte_bits(uint32_t n) { return (n * 0x01020408u) >> 24 & 15u; }
+// The bits of a block's 64 keys below `seen` (relative to the block's first).
+__device__ __forceinline__ uint64_t seen_bits(int seen) {
+  return seen >= 64 ? ~0ull : (seen <= 0 ? 0ull : (1ull << seen) - 1ull);
 }
 // Bytes of w that are not zero, as 0xff each.
 __device__ __forceinline__ uint32_t set_bytes(uint32_t w) {
@@ -96,6 +110,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   __shared__ float sm_o[4][16][OS];
   __shared__ float2 sm_ml[4][16 * MT];
   __shared__ float sm_l[16], sm_lse[16];
+  __shared__ uint64_t sm_nan[4][HD];
   const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, split = blockIdx.x % a.splits;
   const int r0 = blockIdx.x / a.splits * (16 * MT);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
@@ -103,8 +118,8 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   const int rows = m * a.G, R = a.n * a.G;
   if (r0 >= rows) return;
   const int last = min(r0 + 16 * MT, rows) - 1;
-  const int kmax = held + last / a.G + 1;       // keys that any row sees
-  const int kall = held + r0 / a.G + 1;         // keys that every row sees, but for the mask
+  const int kmax = held + a.by_g(last) + 1;       // keys that any row sees
+  const int kall = held + a.by_g(r0) + 1;         // keys that every row sees, but for the mask
   const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
   if (split >= used) return;
   const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
@@ -114,9 +129,9 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int r = r0 + 16 * t + l16;
-    seen[t] = r < rows ? held + r / a.G + 1 : 0;
-    const int rc = min(r, rows - 1);
-    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
+    const int rc = min(r, rows - 1), tok = a.by_g(rc);
+    seen[t] = r < rows ? held + tok + 1 : 0;
+    const uint16_t *src = a.q + (((long)b * a.n + tok) * a.H + kv * a.G + rc - tok * a.G) * HD;
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
       q[t][2 * i] = load_q(src + 64 * i + g * 16, a.flip);
@@ -163,19 +178,26 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
         vis[i] &= left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
       }
     }
-    // what no row sees may hold anything, NaN among it, and 0 x NaN is NaN; a NaN that only later
-    // rows see is taken out too and added for them apart
+    // What no row sees may hold anything, NaN among it, and 0 x NaN is NaN: such values become 0.  A
+    // NaN that some rows see becomes 0 too, and NaN is what these rows get for it afterwards.
     bool odd = false;
     if (!full) {
       uint32_t any = 0;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d) {
+        uint32_t bits = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           vw[d][i] &= vis[i];
-          any |= nan_bytes(vw[d][i]);
+          const uint32_t n = nan_bytes(vw[d][i]);
+          vw[d][i] &= ~(n * 255u);
+          bits |= byte_bits(n) << (4 * i);
         }
+        reinterpret_cast<part16 *>(&sm_nan[wave][16 * d + l16])[g] = (uint16_t)bits;
+        any |= bits;
+      }
       odd = __any(any != 0);
+      wave_lds_order();
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -227,32 +249,21 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         o[t][d] *= corr;
-        if (!odd) {
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][0], vw[d][1], vs), p[0], o[t][d], 0, 0, 0);
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][2], vw[d][3], vs), p[1], o[t][d], 0, 0, 0);
-        } else {
-          // finite values as ever; a second product counts the NaN among the keys each row sees
-          uint32_t fin[4], bad[4];
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][0], vw[d][1], vs), p[0], o[t][d], 0, 0, 0);
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(vw[d][2], vw[d][3], vs), p[1], o[t][d], 0, 0, 0);
+      }
+      if (odd) {
+        uint64_t keys = 0;               // that the lane's row sees
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t nb = nan_bytes(vw[d][i]);
-            fin[i] = vw[d][i] & ~(nb * 255u);
-            bad[i] = nb * 0x38u;                 // e4m3 1.0
-          }
-          bf16x8 one[2];
+        for (int i = 0; i < 4; ++i) keys |= (uint64_t)byte_bits(vis[i] & 0x01010101u) << (16 * g + 4 * i);
+        keys |= __shfl_xor(keys, 16);
+        keys |= __shfl_xor(keys, 32);
+        keys &= seen_bits(seen[t] - j0);
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              one[x >> 1][(x & 1) * 4 + e] = (__bf16)(s[x][e] == kNegInf ? 0.f : 1.f);
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(fin[0], fin[1], vs), p[0], o[t][d], 0, 0, 0);
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(fin[2], fin[3], vs), p[1], o[t][d], 0, 0, 0);
-          f32x4 cn = {0, 0, 0, 0};
-          cn = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(bad[0], bad[1], 1.f), one[0], cn, 0, 0, 0);
-          cn = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(bad[2], bad[3], 1.f), one[1], cn, 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][d][e] = cn[e] > 0.f ? __builtin_nanf("") : o[t][d][e];
-        }
+          for (int e = 0; e < 4; ++e)
+            if (sm_nan[wave][16 * d + 4 * g + e] & keys) o[t][d][e] = __builtin_nanf("");
       }
     }
   }
@@ -300,7 +311,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
       } else {
         const float inv = sm_l[row] == 0.f ? 0.f : 1.f / sm_l[row];
         const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
-        *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
+        *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
       }
     }
   }
@@ -329,6 +340,20 @@ __device__ __forceinline__ int key_swz(int row) {
 }
 __device__ __forceinline__ int val_swz(int dim) { return (dim >> 2) & 3; }
 
+// LDS DMA of 4 B per lane to lds + 4 * lane (lds must be wave-uniform), as dma16.
+__device__ __forceinline__ void dma4(const void *gp, uint32_t lds) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane(lds);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "global_load_lds_dword %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(gp), "s"(l)
+      : "memory");
+}
+
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
@@ -337,24 +362,25 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   constexpr int DMAS = TILE / 16 / 256;         // DMA instructions of a wave for either
   constexpr int STAGES = 3;
   __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
+  __shared__ uint64_t sm_nan[4][HD];
   // pairs fastest: an XCD (workgroups go round the 8 in turn) keeps to few pairs' keys; the
   // longest rows first
   const int P = a.B * a.KV, R = a.n * a.G;
   const int hb = blockIdx.x % P, rest = blockIdx.x / P, split = rest % a.splits;
   const int r0 = ((R + 127) / 128 - 1 - rest / a.splits) * 128;
   const int b = hb / a.KV, kv = hb % a.KV;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int rows = m * a.G;
   if (r0 >= rows) return;
-  const int kmax = held + (min(r0 + 128, rows) - 1) / a.G + 1;
+  const int kmax = held + a.by_g(min(r0 + 128, rows) - 1) + 1;
   const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
   if (split >= used) return;
   const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
   const long nblk = a.cap / kQBlock;
   const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
-  const float *ksb = a.ks + hb * nblk, *vsb = a.vs + hb * nblk;
+  const uniform_floats ksb = as_uniform(a.ks + hb * nblk), vsb = as_uniform(a.vs + hb * nblk);
   int ksrc[DMAS], vsrc[DMAS];
 #pragma unroll
   for (int i = 0; i < DMAS; ++i) {
@@ -370,13 +396,14 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int i = 0; i < DMAS; ++i) dma16(vbase + at + vsrc[i], lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
   };
 
-  const int w0 = r0 + 32 * wave, r = w0 + l32, rc = min(r, rows - 1);
-  const int seen = r < rows ? held + r / a.G + 1 : 0;                       // keys that the lane's row sees
-  const int wmax = w0 < rows ? held + (min(w0 + 32, rows) - 1) / a.G + 1 : 0;   // that any row of the wave sees
-  const int wall = held + w0 / a.G + 1;                                     // that every one does
+  const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
+  const int seen = r < rows ? held + tok + 1 : 0;                              // keys that the lane's row sees
+  const int wmax = w0 < rows ? held + a.by_g(min(w0 + 32, rows) - 1) + 1 : 0;  // that any row of the wave sees
+  const int wall = held + a.by_g(w0) + 1;                                      // that every one does
+  const long at_q = (((long)b * a.n + tok) * a.H + head) * HD;
   bf16x8 q[HD / 16];
   {
-    const uint16_t *src = a.q + (((long)b * a.n + rc / a.G) * a.H + kv * a.G + rc % a.G) * HD;
+    const uint16_t *src = a.q + at_q;
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) {
       q[2 * i] = load_q(src + (2 * i + h) * 16, a.flip);
@@ -397,10 +424,9 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
 
-  auto block = [&](auto full_tag, int blk, const uint8_t *kt, const uint8_t *vt) {
+  auto block = [&](auto full_tag, int blk, const uint8_t *kt, const uint8_t *vt, float ks, float vs) {
     constexpr bool FULL = decltype(full_tag)::value;
     const int j0 = blk * kQBlock;
-    const float ks = ksb[blk], vs = vsb[blk];
     uint32_t vis[8];                 // the lane's 32 keys that some row may see, by bytes
     if constexpr (!FULL) {
 #pragma unroll
@@ -461,64 +487,68 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
         sum += y;
         p[2 * t + e / 8][e % 8] = (__bf16)y;
       }
+    uint32_t any = 0;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      u32x4 w[2];
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w[i] = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
-      bool odd = false;
-      if constexpr (!FULL) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
+        if constexpr (!FULL) {       // as in k_qattn
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            w[i][x] &= vis[4 * i + x];
-            any |= nan_bytes(w[i][x]);
+            w[x] &= vis[4 * i + x];
+            const uint32_t n = nan_bytes(w[x]);
+            w[x] &= ~(n * 255u);
+            any |= n;
           }
-        odd = __any(any != 0);
-      }
-      if (!odd) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][0], w[i][1], vs), p[2 * i], o[d], 0, 0, 0);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][2], w[i][3], vs), p[2 * i + 1], o[d], 0, 0, 0);
         }
-      } else {
-        // as in k_qattn: finite values, then NaN for the rows that see one
-        f32x16 cn;
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], vs), p[2 * i], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], vs), p[2 * i + 1], o[d], 0, 0, 0);
+      }
+    if constexpr (!FULL) {
+      if (__any(any != 0)) {
+        uint32_t mine = 0;               // the lane's 32 keys that some row may see
 #pragma unroll
-        for (int e = 0; e < 16; ++e) cn[e] = 0.f;
+        for (int i = 0; i < 8; ++i) mine |= byte_bits(vis[i] & 0x01010101u) << (4 * i);
+        const uint32_t other = __shfl_xor(mine, 32);
+        const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
+#pragma unroll 1
+        for (int d = 0; d < DT; ++d) {
+          uint32_t bits = 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t n0 = nan_bytes(w[i][2 * x]), n1 = nan_bytes(w[i][2 * x + 1]);
-            bf16x8 one;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) one[e] = (__bf16)(s[i][8 * x + e] == kNegInf ? 0.f : 1.f);
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[i][2 * x] & ~(n0 * 255u), w[i][2 * x + 1] & ~(n1 * 255u), vs), p[2 * i + x], o[d], 0, 0, 0);
-            cn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(n0 * 0x38u, n1 * 0x38u, 1.f), one, cn, 0, 0, 0);
+            for (int x = 0; x < 4; ++x) bits |= byte_bits(nan_bytes(w[x])) << (16 * i + 4 * x);
           }
+          reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
+        }
+        wave_lds_order();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] = cn[e] > 0.f ? __builtin_nanf("") : o[d][e];
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (sm_nan[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4] & keys) o[d][e] = __builtin_nanf("");
       }
     }
   };
 
   int stage = 0;
+  float ks = ksb[blo], vs = vsb[blo];
   for (int blk = blo; blk < bhi; ++blk) {
     // this block's DMAs are done when at most the next one's are outstanding
     if (blk + 1 < bhi) wait_vm<2 * DMAS>();
     else wait_vm<0>();
     lds_barrier();                   // and the other waves', and everyone has left the oldest stage
     if (blk + 2 < bhi) fetch(blk + 2, stage == 0 ? 2 : stage - 1);
-    const int j0 = blk * kQBlock;
+    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
+    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
     const uint8_t *kt = sm[stage][0], *vt = sm[stage][1];
     if (j0 < wmax) {
-      if (!a.mask && j0 + kQBlock <= wall) block(std::true_type{}, blk, kt, vt);
-      else block(std::false_type{}, blk, kt, vt);
+      if (!a.mask && j0 + kQBlock <= wall) block(std::true_type{}, blk, kt, vt, ks, vs);
+      else block(std::false_type{}, blk, kt, vt, ks, vs);
     }
+    ks = ks_next, vs = vs_next;
     stage = stage == 2 ? 0 : stage + 1;
   }
 
@@ -537,7 +567,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   } else {
     if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t *dst = a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD;
+    uint16_t *dst = a.out + at_q;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -567,7 +597,7 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   if (r < join_rows) {
     if (r >= rows) return;
     const int rt = r / a.tile_rows * a.tile_rows, last = min(rt + a.tile_rows, rows) - 1;
-    const int used = splits_used(held + last / a.G + 1, a.splits);
+    const int used = splits_used(held + a.by_g(last) + 1, a.splits);
     const int sg = tid / TPR, d = tid % TPR * 4;
     const long at = (long)hb * R + r;
     float mt = kNegInf, l = 0.f;
@@ -598,7 +628,7 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
       for (int i = 0; i < SG; ++i) t += *reinterpret_cast<const f32x4 *>(&sm_y[i][d]);
       t *= sum == 0.f ? 0.f : 1.f / sum;
       const bf16x4 w = {(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
-      *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + r / a.G) * a.H + kv * a.G + r % a.G) * HD + d) = w;
+      *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
       if (a.lse && tid == 0) a.lse[at] = log_sum(top, sum);
     }
     return;
@@ -655,10 +685,11 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   constexpr int PC = HD / 8;                    // 16-byte pieces of a query row
   constexpr int TILE = 32 * HD * 2, DMAS = TILE / 16 / 256;
   __shared__ __align__(1024) uint8_t sm[3][TILE];
+  __shared__ float sm_l[3][4][64];              // a wave's copy of the tile's row sums, twice
   const int P = a.B * a.KV, R = a.n * a.G;
   const int hb = blockIdx.x % P, rest = blockIdx.x / P, rs = rest % row_splits, j0 = rest / row_splits * kGroupKeys;
   const int b = hb / a.KV, kv = hb % a.KV;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int rows = m * a.G, seen = held + m;
   if (m == 0 || j0 >= seen) return;
@@ -676,21 +707,19 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
       // S^T row x of tile t is key 32 t + x
       const u32x4 w = *reinterpret_cast<const u32x4 *>(
           a.k + ((long)hb * a.cap + (long)blk * kQBlock + 32 * t + l32) * HD + (2 * i + h) * 16);
-      k[t][2 * i] = dequant8(w[0], w[1], ks);
-      k[t][2 * i + 1] = dequant8(w[2], w[3], ks);
+      k[t][2 * i] = dequant8(w[0], w[1], a.flip ? -ks : ks);
+      k[t][2 * i + 1] = dequant8(w[2], w[3], a.flip ? -ks : ks);
     }
   const uint16_t *qb = a.q + ((long)b * a.n * a.H + kv * a.G) * HD;
+  const float *lse = a.lse + (long)hb * R;
   auto fetch = [&](int tile, int stage) {
 #pragma unroll
     for (int i = 0; i < DMAS; ++i) {
-      const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(tile * 32 + row, rows - 1);
+      const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(tile * 32 + row, rows - 1), tok = a.by_g(r);
       const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
-      dma16(qb + ((long)(r / a.G) * a.H + r % a.G) * HD + piece * 8, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
+      dma16(qb + ((long)tok * (a.H - a.G) + r) * HD + piece * 8, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
     }
-  };
-  auto load_l = [&](int tile) {
-    const int r = tile * 32 + l32;
-    return r < rows ? a.lse[(long)hb * R + r] : __builtin_inff();
+    dma4(lse + min(tile * 32 + l32, rows - 1), lds_addr(&sm_l[stage][wave][0]));
   };
   f32x16 acc[2];
 #pragma unroll
@@ -698,25 +727,20 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   loads_done();
-  float next = 0.f;
-  if (lo < hi) {
-    next = load_l(lo);
-    fetch(lo, 0);
-    if (lo + 1 < hi) fetch(lo + 1, 1);
-  }
+  if (lo < hi) fetch(lo, 0);
+  if (lo + 1 < hi) fetch(lo + 1, 1);
   const int qx = HD == 128 ? l32 & 15 : (l32 >> 1) & 7;
   int stage = 0;
   for (int tile = lo; tile < hi; ++tile) {
-    if (tile + 1 < hi) wait_vm<DMAS>();
+    if (tile + 1 < hi) wait_vm<DMAS + 1>();
     else wait_vm<0>();
     lds_barrier();
-    const float L = next;
-    if (tile + 1 < hi) next = load_l(tile + 1);
+    const float L = sm_l[stage][wave][l32];
     if (tile + 2 < hi) fetch(tile + 2, stage == 0 ? 2 : stage - 1);
     const uint8_t *qt = sm[stage] + l32 * HD * 2;
     stage = stage == 2 ? 0 : stage + 1;
     const int r = tile * 32 + l32;
-    if (w0 >= held + min(tile * 32 + 31, rows - 1) / a.G + 1) continue;      // the last row sees none
+    if (w0 >= held + a.by_g(min(tile * 32 + 31, rows - 1)) + 1) continue;      // the last row sees none
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -727,17 +751,17 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         // piece of 8 elements: dims (2 i + h) 16 + 8 x
-        const bf16x8 q = load_q(reinterpret_cast<const uint16_t *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16), a.flip);
+        const bf16x8 q = *reinterpret_cast<const bf16x8 *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16);
         s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][2 * i + x], q, s[0], 0, 0, 0);
         s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][2 * i + x], q, s[1], 0, 0, 0);
       }
-    if (tile * 32 + 32 <= rows && w0 + kWaveKeys <= held + tile * 32 / a.G + 1) {
+    if (tile * 32 + 32 <= rows && w0 + kWaveKeys <= held + a.by_g(tile * 32) + 1) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], a.c, -L));
     } else {
-      const int see = r < rows ? held + r / a.G + 1 : 0;
+      const int see = r < rows ? held + a.by_g(r) + 1 : 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -860,6 +884,7 @@ fc_status launch_qcache_attention(fc_ctx *ctx, const fc_qcache &c, const uint16_
   a.c = std::max(std::fabs(scale) * kLog2e, 1.2e-38f);
   a.flip = scale < 0.f ? 0x80008000u : 0u;
   a.B = B, a.n = n, a.H = n_heads, a.KV = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.cap = c.capacity;
+  a.by_g = quot_by(a.G);
   return c.head_dim == 128 ? run_qattn<128>(ctx, a, accumulate, st) : run_qattn<64>(ctx, a, accumulate, st);
 }
 

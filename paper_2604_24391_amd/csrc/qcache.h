@@ -55,12 +55,36 @@ __device__ __forceinline__ uint32_t rescale_e4m3(uint32_t w, float ratio) {
   return pack_e4m3(x.x * ratio, x.y * ratio, x.z * ratio, x.w * ratio);
 }
 
-// Rows held and rows new of item b, clamped so that no value makes a kernel leave its buffers.
+// Rows held and rows new of item b (the same in every lane), clamped so that no value makes a
+// kernel leave its buffers.
 __device__ __forceinline__ int q_held(const int32_t *len, int b, int cap) {
-  return min(max(len[b], 0), cap);
+  return __builtin_amdgcn_readfirstlane(min(max(len[b], 0), cap));
 }
 __device__ __forceinline__ int q_new(const int32_t *n_new, int b, int n, int held, int cap) {
-  return min(n_new ? min(max(n_new[b], 0), n) : n, cap - held);
+  return min(n_new ? __builtin_amdgcn_readfirstlane(min(max(n_new[b], 0), n)) : n, cap - held);
+}
+
+// Numbers that no kernel of the launch writes, at an index that all lanes share: read by the scalar
+// unit, whose loads no wait for vector loads in flight touches.
+typedef const __attribute__((address_space(4))) float *uniform_floats;
+__device__ __forceinline__ uniform_floats as_uniform(const float *p) {
+  return (uniform_floats)(uintptr_t)p;
+}
+
+// Quotients of numbers up to 2^30 by a divisor d from 1 to 2^24: i / d = mulhi(4 i, magic) >> shift
+// with shift = ceil(log2 d), magic = ceil(2^(30 + shift) / d) <= 2^30 + ...: magic d - 2^(30 + shift) < d
+// <= 2^shift, so the error i (magic d - 2^(30 + shift)) / 2^(30 + shift) stays below 1 for i <= 2^30.
+struct Quot {
+  uint32_t magic;
+  int shift;
+  __device__ __forceinline__ int operator()(int i) const {
+    return (int)(__umulhi((uint32_t)i << 2, magic) >> shift);
+  }
+};
+inline Quot quot_by(int d) {
+  int s = 0;
+  while ((1L << s) < d) ++s;
+  return Quot{(uint32_t)(((1UL << (30 + s)) + d - 1) / d), s};
 }
 
 }  // namespace
