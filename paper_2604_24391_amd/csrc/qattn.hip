@@ -20,7 +20,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "fc_internal.h"
 #include "qcache.h"
@@ -424,23 +423,19 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
 
-  auto block = [&](auto full_tag, int blk, const uint8_t *kt, const uint8_t *vt, float ks, float vs) {
-    constexpr bool FULL = decltype(full_tag)::value;
-    const int j0 = blk * kQBlock;
-    uint32_t vis[8];                 // the lane's 32 keys that some row may see, by bytes
-    if constexpr (!FULL) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int left = wmax - (j0 + h * 32 + 4 * i);
-        vis[i] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
-      }
-      if (a.mask) {
-        const u32x4 *mw = reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + h * 32);
-        const u32x4 m0 = mw[0], m1 = mw[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vis[i] &= set_bytes(m0[i]), vis[4 + i] &= set_bytes(m1[i]);
-      }
-    }
+  int stage = 0;
+  float ks = ksb[blo], vs = vsb[blo];
+  for (int blk = blo; blk < bhi; ++blk) {
+    // this block's DMAs are done when at most the next one's are outstanding
+    if (blk + 1 < bhi) wait_vm<2 * DMAS>();
+    else wait_vm<0>();
+    lds_barrier();                   // and the other waves', and everyone has left the oldest stage
+    if (blk + 2 < bhi) fetch(blk + 2, stage == 0 ? 2 : stage - 1);
+    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
+    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
+    const uint8_t *kt = sm[stage][0], *vt = sm[stage][1];
+    stage = stage == 2 ? 0 : stage + 1;
+    if (j0 >= wmax) continue;
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -453,14 +448,47 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
       }
     }
-    if constexpr (!FULL) {
+    u32x4 vw[DT][2];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) vw[d][i] = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
+    // a block that some row of the wave may not see whole
+    const bool part = a.mask || j0 + kQBlock > wall;
+    uint32_t mine = ~0u, any = 0;    // the lane's 32 keys that some row may see; NaN among them
+    if (part) {
+      uint32_t vis[8];               // by bytes
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int left = wmax - (j0 + h * 32 + 4 * i);
+        vis[i] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+      }
+      if (a.mask) {
+        const u32x4 *mw = reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + h * 32);
+        const u32x4 m0 = mw[0], m1 = mw[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vis[i] &= set_bytes(m0[i]), vis[4 + i] &= set_bytes(m1[i]);
+      }
+      mine = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mine |= byte_bits(vis[i] & 0x01010101u) << (4 * i);
+      const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + h * 32 + t * 16 + e;
-          if (!(j < seen && (vis[4 * t + e / 4] >> (8 * (e & 3)) & 1u))) s[t][e] = kNegInf;
-        }
+        for (int e = 0; e < 16; ++e)
+          if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
+      // values as in k_qattn
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t w = vw[d][i][x] & vis[4 * i + x], n = nan_bytes(w);
+            vw[d][i][x] = w & ~(n * 255u);
+            any |= n;
+          }
     }
     float top = kNegInf;
 #pragma unroll
@@ -487,69 +515,35 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
         sum += y;
         p[2 * t + e / 8][e % 8] = (__bf16)y;
       }
-    uint32_t any = 0;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
-        if constexpr (!FULL) {       // as in k_qattn
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            w[x] &= vis[4 * i + x];
-            const uint32_t n = nan_bytes(w[x]);
-            w[x] &= ~(n * 255u);
-            any |= n;
-          }
-        }
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], vs), p[2 * i], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], vs), p[2 * i + 1], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][i][0], vw[d][i][1], vs), p[2 * i], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][i][2], vw[d][i][3], vs), p[2 * i + 1], o[d], 0, 0, 0);
       }
-    if constexpr (!FULL) {
-      if (__any(any != 0)) {
-        uint32_t mine = 0;               // the lane's 32 keys that some row may see
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mine |= byte_bits(vis[i] & 0x01010101u) << (4 * i);
-        const uint32_t other = __shfl_xor(mine, 32);
-        const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
+    if (part && __any(any != 0)) {
+      const uint32_t other = __shfl_xor(mine, 32);
+      const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
 #pragma unroll 1
-        for (int d = 0; d < DT; ++d) {
-          uint32_t bits = 0;
+      for (int d = 0; d < DT; ++d) {
+        uint32_t bits = 0;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
+        for (int i = 0; i < 2; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
 #pragma unroll
-            for (int x = 0; x < 4; ++x) bits |= byte_bits(nan_bytes(w[x])) << (16 * i + 4 * x);
-          }
-          reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
+          for (int x = 0; x < 4; ++x) bits |= byte_bits(nan_bytes(w[x])) << (16 * i + 4 * x);
         }
-        wave_lds_order();
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (sm_nan[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4] & keys) o[d][e] = __builtin_nanf("");
+        reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
       }
-    }
-  };
-
-  int stage = 0;
-  float ks = ksb[blo], vs = vsb[blo];
-  for (int blk = blo; blk < bhi; ++blk) {
-    // this block's DMAs are done when at most the next one's are outstanding
-    if (blk + 1 < bhi) wait_vm<2 * DMAS>();
-    else wait_vm<0>();
-    lds_barrier();                   // and the other waves', and everyone has left the oldest stage
-    if (blk + 2 < bhi) fetch(blk + 2, stage == 0 ? 2 : stage - 1);
-    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
-    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
-    const uint8_t *kt = sm[stage][0], *vt = sm[stage][1];
-    if (j0 < wmax) {
-      if (!a.mask && j0 + kQBlock <= wall) block(std::true_type{}, blk, kt, vt, ks, vs);
-      else block(std::false_type{}, blk, kt, vt, ks, vs);
+      wave_lds_order();
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (sm_nan[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4] & keys) o[d][e] = __builtin_nanf("");
     }
     ks = ks_next, vs = vs_next;
-    stage = stage == 2 ? 0 : stage + 1;
   }
 
   sum += __shfl_xor(sum, 32);
