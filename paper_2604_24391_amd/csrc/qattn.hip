@@ -362,6 +362,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   constexpr int STAGES = 3;
   __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
   __shared__ uint64_t sm_nan[4][HD];
+  __shared__ __align__(16) uint8_t sm_mask[STAGES][4][256];
   // pairs fastest: an XCD (workgroups go round the 8 in turn) keeps to few pairs' keys; the
   // longest rows first
   const int P = a.B * a.KV, R = a.n * a.G;
@@ -393,6 +394,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int i = 0; i < DMAS; ++i) dma16(kbase + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
 #pragma unroll
     for (int i = 0; i < DMAS; ++i) dma16(vbase + at + vsrc[i], lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
+    // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
+    if (a.mask) dma4(a.mask + (long)b * a.cap + blk * kQBlock + (lane & 15) * 4, lds_addr(&sm_mask[stage][wave][0]));
   };
 
   const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
@@ -423,19 +426,37 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
 
+  u32x4 kw[2][HD / 32];               // the coming block's keys, e4m3
+  auto keys = [&](int st) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i)
+        kw[t][i] = *reinterpret_cast<const u32x4 *>(&sm[st][0][koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16)]);
+  };
+  // this wave's DMAs of all blocks but the last `ahead` are done; the barrier adds the other waves'
+  auto arrived = [&](bool ahead) {
+    if (!ahead) wait_vm<0>();
+    else if (a.mask) wait_vm<2 * DMAS + 1>();
+    else wait_vm<2 * DMAS>();
+    lds_barrier();
+  };
+  arrived(blo + 1 < bhi);
+  keys(0);
   int stage = 0;
   float ks = ksb[blo], vs = vsb[blo];
   for (int blk = blo; blk < bhi; ++blk) {
-    // this block's DMAs are done when at most the next one's are outstanding
-    if (blk + 1 < bhi) wait_vm<2 * DMAS>();
-    else wait_vm<0>();
-    lds_barrier();                   // and the other waves', and everyone has left the oldest stage
-    if (blk + 2 < bhi) fetch(blk + 2, stage == 0 ? 2 : stage - 1);
+    // the stage that the block before was in: every wave has read it, by the barrier below
+    const int next = stage == 2 ? 0 : stage + 1;
+    if (blk + 2 < bhi) fetch(blk + 2, next == 2 ? 0 : next + 1);
     const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
     const float ks_next = ksb[ahead], vs_next = vsb[ahead];
-    const uint8_t *kt = sm[stage][0], *vt = sm[stage][1];
-    stage = stage == 2 ? 0 : stage + 1;
-    if (j0 >= wmax) continue;
+    u32x4 vw[DT][2];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        vw[d][i] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16)]);
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -443,18 +464,21 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) {
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(kt + koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16));
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(kw[t][i][0], kw[t][i][1], ks), q[2 * i], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(kw[t][i][2], kw[t][i][3], ks), q[2 * i + 1], s[t], 0, 0, 0);
       }
     }
-    u32x4 vw[DT][2];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) vw[d][i] = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
-    // a block that some row of the wave may not see whole
-    const bool part = a.mask || j0 + kQBlock > wall;
+    const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
+    u32x4 m0 = {~0u, ~0u, ~0u, ~0u}, m1 = m0;
+    if (a.mask) {
+      m0 = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32]);
+      m1 = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16]);
+    }
+    if (blk + 1 < bhi) {
+      arrived(blk + 2 < bhi);
+      keys(next);
+    }
+    stage = next;
     uint32_t mine = ~0u, any = 0;    // the lane's 32 keys that some row may see; NaN among them
     if (part) {
       uint32_t vis[8];               // by bytes
@@ -464,8 +488,6 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
         vis[i] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
       }
       if (a.mask) {
-        const u32x4 *mw = reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + h * 32);
-        const u32x4 m0 = mw[0], m1 = mw[1];
 #pragma unroll
         for (int i = 0; i < 4; ++i) vis[i] &= set_bytes(m0[i]), vis[4 + i] &= set_bytes(m1[i]);
       }
@@ -480,15 +502,19 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
           if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
       // values as in k_qattn
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d) {
+        uint32_t bits = 0;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const uint32_t w = vw[d][i][x] & vis[4 * i + x], n = nan_bytes(w);
             vw[d][i][x] = w & ~(n * 255u);
-            any |= n;
+            bits |= byte_bits(n) << (16 * i + 4 * x);
           }
+        reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
+        any |= bits;
+      }
     }
     float top = kNegInf;
 #pragma unroll
@@ -525,17 +551,6 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     if (part && __any(any != 0)) {
       const uint32_t other = __shfl_xor(mine, 32);
       const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
-#pragma unroll 1
-      for (int d = 0; d < DT; ++d) {
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16));
-#pragma unroll
-          for (int x = 0; x < 4; ++x) bits |= byte_bits(nan_bytes(w[x])) << (16 * i + 4 * x);
-        }
-        reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
-      }
       wave_lds_order();
 #pragma unroll
       for (int d = 0; d < DT; ++d)
@@ -724,43 +739,59 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   if (lo < hi) fetch(lo, 0);
   if (lo + 1 < hi) fetch(lo + 1, 1);
   const int qx = HD == 128 ? l32 & 15 : (l32 >> 1) & 7;
-  int stage = 0;
-  for (int tile = lo; tile < hi; ++tile) {
-    if (tile + 1 < hi) wait_vm<DMAS + 1>();
+  bf16x8 q[HD / 16];                  // the coming tile's rows, and their sums
+  float L = 0.f;
+  auto queries = [&](int st) {
+    const uint8_t *qt = sm[st] + l32 * HD * 2;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)     // piece of 8 elements: dims (2 i + h) 16 + 8 x
+        q[2 * i + x] = *reinterpret_cast<const bf16x8 *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16);
+    return sm_l[st][wave][l32];
+  };
+  auto arrived = [&](bool ahead) {
+    if (ahead) wait_vm<DMAS + 1>();
     else wait_vm<0>();
     lds_barrier();
-    const float L = sm_l[stage][wave][l32];
-    if (tile + 2 < hi) fetch(tile + 2, stage == 0 ? 2 : stage - 1);
-    const uint8_t *qt = sm[stage] + l32 * HD * 2;
-    stage = stage == 2 ? 0 : stage + 1;
-    const int r = tile * 32 + l32;
-    if (w0 >= held + a.by_g(min(tile * 32 + 31, rows - 1)) + 1) continue;      // the last row sees none
+  };
+  if (lo < hi) {
+    arrived(lo + 1 < hi);
+    L = queries(0);
+  }
+  int stage = 0;
+  for (int tile = lo; tile < hi; ++tile) {
+    const int next = stage == 2 ? 0 : stage + 1;
+    if (tile + 2 < hi) fetch(tile + 2, next == 2 ? 0 : next + 1);
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        // piece of 8 elements: dims (2 i + h) 16 + 8 x
-        const bf16x8 q = *reinterpret_cast<const bf16x8 *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16);
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][2 * i + x], q, s[0], 0, 0, 0);
-        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][2 * i + x], q, s[1], 0, 0, 0);
-      }
+    for (int i = 0; i < HD / 16; ++i) {
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][i], q[i], s[0], 0, 0, 0);
+      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][i], q[i], s[1], 0, 0, 0);
+    }
+    const float sub = L;
+    if (tile + 1 < hi) {
+      arrived(tile + 2 < hi);
+      L = queries(next);
+    }
+    stage = next;
+    const int r = tile * 32 + l32;
     if (tile * 32 + 32 <= rows && w0 + kWaveKeys <= held + a.by_g(tile * 32) + 1) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], a.c, -L));
+        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], a.c, -sub));
     } else {
       const int see = r < rows ? held + a.by_g(r) + 1 : 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float p = exp2_fast(fmaf(s[t][e], a.c, -L));
+          const float p = exp2_fast(fmaf(s[t][e], a.c, -sub));
           acc[t][e] += w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4 < see ? p : 0.f;
         }
     }
