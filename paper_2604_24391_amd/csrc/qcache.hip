@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "fc_internal.h"
 #include "qcache.h"
@@ -228,37 +229,48 @@ constexpr int kPickThreads = 1024;
 // Weights in an order of unsigned integers; a NaN and what lies below the finite numbers
 // count as the lowest finite one, -0 as 0.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  const float low = -3.402823466e38f;
-  w = (w >= low ? w : low) + 0.f;
-  const uint32_t u = __float_as_uint(w);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(fmaxf(w, -3.402823466e38f) + 0.f);
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
-__device__ __forceinline__ int pick_scan(int f, int *wsum, int *tot) {
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const unsigned long long bits = __ballot(f);
-  const int pre = __popcll(bits & ((1ull << lane) - 1ull));
-  __syncthreads();
-  if (lane == 0) wsum[w] = __popcll(bits);
-  __syncthreads();
-  int base = 0, all = 0;
+constexpr int kPickWaves = kPickThreads / 64;
+
+// Sum of a number over the threads before this one (waves in order, lanes in order); total: over all.
+__device__ __forceinline__ int pick_scan(int x, int *wsum, int &total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int inc = x;
 #pragma unroll
-  for (int i = 0; i < kPickThreads / 64; ++i) {
-    if (i < w) base += wsum[i];
-    all += wsum[i];
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(inc, o);
+    if (lane >= o) inc += y;
   }
-  *tot = all;
-  return base + pre;
+  __syncthreads();
+  if (lane == 63) wsum[w] = inc;
+  __syncthreads();
+  int base = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < kPickWaves; ++i) {
+    if (i < w) base += wsum[i];
+    total += wsum[i];
+  }
+  return base + inc - x;
 }
 
-// The kept rows of one head in ascending order: a radix select over 8 bits of the keys at a
-// time finds the smallest kept key and how many rows of that key stay (the lowest ones).
+// The kept rows of one head in ascending order.  A radix select over 11, 11 and 10 bits of the
+// weights' keys finds the smallest kept key and how many rows of that key stay (the lowest ones);
+// then every wave counts, and writes down, what stays of its own run of rows.
+// Weights share few exponents, so the first digit's counts stand in 16 copies, one for every
+// fourth lane: one copy had the lanes of a wave wait for each other (166 us for 65536 rows
+// against 27).  IT > 0: a lane holds IT keys in registers (up to 1024 IT rows); IT = 0 reads the
+// weights anew in each pass.
+template <int IT>
 __global__ __launch_bounds__(kPickThreads) void k_qevict_pick(EvictArgs a) {
-  __shared__ int hist[256];
-  __shared__ int wsum[kPickThreads / 64];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  const int b = blockIdx.x / a.KV, tid = threadIdx.x;
+  constexpr int BINS = 2048, COPIES = IT == 4 ? 4 : 16;   // fewer to clear and to add up for few rows
+  __shared__ __align__(16) int hist[BINS * COPIES];   // 128 KB of 16 copies: one workgroup on a CU
+  __shared__ int wsum[kPickWaves], wabove[kPickWaves], wties[kPickWaves];
+  __shared__ int s_digit, s_need;
+  const int b = blockIdx.x / a.KV, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = q_held(a.len, b, a.cap);
   const float *w = a.weight + (long)blockIdx.x * a.cap;
   int32_t *kept = a.kept + (long)blockIdx.x * a.keep;
@@ -270,58 +282,133 @@ __global__ __launch_bounds__(kPickThreads) void k_qevict_pick(EvictArgs a) {
   }
   const int lo = a.sink, hi = n - a.recent;              // rows that compete: [lo, hi)
   const int take = a.keep - a.sink - a.recent;           // < hi - lo
-  uint32_t prefix = 0;
+
+  // Keys of rows that compete are at least 0x00800000 (the lowest finite number's); the others,
+  // which stay whatever their weight or lie behind the last row, get 0.
+  // a wave's run of rows: `runs` times 64, row = first + 64 i
+  const int runs = IT ? IT : (n + kPickThreads - 1) / kPickThreads;
+  const int first = wave * runs * 64 + lane;
+  auto load = [&](int i) {
+    const int j = first + 64 * i;
+    const uint32_t u = weight_key(w[min(j, a.cap - 1)]);   // no branch: the loads of a pass overlap
+    return j >= lo && j < hi ? u : 0u;
+  };
+  uint32_t key[IT ? IT : 1];
+#pragma unroll
+  for (int i = 0; i < IT; ++i) key[i] = load(i);
+  auto each = [&](auto f) {                    // f(row, its key)
+    if constexpr (IT > 0) {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) f(first + 64 * i, key[i]);
+    } else {
+      // 16 loads at a time, the last ones repeated where the run ends
+      for (int i = 0; i < runs; i += 16) {
+        const int j0 = wave * runs * 64 + 64 * i, j1 = wave * runs * 64 + 64 * runs;
+        float x[16];
+        if (j0 + 1024 <= j1 && j0 >= lo && j0 + 1024 <= hi) {      // all of them compete
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = w[j0 + lane + 64 * e];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) f(j0 + lane + 64 * e, weight_key(x[e]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = w[min(j0 + lane + 64 * e, a.cap - 1)];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = j0 + lane + 64 * e;
+            if (j0 + 64 * e < j1) f(j, j >= lo && j < hi ? weight_key(x[e]) : 0u);
+          }
+        }
+      }
+    }
+  };
+
+  uint32_t prefix = ~0u;               // no row competes for a place: none is above or ties
   int need = take;
   if (take > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int x = tid; x < 256; x += kPickThreads) hist[x] = 0;
+    auto digit = [&](auto tag) {
+      constexpr int step = decltype(tag)::value;           // bits 31-21, 20-10, 9-0
+      constexpr int shift = step == 0 ? 21 : (step == 1 ? 10 : 0), copies = step == 0 ? COPIES : 1;
+      constexpr uint32_t mask = step == 2 ? 1023u : 2047u;
+      for (int x = tid; x < BINS * copies / 4; x += kPickThreads) reinterpret_cast<int4 *>(hist)[x] = make_int4(0, 0, 0, 0);
       __syncthreads();
-      for (int j = lo + tid; j < hi; j += kPickThreads) {
-        const uint32_t u = weight_key(w[j]);
-        if (shift == 24 || (u >> (shift + 8)) == prefix) atomicAdd(&hist[(u >> shift) & 255u], 1);
+      each([&](int, uint32_t u) {
+        if (step == 0 ? u != 0u : u >> (step == 1 ? 21 : 10) == prefix)
+          atomicAdd(&hist[(u >> shift & mask) * copies + (step == 0 ? lane & (COPIES - 1) : 0)], 1);
+      });
+      __syncthreads();
+      // thread t: bins 2047 - 2 t and 2046 - 2 t, so that a scan runs from the largest key down
+      int c[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int bin = BINS - 1 - 2 * tid - e;
+        c[e] = 0;
+        if constexpr (step == 0) {
+#pragma unroll
+          for (int x = 0; x < COPIES / 4; ++x) {
+            const int4 y = reinterpret_cast<const int4 *>(hist)[bin * (COPIES / 4) + x];
+            c[e] += y.x + y.y + y.z + y.w;
+          }
+        } else {
+          c[e] = hist[bin];
+        }
       }
+      int total;
+      const int before = pick_scan(c[0] + c[1], wsum, total);
+      if (before < need && before + c[0] >= need) s_digit = BINS - 1 - 2 * tid, s_need = need - before;
+      else if (before + c[0] < need && before + c[0] + c[1] >= need) s_digit = BINS - 2 - 2 * tid, s_need = need - before - c[0];
       __syncthreads();
-      if (tid == 0) {
-        int d = 255, above = 0;
-        while (d > 0 && above + hist[d] < need) above += hist[d--];
-        s_prefix = prefix << 8 | (uint32_t)d;
-        s_need = need - above;
-      }
-      __syncthreads();
-      prefix = s_prefix;
+      prefix = step == 0 ? (uint32_t)s_digit : prefix << (step == 1 ? 11 : 10) | (uint32_t)s_digit;
       need = s_need;
-    }
+    };
+    digit(std::integral_constant<int, 0>{});
+    digit(std::integral_constant<int, 1>{});
+    digit(std::integral_constant<int, 2>{});
   }
-  // rows above the smallest kept key and the first `need` rows equal to it
-  int out = 0, ties = 0;
-  for (int j = 0; j < n; j += kPickThreads) {
-    const int r = j + tid;
-    const bool end = r < n && (r < lo || r >= hi);
-    const uint32_t u = r < n ? weight_key(w[r]) : 0u;
-    const bool mid = r < n && !end && take > 0;
-    int all;
-    const bool tie = mid && u == prefix;
-    const int at = ties + pick_scan(tie, wsum, &all);
-    ties += all;
-    const bool stay = end || (mid && u > prefix) || (tie && at < need);
-    const int p = out + pick_scan(stay, wsum, &all);
-    out += all;
-    if (stay && p < a.keep) kept[p] = r;
+  // rows above the smallest kept key, and the first `need` rows equal to it: counted for each wave's
+  // run, then written behind what the waves before keep
+  auto stays = [&](int r, uint32_t u) { return u > prefix || (u == 0u && r < n); };
+  int above = 0, ties = 0;
+  each([&](int r, uint32_t u) {
+    above += __popcll(__ballot(stays(r, u)));
+    ties += __popcll(__ballot(u == prefix));
+  });
+  if (lane == 0) wabove[wave] = above, wties[wave] = ties;
+  __syncthreads();
+  int out = 0, tie = 0;
+  for (int i = 0; i < wave; ++i) {
+    out += wabove[i] + min(max(need - tie, 0), wties[i]);
+    tie += wties[i];
   }
+  const unsigned long long below = (1ull << lane) - 1ull;
+  each([&](int r, uint32_t u) {
+    const unsigned long long t = __ballot(u == prefix);
+    const bool stay = stays(r, u) || (u == prefix && tie + __popcll(t & below) < need);
+    tie += __popcll(t);
+    const unsigned long long k = __ballot(stay);
+    const int to = out + __popcll(k & below);
+    out += __popcll(k);
+    if (stay && to < a.keep) kept[to] = r;
+  });
 }
 
-// One block of 64 kept rows of one head: gathered, scaled anew, written.
+// One block of 64 kept rows of one head: gathered, scaled anew, written.  Key rows are read alone;
+// values lie by columns, so each source block with a kept row in it is read whole (8 KB at hd
+// 128), four at a time through LDS, where single bytes cost nothing.
 template <int HD>
 __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
   constexpr int TPR = HD / 16, RPP = kQThreads / TPR, KP = kQBlock / RPP;
   constexpr int TPD = kQThreads / HD, KPT = kQBlock / TPD;   // threads of a value column, keys of each
+  constexpr int GROUP = 4, VSTR = kQBlock + 4;               // source blocks at a time; off the bank period
+  constexpr int CPT = HD * kQBlock / 16 / kQThreads;         // 16-byte pieces of a block for each thread
   __shared__ int src[kQBlock];
   __shared__ float red[2][kQThreads / 64];
+  __shared__ __align__(16) uint8_t vt[GROUP][HD * VSTR];
   const int hb = blockIdx.y, b = hb / a.KV, blk = blockIdx.x, j0 = blk * kQBlock, tid = threadIdx.x;
   const int n = q_held(a.len, b, a.cap), left = min(n, a.keep), cnt = min(left - j0, kQBlock);
   if (cnt <= 0) return;
-  if (tid < kQBlock)
-    src[tid] = tid < cnt ? min(max(a.kept[(long)hb * a.keep + j0 + tid], 0), a.cap - 1) : 0;
+  // (the last row again behind the end, so that src stays ascending)
+  if (tid < kQBlock) src[tid] = min(max(a.kept[(long)hb * a.keep + j0 + min(tid, cnt - 1)], 0), a.cap - 1);
   __syncthreads();
   const long nblk = a.cap / kQBlock, nblk2 = a.cap2 / kQBlock;
   const float *ks = a.ks + hb * nblk, *vs = a.vs + hb * nblk;
@@ -330,36 +417,59 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
   float kmul[KP], kmax = 0.f;
 #pragma unroll
   for (int p = 0; p < KP; ++p) {
-    const int t = p * RPP + row;
-    if (t < cnt) {
-      const int s = src[t];
-      kr[p] = *reinterpret_cast<const uint4 *>(a.k + ((long)hb * a.cap + s) * HD + sub * 16);
-      kmul[p] = ks[s / kQBlock];
-      const uint32_t w[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 x = unpack_e4m3(w[i]);
-        kmax = fmaxf(kmax, kmul[p] * fmaxf(fmaxf(finite_abs(x.x), finite_abs(x.y)), fmaxf(finite_abs(x.z), finite_abs(x.w))));
-      }
-    }
+    const int s = src[p * RPP + row];
+    kr[p] = *reinterpret_cast<const uint4 *>(a.k + ((long)hb * a.cap + s) * HD + sub * 16);
+    kmul[p] = ks[s / kQBlock];
   }
   const int d = tid / TPD, v0 = tid % TPD * KPT;
-  const uint8_t *vb = a.v + (long)hb * a.cap * HD + d * kQBlock;
-  float vr[KPT], vmax = 0.f;
+  const uint8_t *vb = a.v + (long)hb * a.cap * HD;
+  uint32_t vc[KPT / 4];                 // codes of the thread's keys of its column
+  float vmul[KPT], vmax = 0.f;
 #pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    vr[i] = 0.f;
-    if (v0 + i < cnt) {
-      const int s = src[v0 + i];
-      vr[i] = unpack_e4m3(vb[(long)(s / kQBlock) * (HD * kQBlock) + s % kQBlock]).x * vs[s / kQBlock];
-      vmax = fmaxf(vmax, finite_abs(vr[i]));
+  for (int i = 0; i < KPT / 4; ++i) vc[i] = 0;
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) vmul[i] = vs[src[v0 + i] / kQBlock];
+  const int b0 = src[0] / kQBlock, b1 = src[cnt - 1] / kQBlock;
+  for (int g = b0; g <= b1; g += GROUP) {
+    uint4 x[GROUP][CPT];
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i)
+#pragma unroll
+      for (int c = 0; c < CPT; ++c)
+        x[i][c] = *reinterpret_cast<const uint4 *>(vb + (long)min(g + i, b1) * (HD * kQBlock) + (c * kQThreads + tid) * 16);
+    if (g > b0) __syncthreads();        // the group before has been read
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i)
+#pragma unroll
+      for (int c = 0; c < CPT; ++c) {
+        const int p = c * kQThreads + tid;
+        uint32_t *to = reinterpret_cast<uint32_t *>(&vt[i][p / 4 * VSTR + p % 4 * 16]);
+        to[0] = x[i][c].x, to[1] = x[i][c].y, to[2] = x[i][c].z, to[3] = x[i][c].w;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int s = src[v0 + i], at = s / kQBlock - g;
+      if (at >= 0 && at < GROUP) vc[i / 4] |= (uint32_t)vt[at][d * VSTR + s % kQBlock] << (8 * (i % 4));
     }
   }
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    kmax = fmaxf(kmax, __shfl_xor(kmax, o));
-    vmax = fmaxf(vmax, __shfl_xor(vmax, o));
+  for (int p = 0; p < KP; ++p) {
+    const uint32_t w[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = unpack_e4m3(w[i]);
+      kmax = fmaxf(kmax, kmul[p] * fmaxf(fmaxf(finite_abs(x.x), finite_abs(x.y)), fmaxf(finite_abs(x.z), finite_abs(x.w))));
+    }
   }
+#pragma unroll
+  for (int i = 0; i < KPT / 4; ++i) {
+    const float4 x = unpack_e4m3(vc[i]);
+    vmax = fmaxf(vmax, fmaxf(fmaxf(finite_abs(x.x) * vmul[4 * i], finite_abs(x.y) * vmul[4 * i + 1]),
+                             fmaxf(finite_abs(x.z) * vmul[4 * i + 2], finite_abs(x.w) * vmul[4 * i + 3])));
+  }
+  kmax = wave_max(kmax);
+  vmax = wave_max(vmax);
   if (tid % 64 == 0) red[0][tid / 64] = kmax, red[1][tid / 64] = vmax;
   __syncthreads();
 #pragma unroll
@@ -376,18 +486,19 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
     }
   }
   uint8_t *vd = a.v2 + ((long)hb * nblk2 + blk) * (HD * kQBlock) + d * kQBlock + v0;
-  uint32_t w[KPT / 4];
 #pragma unroll
-  for (int i = 0; i < KPT / 4; ++i)
-    w[i] = pack_e4m3(vr[4 * i] * vi, vr[4 * i + 1] * vi, vr[4 * i + 2] * vi, vr[4 * i + 3] * vi);
+  for (int i = 0; i < KPT / 4; ++i) {
+    const float4 x = unpack_e4m3(vc[i]);
+    vc[i] = pack_e4m3(x.x * (vmul[4 * i] * vi), x.y * (vmul[4 * i + 1] * vi), x.z * (vmul[4 * i + 2] * vi), x.w * (vmul[4 * i + 3] * vi));
+  }
   if (cnt == kQBlock) {
 #pragma unroll
     for (int i = 0; i < KPT / 16; ++i)
-      reinterpret_cast<uint4 *>(vd)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      reinterpret_cast<uint4 *>(vd)[i] = make_uint4(vc[4 * i], vc[4 * i + 1], vc[4 * i + 2], vc[4 * i + 3]);
   } else {
 #pragma unroll
     for (int i = 0; i < KPT; ++i)
-      if (v0 + i < cnt) vd[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+      if (v0 + i < cnt) vd[i] = (uint8_t)(vc[i / 4] >> (8 * (i % 4)));
   }
   if (a.weight2 && tid < cnt) a.weight2[(long)hb * a.cap2 + j0 + tid] = a.weight[(long)hb * a.cap + src[tid]];
 }
@@ -435,7 +546,10 @@ fc_status launch_qcache_evict(fc_ctx *ctx, const fc_qcache &s, const fc_qcache &
   a.keep = keep, a.sink = sink, a.recent = recent;
   {
     ProfScope ps(ctx, st, "fc_qevict_pick");
-    hipLaunchKernelGGL(k_qevict_pick, dim3((unsigned)(B * a.KV)), dim3(kPickThreads), 0, st, a);
+    const dim3 grid((unsigned)(B * a.KV)), block(kPickThreads);
+    if (a.cap <= 4 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<4>, grid, block, 0, st, a);
+    else if (a.cap <= 16 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<16>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(k_qevict_pick<0>, grid, block, 0, st, a);
     FC_LAUNCH_OK(st, "k_qevict_pick");
   }
   const dim3 grid((unsigned)((keep + kQBlock - 1) / kQBlock), (unsigned)(B * a.KV));
