@@ -745,6 +745,8 @@ static fc_status check_qcache(fc_ctx *ctx, const fc_qcache *c, int B, const char
   if (B < 1 || c->n_kv_heads < 1 || (long)B * c->n_kv_heads > 65535)
     return fail(FC_ERR_SHAPE, "%s: B=%d items of %d key-value heads (B n_kv from 1 to 65535)", who, B,
                 c->n_kv_heads);
+  if ((long)B * c->n_kv_heads * c->capacity > (1L << 42) / c->head_dim)
+    return fail(FC_ERR_UNSUPPORTED, "%s: a cache of more than 2^42 bytes", who);
   return FC_OK;
 }
 

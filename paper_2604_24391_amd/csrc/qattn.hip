@@ -38,12 +38,14 @@ struct QAttnArgs {
   uint16_t *out;
   const int32_t *len, *n_new;
   const uint8_t *mask;               // [B][cap], or null
-  float2 *ml;                        // [splits][B KV][R] running maximum (log2) and sum
-  float *part;                       // [splits][B KV][R][hd] unnormalised outputs
+  float2 *ml;                        // running maximum (log2) and sum of each split's rows,
+  float *part;                       // unnormalised outputs [..][hd]: k_qattn [KV][slots][R], k_qattn_rows
+                                     // [splits][B KV][R]
+  int2 *plan;                        // [B] k_qattn: an item's first slot and its slots
   float *lse;                        // [B KV][R] log2 of each row's sum, or null
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
-  int B, n, H, KV, G, cap, splits, tile_rows;
+  int B, n, H, KV, G, cap, splits, tile_rows, slots;
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
 };
@@ -86,11 +88,64 @@ __device__ __forceinline__ bf16x8 load_q(const uint16_t *src, uint32_t flip) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Splits that the key blocks of one tile of rows are dealt over: lengths are known on the device
-// only, so the grid has room for `splits`, and a short item uses no more than leaves each of
-// them four blocks (one per wave).
+// Splits that the key blocks of one tile of rows are dealt over (k_qattn_rows): lengths are known on
+// the device only, so the grid has room for `splits`, and a short item uses no more than leaves
+// each of them four blocks.
 __device__ __forceinline__ int splits_used(int kmax, int splits) {
   return max(1, min(splits, (kmax + 4 * kQBlock - 1) / (4 * kQBlock)));
+}
+// k_qattn deals a.slots workgroups of each key-value head over the items by their lengths, `per`
+// blocks to each: with the same number for every item, the longest one of a ragged batch would
+// keep few CUs busy to the end.  Items take ceil(blocks / per) slots in order; per = ceil(all
+// blocks / (slots - items)) leaves room for what the quotients round up, and at least four blocks
+// (one per wave) to a slot.
+struct Share {
+  int item, start, used, per;       // the item, its first slot, its slots, blocks of each
+  int held, m;                      // its rows held and new
+};
+// The share of the item that slot `slot` falls to (item -1: none).
+__device__ __forceinline__ Share share_of(const QAttnArgs &a, int slot) {
+  const int lane = threadIdx.x & 63;
+  int held = 0, m = 0;                // of item i + lane
+  auto blocks = [&](int i) {
+    const int j = min(i + lane, a.B - 1);
+    held = min(max(a.len[j], 0), a.cap);
+    m = min(a.n_new ? min(max(a.n_new[j], 0), a.n) : a.n, a.cap - held);
+    return i + lane < a.B && m > 0 ? (held + m + kQBlock - 1) / kQBlock : 0;
+  };
+  const int room = max(1, a.slots - a.B);
+  int x = blocks(0);
+  if (a.B == 1) {
+    const int n = __builtin_amdgcn_readfirstlane(x), per = max(4, (n + a.slots - 1) / a.slots), used = (n + per - 1) / per;
+    return Share{slot < used ? 0 : -1, 0, used, per, __builtin_amdgcn_readfirstlane(held), __builtin_amdgcn_readfirstlane(m)};
+  }
+  unsigned all = (unsigned)x;         // below 2^30 for a cache of 2^42 bytes, the largest there is
+  for (int i = 64; i < a.B; i += 64) all += (unsigned)blocks(i);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
+  if (a.B > 64) x = blocks(0);
+  const unsigned per = a.slots > a.B ? max(4u, (all + room - 1) / (unsigned)room) : 1u << 30;
+  int run = 0;
+  for (int i = 0;;) {
+    const int u = (int)(((unsigned)x + per - 1) / per);
+    int inc = u;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o);
+      if (lane >= o) inc += y;
+    }
+    const int at = run + inc - u;
+    const unsigned long long hit = __ballot(slot >= at && slot < at + u);
+    if (hit) {
+      const int l = __ffsll((long long)hit) - 1;
+      return Share{i + l, __builtin_amdgcn_readlane(at, l), __builtin_amdgcn_readlane(u, l), (int)per,
+                   __builtin_amdgcn_readlane(held, l), __builtin_amdgcn_readlane(m, l)};
+    }
+    run += __builtin_amdgcn_readlane(inc, 63);
+    i += 64;
+    if (i >= a.B) return Share{-1, 0, 0, (int)per, 0, 0};
+    x = blocks(i);
+  }
 }
 // log2 of the sum of 2^S of a row from its maximum and sum: the probability of key j is 2^(S_j - L).
 // A row that sees no key gets +inf (every weight 0).
@@ -99,9 +154,22 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 }
 __device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 0.f : exp2_fast(y - L); }
 
-// MT tiles of 16 rows against a run of key blocks; the 4 waves of a workgroup take blocks in
-// turn and their results are joined in LDS.  One split writes the outputs, several their parts.
-template <int HD, int MT>
+// All rows of an item (MT tiles of 16) against a run of its key blocks, which go round the 4 waves;
+// these are joined in LDS.  One split writes the outputs, several their parts.
+// Memory bounds it (MT = 1: about 1000 vector cycles for a block's 16 KB, at 8 waves on a CU
+// several times what HBM delivers), so loads run ahead: each next block's keys are read when the
+// scores have used theirs, its values after the outputs.
+//
+// NT: loads without a place in the memory-side cache.  A cache larger than that (256 MB) is 76.6
+// instead of 83.8 us for eight items of 53 k rows; one that fits, and is there from the step before,
+// would be 26 instead of 22 us for sixteen of 3 k.
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const uint8_t *p) {
+  const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+  return NT ? __builtin_nontemporal_load(q) : *q;
+}
+
+template <int HD, int MT, bool NT>
 __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   constexpr int KC = HD / 64;                   // 16-byte pieces of a key row that a lane holds
   constexpr int DT = HD / 16;                   // output tiles of 16 dims
@@ -110,59 +178,60 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   __shared__ float2 sm_ml[4][16 * MT];
   __shared__ float sm_l[16], sm_lse[16];
   __shared__ uint64_t sm_nan[4][HD];
-  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, split = blockIdx.x % a.splits;
-  const int r0 = blockIdx.x / a.splits * (16 * MT);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
-  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  const int rows = m * a.G, R = a.n * a.G;
-  if (r0 >= rows) return;
-  const int last = min(r0 + 16 * MT, rows) - 1;
-  const int kmax = held + a.by_g(last) + 1;       // keys that any row sees
-  const int kall = held + a.by_g(r0) + 1;         // keys that every row sees, but for the mask
-  const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
-  if (split >= used) return;
-  const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
-
+  const Share sh = share_of(a, blockIdx.x);
+  if (sh.item < 0) return;
+  const int b = sh.item, kv = blockIdx.y, hb = b * a.KV + kv, R = a.n * a.G;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+  const int held = sh.held, m = sh.m, rows = m * a.G;   // m > 0
+  const int kmax = held + m;                    // keys that any row sees
+  const int kall = held + 1;                    // keys that every row sees, but for the mask
+  const int blocks = (kmax + kQBlock - 1) / kQBlock, blo = (blockIdx.x - sh.start) * sh.per;
+  const int bhi = min(blocks - blo, sh.per) + blo;
+  const long slot = (long)kv * a.slots + blockIdx.x;
+  if (a.plan && kv == 0 && blo == 0 && tid == 0) a.plan[b] = make_int2(sh.start, sh.used);
+  const int nblk = a.cap / kQBlock;
+  // S^T row m of tile t is key (m / 4) 16 + 4 t + m % 4
+  const uint8_t *kbase = a.k + (long)hb * a.cap * HD + ((l16 >> 2) * 16 + (l16 & 3)) * HD + g * 16;
+  const uint8_t *vbase = a.v + (long)hb * a.cap * HD + l16 * kQBlock + g * 16;
+  const uniform_floats ksb = as_uniform(a.ks + (long)hb * nblk), vsb = as_uniform(a.vs + (long)hb * nblk);
+  u32x4 kw[4][KC], vw[DT];
+  auto load_k = [&](int blk) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+        kw[t][i] = load16<NT>(kbase + (long)blk * (HD * kQBlock) + 4 * t * HD + 64 * i);
+  };
+  auto load_v = [&](int blk) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vw[d] = load16<NT>(vbase + (long)blk * (HD * kQBlock) + 16 * d * kQBlock);
+  };
+  const int at0 = min(blo + wave, nblk - 1);
+  load_k(at0);
+  load_v(at0);
+  float ks = ksb[at0], vs = vsb[at0];
   bf16x8 q[MT][2 * KC];
   int seen[MT];                                 // keys that the lane's row sees
+  f32x4 o[MT][DT];
+  float mx[MT], sum[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const int r = r0 + 16 * t + l16;
-    const int rc = min(r, rows - 1), tok = a.by_g(rc);
+    const int r = 16 * t + l16, tok = a.by_g(min(r, rows - 1));
     seen[t] = r < rows ? held + tok + 1 : 0;
-    const uint16_t *src = a.q + (((long)b * a.n + tok) * a.H + kv * a.G + rc - tok * a.G) * HD;
+    const uint16_t *src = a.q + (((long)b * a.n + tok) * a.H + kv * a.G + min(r, rows - 1) - tok * a.G) * HD;
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
       q[t][2 * i] = load_q(src + 64 * i + g * 16, a.flip);
       q[t][2 * i + 1] = load_q(src + 64 * i + g * 16 + 8, a.flip);
     }
-  }
-  f32x4 o[MT][DT];
-  float mx[MT], sum[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
     mx[t] = kNegInf, sum[t] = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0, 0, 0, 0};
   }
-  const long nblk = a.cap / kQBlock;
-  const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
-  const float *ksb = a.ks + hb * nblk, *vsb = a.vs + hb * nblk;
 
   for (int blk = blo + wave; blk < bhi; blk += 4) {
-    const int j0 = blk * kQBlock;
-    u32x4 kw[4][KC], vw[DT];
-    // S^T row m of tile t is key (m / 4) 16 + 4 t + m % 4
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int i = 0; i < KC; ++i)
-        kw[t][i] = *reinterpret_cast<const u32x4 *>(
-            kbase + (long)(j0 + (l16 >> 2) * 16 + 4 * t + (l16 & 3)) * HD + 64 * i + g * 16);
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-      vw[d] = *reinterpret_cast<const u32x4 *>(vbase + (long)blk * (HD * kQBlock) + (16 * d + l16) * kQBlock + g * 16);
-    const float ks = ksb[blk], vs = vsb[blk];
+    const int j0 = blk * kQBlock, next = min(blk + 4, nblk - 1);
+    const float ks_next = ksb[next], vs_next = vsb[next];
     const bool full = !a.mask && j0 + kQBlock <= kall;
     uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};      // the lane's 16 keys that some row may see, by bytes
     if (!full) {
@@ -210,6 +279,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(kw[x][i][2], kw[x][i][3], ks), q[t][2 * i + 1], s[x], 0, 0, 0);
         }
       }
+      if (t == MT - 1) load_k(next);
       float top = kNegInf;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
@@ -224,7 +294,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
           top = fmaxf(top, y);
         }
       if (MT == 1 && a.logit && seen[t]) {
-        float *to = a.logit + ((long)hb * R + r0 + 16 * t + l16) * a.cap + j0 + g * 16;
+        float *to = a.logit + ((long)hb * R + 16 * t + l16) * a.cap + j0 + g * 16;
 #pragma unroll
         for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(to + 4 * x) = s[x];
       }
@@ -265,6 +335,8 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
             if (sm_nan[wave][16 * d + 4 * g + e] & keys) o[t][d][e] = __builtin_nanf("");
       }
     }
+    load_v(next);
+    ks = ks_next, vs = vs_next;
   }
 
   // the four waves' parts of each row, joined; a lane's group g holds the sum over its own keys
@@ -289,9 +361,9 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sm_o[wave][l16][16 * d + 4 * g + e] = o[t][d][e] * f;
-    const int rt = r0 + 16 * t;
+    const int rt = 16 * t;
     if (wave == 0 && g == 0) {
-      if (a.ml && rt + l16 < rows) a.ml[((long)split * a.B * a.KV + hb) * R + rt + l16] = make_float2(mt, l);
+      if (a.ml && rt + l16 < rows) a.ml[slot * R + rt + l16] = make_float2(mt, l);
       if (a.lse && rt + l16 < rows) a.lse[(long)hb * R + rt + l16] = log_sum(mt, l);
       sm_l[l16] = l;
       sm_lse[l16] = log_sum(mt, l);
@@ -305,7 +377,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
       for (int e = 0; e < 4; ++e)
         y[e] = sm_o[0][row][d + e] + sm_o[1][row][d + e] + sm_o[2][row][d + e] + sm_o[3][row][d + e];
       if (a.splits > 1) {
-        *reinterpret_cast<float4 *>(a.part + (((long)split * a.B * a.KV + hb) * R + r) * HD + d) =
+        *reinterpret_cast<float4 *>(a.part + (slot * R + r) * HD + d) =
             make_float4(y[0], y[1], y[2], y[3]);
       } else {
         const float inv = sm_l[row] == 0.f ? 0.f : 1.f / sm_l[row];
@@ -602,13 +674,21 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tid = threadIdx.x;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x;
-  const long step = (long)a.B * a.KV * R;
+  // part s of row r: at + s step
+  long step, at0;
+  int used;
+  if (a.slots) {
+    const int2 sh = a.plan[b];        // not written for an item without rows, which returns below
+    step = R, at0 = ((long)kv * a.slots + sh.x) * R, used = sh.y;
+  } else {
+    const int rt = r / a.tile_rows * a.tile_rows;
+    step = (long)a.B * a.KV * R, at0 = (long)hb * R;
+    used = splits_used(held + a.by_g(min(rt + a.tile_rows, max(rows, 1)) - 1) + 1, a.splits);
+  }
   if (r < join_rows) {
     if (r >= rows) return;
-    const int rt = r / a.tile_rows * a.tile_rows, last = min(rt + a.tile_rows, rows) - 1;
-    const int used = splits_used(held + a.by_g(last) + 1, a.splits);
     const int sg = tid / TPR, d = tid % TPR * 4;
-    const long at = (long)hb * R + r;
+    const long at = at0 + r;
     float mt = kNegInf, l = 0.f;
     f32x4 y = {0, 0, 0, 0};
     for (int s = sg; s < used; s += SG) {
@@ -638,7 +718,7 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
       t *= sum == 0.f ? 0.f : 1.f / sum;
       const bf16x4 w = {(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
       *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
-      if (a.lse && tid == 0) a.lse[at] = log_sum(top, sum);
+      if (a.lse && tid == 0) a.lse[(long)hb * R + r] = log_sum(top, sum);
     }
     return;
   }
@@ -646,11 +726,11 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   if (m == 0 || j0 >= seen) return;
   {
     // 16 threads to a row
-    const int row = tid / 16, used = splits_used(seen, a.splits);
+    const int row = tid / 16;
     float mt = kNegInf, l = 0.f;
     if (row < rows)
       for (int s = tid % 16; s < used; s += 16) {
-        const float2 z = a.ml[s * step + (long)hb * R + row];
+        const float2 z = a.ml[s * step + at0 + row];
         const float mn = fmaxf(mt, z.x), ref = mn == kNegInf ? 0.f : mn;
         l = l * exp2_fast(mt - ref) + z.y * exp2_fast(z.x - ref);
         mt = mn;
@@ -830,26 +910,28 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const bool many = R > 64;
   const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4), tile = many ? 128 : 16 * MT;
   const long tiles = (R + tile - 1) / tile;
-  // workgroups for four on every CU (of the many-row kernel: two), as long as each split keeps
-  // four blocks (one per wave)
-  long splits = std::max<long>(1, ((many ? 2L : 4L) * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
+  // workgroups for one on every CU (of k_qattn_rows two), as long as each split keeps four blocks (one
+  // per wave of k_qattn)
+  long splits = std::max<long>(1, ((many ? 2L : 1L) * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
   splits = std::min<long>(splits, std::max(1, a.cap / kQBlock / 4));
   const long per = pairs * R, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
   // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
   // of at least two splits; else the weights compute them again from each row's sum
-  const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD <= ws;
-  const long side = !weigh ? 0 : logit ? per * a.cap : up4(per);
+  const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
+  const long side = (!weigh ? 0 : logit ? per * a.cap : up4(per)) + up4(2L * a.B);
   splits = std::max<long>(1, std::min<long>(splits, (ws - side) / (up4(2 * per) + per * HD)));
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   a.splits = (int)splits;
   a.tile_rows = tile;
+  a.slots = many ? 0 : (int)(splits * a.B);
   float *at = ctx->part;
   if (logit) a.logit = at;
   else if (weigh) a.lse = at;
   at += side;
   if (splits > 1) {
+    a.plan = reinterpret_cast<int2 *>(at - up4(2L * a.B));
     a.part = at;
     a.ml = reinterpret_cast<float2 *>(at + splits * per * HD);
   }
@@ -860,11 +942,13 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     hipLaunchKernelGGL(k_qattn_rows<HD>, dim3((unsigned)(pairs * tiles * splits)), dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn_rows");
   } else {
-    const dim3 grid((unsigned)(tiles * splits), (unsigned)pairs);
+    const dim3 grid((unsigned)a.slots, (unsigned)a.KV);
     ProfScope ps(ctx, st, "fc_qattn");
-    if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1>), grid, dim3(256), 0, st, a);
-    else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_qattn<HD, 4>), grid, dim3(256), 0, st, a);
+    const bool big = pairs * a.cap * HD * 2 > (256L << 20);
+    if (MT == 1 && big) hipLaunchKernelGGL((k_qattn<HD, 1, true>), grid, dim3(256), 0, st, a);
+    else if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1, false>), grid, dim3(256), 0, st, a);
+    else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_qattn<HD, 4, false>), grid, dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn");
   }
   if (splits > 1) {
