@@ -913,6 +913,9 @@ class RopeAxes:
         return 3 if any(self.section) else 1
 
 
+_INT32, _BF16 = torch.int32, torch.bfloat16
+
+
 def _arg(dev: int, t: torch.Tensor, dtype, numel: int, name: str, align: int = 16):
     """Pointer of a contiguous tensor of at least numel elements on GPU `dev`."""
     p = t.data_ptr()
@@ -928,7 +931,9 @@ def _ints(dev: int, t: torch.Tensor | None, numel: int, name: str):
     """The same of int32 numbers, which need no more than their own alignment; None: null."""
     if t is None:
         return None
-    return _arg(dev, t, torch.int32, numel, name, 4)
+    if t.get_device() == dev and t.dtype is _INT32 and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    return _arg(dev, t, _INT32, numel, name, 4)     # for its error
 
 
 # torch's current stream as a number without a Stream object around it (1.2 us of a 3 us launch)
@@ -944,7 +949,7 @@ def _qrows(dev: int, t: torch.Tensor, B: int, n: int, heads: int, hd: int, name:
     """Pointer and strides of [B, n, heads, hd] rows whose heads lie side by side."""
     if t.shape != (B, n, heads, hd):
         raise ValueError(f"{name} is {tuple(t.shape)}, not {(B, n, heads, hd)}")
-    if t.get_device() != dev or t.dtype is not torch.bfloat16:
+    if t.get_device() != dev or t.dtype is not _BF16:
         raise ValueError(f"{name} must be a bfloat16 tensor on GPU {dev}")
     item, row, head, one = t.stride()
     if one != 1 or (head != hd and heads > 1):
@@ -962,7 +967,7 @@ def fc_qcache_append(ctx: Context, cache: QCache, rope: RopeAxes, q: torch.Tenso
     queries go to q_out [B, n, n_heads, hd]; q and q_out may both be None.  lens is not
     advanced: it serves every layer of the step."""
     dev = ctx.device
-    B, n = k.shape[:2]
+    B, n, _, _ = k.shape
     Bc, kv, _, hd = cache.k.shape
     if B != Bc or cache.k.get_device() != dev:
         raise ValueError(f"k has {B} items, the cache {Bc} on {cache.k.device}, the context is on GPU {dev}")
