@@ -71,6 +71,8 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 }
 // The four low bits of such bytes, side by side.
 __device__ __forceinline__ uint32_t byte_bits(uint32_t n) { return (n * 0x01020408u) >> 24 & 15u; }
+// The four low bits of b as bytes of 0xff.
+__device__ __forceinline__ uint32_t bit_bytes(uint32_t b) { return ((b & 15u) * 0x00204081u & 0x01010101u) * 255u; }
 // The bits of a block's 64 keys below `seen` (relative to the block's first).
 __device__ __forceinline__ uint64_t seen_bits(int seen) {
   return seen >= 64 ? ~0ull : (seen <= 0 ? 0ull : (1ull << seen) - 1ull);
@@ -398,8 +400,8 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   }
 }
 
-// Many rows: 4 waves of 32 rows each share the key blocks, which the DMA brings into LDS three
-// deep (16 KB a block at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
+// Many rows: 4 waves of 32 rows each share the key blocks, which the DMA brings into LDS a block
+// ahead (16 KB each at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
 // back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
 // a lane holds one row and, of a block's keys, the 32 of its half wave.
 //
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   constexpr int DT = HD / 32;                   // output tiles of 32 dims
   constexpr int TILE = kQBlock * HD;            // bytes of a block's keys, and of its values
   constexpr int DMAS = TILE / 16 / 256;         // DMA instructions of a wave for either
-  constexpr int STAGES = 3;
+  constexpr int STAGES = 2;
   __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
   __shared__ uint64_t sm_nan[4][HD];
   __shared__ __align__(16) uint8_t sm_mask[STAGES][4][256];
@@ -486,7 +488,6 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   }
   loads_done();
   fetch(blo, 0);
-  if (blo + 1 < bhi) fetch(blo + 1, 1);
 
   // S^T row x of tile t is key ((x / 4) % 2) 32 + 16 t + x / 8 4 + x % 4
   const int kr = ((l32 >> 2) & 1) * 32 + (l32 >> 3) * 4 + (l32 & 3);
@@ -498,95 +499,47 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
 
-  u32x4 kw[2][HD / 32];               // the coming block's keys, e4m3
-  auto keys = [&](int st) {
+  int stage = 0;
+  float ks = ksb[blo], vs = vsb[blo];
+  for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
+    wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
+    lds_barrier();                   // every wave has left the other stage
+    if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1);
+    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
+    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
+    f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i)
-        kw[t][i] = *reinterpret_cast<const u32x4 *>(&sm[st][0][koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16)]);
-  };
-  // this wave's DMAs of all blocks but the last `ahead` are done; the barrier adds the other waves'
-  auto arrived = [&](bool ahead) {
-    if (!ahead) wait_vm<0>();
-    else if (a.mask) wait_vm<2 * DMAS + 1>();
-    else wait_vm<2 * DMAS>();
-    lds_barrier();
-  };
-  arrived(blo + 1 < bhi);
-  keys(0);
-  int stage = 0;
-  float ks = ksb[blo], vs = vsb[blo];
-  for (int blk = blo; blk < bhi; ++blk) {
-    // the stage that the block before was in: every wave has read it, by the barrier below
-    const int next = stage == 2 ? 0 : stage + 1;
-    if (blk + 2 < bhi) fetch(blk + 2, next == 2 ? 0 : next + 1);
-    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
-    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
-    u32x4 vw[DT][2];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        vw[d][i] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + i) ^ vx) * 16)]);
-    f32x16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) {
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(kw[t][i][0], kw[t][i][1], ks), q[2 * i], s[t], 0, 0, 0);
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(kw[t][i][2], kw[t][i][3], ks), q[2 * i + 1], s[t], 0, 0, 0);
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(&sm[stage][0][koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16)]);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
       }
-    }
     const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
-    u32x4 m0 = {~0u, ~0u, ~0u, ~0u}, m1 = m0;
-    if (a.mask) {
-      m0 = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32]);
-      m1 = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16]);
-    }
-    if (blk + 1 < bhi) {
-      arrived(blk + 2 < bhi);
-      keys(next);
-    }
-    stage = next;
     uint32_t mine = ~0u, any = 0;    // the lane's 32 keys that some row may see; NaN among them
     if (part) {
-      uint32_t vis[8];               // by bytes
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int left = wmax - (j0 + h * 32 + 4 * i);
-        vis[i] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
-      }
+      mine = (uint32_t)(seen_bits(wmax - j0) >> (32 * h));
       if (a.mask) {
+        uint32_t bits = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vis[i] &= set_bytes(m0[i]), vis[4 + i] &= set_bytes(m1[i]);
+        for (int i = 0; i < 2; ++i) {
+          const u32x4 mw = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16 * i]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) bits |= byte_bits(set_bytes(mw[x]) & 0x01010101u) << (16 * i + 4 * x);
+        }
+        mine &= bits;
       }
-      mine = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) mine |= byte_bits(vis[i] & 0x01010101u) << (4 * i);
       const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
-      // values as in k_qattn
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t w = vw[d][i][x] & vis[4 * i + x], n = nan_bytes(w);
-            vw[d][i][x] = w & ~(n * 255u);
-            bits |= byte_bits(n) << (16 * i + 4 * x);
-          }
-        reinterpret_cast<part32 *>(&sm_nan[wave][32 * d + l32])[h] = bits;
-        any |= bits;
-      }
     }
     float top = kNegInf;
 #pragma unroll
@@ -604,22 +557,41 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
       for (int d = 0; d < DT; ++d) o[d] *= corr;
     }
     const float sub = ref == kNegInf ? 0.f : ref;
-    bf16x8 p[4];
+    // 16 keys of the lane at a time: their values, their exponentials, their products
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
+      u32x4 vw[DT];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float y = exp2_fast(fmaf(s[t][e], a.c, -sub));
-        sum += y;
-        p[2 * t + e / 8][e % 8] = (__bf16)y;
+      for (int d = 0; d < DT; ++d)
+        vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + t) ^ vx) * 16)]);
+      if (part) {                    // as in k_qattn
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t w = vw[d][x] & bit_bytes(mine >> (16 * t + 4 * x)), n = nan_bytes(w);
+            vw[d][x] = w & ~(n * 255u);
+            bits |= byte_bits(n) << (4 * x);
+          }
+          reinterpret_cast<part16 *>(&sm_nan[wave][32 * d + l32])[2 * h + t] = (uint16_t)bits;
+          any |= bits;
+        }
       }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][i][0], vw[d][i][1], vs), p[2 * i], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][i][2], vw[d][i][3], vs), p[2 * i + 1], o[d], 0, 0, 0);
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = exp2_fast(fmaf(s[t][8 * i + e], a.c, -sub));
+          sum += y;
+          p[e] = (__bf16)y;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][2 * i], vw[d][2 * i + 1], vs), p, o[d], 0, 0, 0);
       }
+    }
     if (part && __any(any != 0)) {
       const uint32_t other = __shfl_xor(mine, 32);
       const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
@@ -799,16 +771,37 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
       k[t][2 * i] = dequant8(w[0], w[1], a.flip ? -ks : ks);
       k[t][2 * i + 1] = dequant8(w[2], w[3], a.flip ? -ks : ks);
     }
+  // where each of this lane's pieces comes from: 32 rows on with each tile, over the other heads
+  // wherever a token ends; rows behind the last one are read as the last one
   const uint16_t *qb = a.q + ((long)b * a.n * a.H + kv * a.G) * HD;
   const float *lse = a.lse + (long)hb * R;
-  auto fetch = [&](int tile, int stage) {
+  const int step_t = a.by_g(32), step_g = 32 - step_t * a.G;
+  const long skip = (long)(a.H - a.G) * HD, step_p = 32L * HD + step_t * skip;
+  const uint16_t *src[DMAS];
+  int head[DMAS];
+#pragma unroll
+  for (int i = 0; i < DMAS; ++i) {
+    const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = lo * 32 + row, tok = a.by_g(r);
+    const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
+    head[i] = r - tok * a.G;
+    src[i] = qb + (long)tok * skip + (long)r * HD + piece * 8;
+  }
+  int filled = lo;                    // tile that the pointers stand at
+  auto fetch = [&](int stage) {
 #pragma unroll
     for (int i = 0; i < DMAS; ++i) {
-      const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(tile * 32 + row, rows - 1), tok = a.by_g(r);
-      const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
-      dma16(qb + ((long)tok * (a.H - a.G) + r) * HD + piece * 8, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
+      const uint16_t *at = src[i];
+      if (filled * 32 + 32 > rows) {
+        const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(filled * 32 + row, rows - 1);
+        at = qb + (long)a.by_g(r) * skip + (long)r * HD + ((p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) * 8;
+      }
+      dma16(at, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
+      src[i] += step_p;
+      head[i] += step_g;
+      if (head[i] >= a.G) head[i] -= a.G, src[i] += skip;
     }
-    dma4(lse + min(tile * 32 + l32, rows - 1), lds_addr(&sm_l[stage][wave][0]));
+    dma4(lse + min(filled * 32 + l32, rows - 1), lds_addr(&sm_l[stage][wave][0]));
+    ++filled;
   };
   f32x16 acc[2];
 #pragma unroll
@@ -816,8 +809,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   loads_done();
-  if (lo < hi) fetch(lo, 0);
-  if (lo + 1 < hi) fetch(lo + 1, 1);
+  if (lo < hi) fetch(0);
+  if (lo + 1 < hi) fetch(1);
   const int qx = HD == 128 ? l32 & 15 : (l32 >> 1) & 7;
   bf16x8 q[HD / 16];                  // the coming tile's rows, and their sums
   float L = 0.f;
@@ -842,7 +835,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   int stage = 0;
   for (int tile = lo; tile < hi; ++tile) {
     const int next = stage == 2 ? 0 : stage + 1;
-    if (tile + 2 < hi) fetch(tile + 2, next == 2 ? 0 : next + 1);
+    if (tile + 2 < hi) fetch(next == 2 ? 0 : next + 1);
     f32x16 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
