@@ -239,7 +239,8 @@ typedef struct {
   uint8_t *k;               /* [B][n_kv][capacity][head_dim]                               */
   uint8_t *v;               /* [B][n_kv][capacity / 64][head_dim][64]: by columns of a block */
   float *k_scale, *v_scale; /* [B][n_kv][capacity / 64]                                    */
-  float *weight;            /* [B][n_kv][capacity] attention weight received so far, or NULL */
+  float *weight;            /* [B][n_kv][capacity] attention weight received so far, or NULL;
+                               like k and v 16-byte aligned                            */
   int32_t n_kv_heads;
   int32_t head_dim;         /* 64 or 128 */
   int32_t capacity;         /* rows of each item and head; a multiple of 64, up to 2^30 */
@@ -497,13 +498,14 @@ fc_status fc_phase_correlate_rotation(fc_ctx *ctx, const float *frames_prev,
  *          (no call advances it: the caller adds n_new after the step's last layer);
  *   n_new: [B] int32 rows that item b brings, its first n_new[b] of the n; NULL: all n;
  *   q_out: [B][n][n_heads][head_dim] bf16 rotated queries (NULL with q NULL); it may be q
- *          itself in that layout, and overlaps no other input.  Rows from n_new[b] on are
- *          left as they are.
+ *          itself in that layout; no other buffer overlaps it or the cache's.  Rows from
+ *          n_new[b] on are left as they are.
  * A block's scale is the smallest power of two s >= 2^-100 with all its new numbers within
  * 448 s, and at least what it was if it held rows before (these are rounded again where it
  * grows).  Numbers are rounded to nearest even from float32; an infinity is held as
  * +-448 s, a NaN as a NaN, and neither sets the scale.  The new rows' weights are set to 0.
- * Rows past the capacity are dropped.  Counts outside their ranges are clamped. */
+ * Rows past the capacity are dropped, their q_out (and out, in the attention) left as it is.
+ * Counts outside their ranges are clamped. */
 fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_axes *rope,
                            const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
                            const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
@@ -517,8 +519,9 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  *   len, n_new: as given to the append;
  *   key_mask: [B][capacity] uint8 (16-byte aligned), or NULL: every row is seen;
  *   out:      [B][n][n_heads][head_dim] bf16: softmax(scale q k) v; a token that sees no
- *             row gets 0; tokens from n_new[b] on are left as they are;
- *   scale:    usually 1 / sqrt(head_dim);
+ *             row gets 0; tokens from n_new[b] on are left as they are; no other buffer
+ *             overlaps it;
+ *   scale:    finite, usually 1 / sqrt(head_dim);
  *   accumulate: 1: weight[b][h][j] += the sum of the probabilities that row j has received
  *             from the tokens and the query heads of its group (cache->weight is needed).
  * What is hidden from a token has no effect on it, whatever its bytes.  The partial results

@@ -735,8 +735,8 @@ static fc_status check_qcache(fc_ctx *ctx, const fc_qcache *c, int B, const char
   if (!c) return fail(FC_ERR_INVALID_ARG, "%s: null cache descriptor", who);
   if (!c->k || !c->v || !c->k_scale || !c->v_scale)
     return fail(FC_ERR_INVALID_ARG, "%s: null cache buffer", who);
-  if (((uintptr_t)c->k | (uintptr_t)c->v) % 16)
-    return fail(FC_ERR_INVALID_ARG, "%s: the cache's k and v must be 16-byte aligned", who);
+  if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->weight) % 16)
+    return fail(FC_ERR_INVALID_ARG, "%s: the cache's k, v and weight must be 16-byte aligned", who);
   if (c->head_dim != 64 && c->head_dim != 128)
     return fail(FC_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128)", who, c->head_dim);
   if (c->capacity < FC_QCACHE_BLOCK || c->capacity % FC_QCACHE_BLOCK || c->capacity > (1 << 30))
@@ -749,6 +749,29 @@ static fc_status check_qcache(fc_ctx *ctx, const fc_qcache *c, int B, const char
     return fail(FC_ERR_UNSUPPORTED, "%s: a cache of more than 2^42 bytes", who);
   return FC_OK;
 }
+
+// Buffers of one call: the first `written` are written, and share memory with no other one.
+struct QBuffers {
+  const void *p[16];
+  size_t n[16];
+  int count = 0, written = 0;
+  void add(const void *ptr, size_t bytes) { p[count] = ptr, n[count++] = bytes; }
+  void add(const fc_qcache &c, int B) {
+    const size_t rows = (size_t)B * c.n_kv_heads * c.capacity, scales = rows / FC_QCACHE_BLOCK * sizeof(float);
+    add(c.k, rows * c.head_dim);
+    add(c.v, rows * c.head_dim);
+    add(c.k_scale, scales);
+    add(c.v_scale, scales);
+    add(c.weight, rows * sizeof(float));
+  }
+  void end_written() { written = count; }
+  bool clash() const {
+    for (int i = 0; i < written; ++i)
+      for (int j = i + 1; j < count; ++j)
+        if (fc::overlap2(p[i], n[i], p[j], n[j])) return true;
+    return false;
+  }
+};
 
 static fc_status check_qrows(const fc_qcache &c, int n_heads, int B, int n, const char *who) {
   if (n_heads < 1 || n_heads % c.n_kv_heads)
@@ -781,7 +804,15 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
                 sec[0], sec[1], sec[2], c.head_dim / 2);
   const uint16_t *in[3] = {x.q, x.k, x.v};
   const int64_t row[3] = {x.q_row, x.k_row, x.v_row}, item[3] = {x.q_item, x.k_item, x.v_item};
-  const size_t qb = (size_t)B * n * x.n_heads * c.head_dim * 2;
+  const size_t qb = (size_t)B * n * x.n_heads * c.head_dim * 2, ib = (size_t)B * sizeof(int32_t);
+  const int axes = sec[0] || sec[1] || sec[2] ? 3 : 1;
+  QBuffers buf;
+  buf.add(c, B);
+  buf.add(q_out, qb);
+  buf.end_written();
+  buf.add(pos, axes * n * ib);
+  buf.add(len, ib);
+  buf.add(n_new, ib);
   if ((uintptr_t)q_out % 16) return fail(FC_ERR_INVALID_ARG, "%s: q_out must be 16-byte aligned", who);
   for (int i = 0; i < 3; ++i) {
     if (!in[i]) continue;
@@ -793,10 +824,11 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
     const size_t bytes = ((size_t)(B - 1) * item[i] + (size_t)(n - 1) * row[i] + width) * 2;
     const bool same = i == 0 && x.q == q_out && (n == 1 || row[0] == width) &&
                       (B == 1 || item[0] == (int64_t)n * width);
-    if (!same && fc::overlap2(in[i], bytes, q_out, qb))
-      return fail(FC_ERR_INVALID_ARG, "%s: q_out overlaps an input (it may be q itself in the same "
-                  "layout)", who);
+    if (!same) buf.add(in[i], bytes);
   }
+  if (buf.clash())
+    return fail(FC_ERR_INVALID_ARG, "%s: q_out or a buffer of the cache overlaps another one (q_out may "
+                "be q itself in the same layout)", who);
   DeviceScope dev(ctx);
   if (dev.st != FC_OK) return dev.st;
   return fc::launch_qcache_append(ctx, c, *rope, x, pos, len, n_new, q_out, B, n,
@@ -820,8 +852,20 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
     return fail(FC_ERR_INVALID_ARG, "%s: accumulate %d (0 or 1)", who, accumulate);
   if (accumulate && !c.weight)
     return fail(FC_ERR_INVALID_ARG, "%s: accumulate needs the cache's weight buffer", who);
-  const size_t qb = (size_t)B * n * n_heads * c.head_dim * 2;
-  if (fc::overlap(q, out, qb)) return fail(FC_ERR_INVALID_ARG, "%s: q and out overlap", who);
+  const size_t qb = (size_t)B * n * n_heads * c.head_dim * 2, ib = (size_t)B * sizeof(int32_t);
+  QBuffers buf;
+  buf.add(out, qb);
+  if (accumulate) buf.add(c.weight, (size_t)B * c.n_kv_heads * c.capacity * sizeof(float));
+  buf.end_written();
+  fc_qcache read = c;
+  read.weight = nullptr;
+  buf.add(read, B);
+  buf.add(q, qb);
+  buf.add(key_mask, (size_t)B * c.capacity);
+  buf.add(len, ib);
+  buf.add(n_new, ib);
+  if (buf.clash())
+    return fail(FC_ERR_INVALID_ARG, "%s: out (or, with accumulate, the weights) overlaps another buffer", who);
   DeviceScope dev(ctx);
   if (dev.st != FC_OK) return dev.st;
   return fc::launch_qcache_attention(ctx, c, q, len, n_new, key_mask, out, n_heads, scale,
@@ -845,25 +889,16 @@ fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *ds
                 who, keep, n_sink, n_recent);
   if (keep > dst->capacity)
     return fail(FC_ERR_SHAPE, "%s: keep %d above the destination's capacity %d", who, keep, dst->capacity);
-  // every buffer that is written against every other one
-  const size_t heads = (size_t)B * src->n_kv_heads;
-  auto parts = [&](const fc_qcache &c, const void **p, size_t *n) {
-    const size_t rows = heads * c.capacity, blocks = rows / FC_QCACHE_BLOCK * sizeof(float);
-    p[0] = c.k, p[1] = c.v, p[2] = c.k_scale, p[3] = c.v_scale, p[4] = c.weight;
-    n[0] = n[1] = rows * c.head_dim, n[2] = n[3] = blocks, n[4] = rows * sizeof(float);
-  };
-  const void *buf[13];
-  size_t bytes[13];
-  parts(*dst, buf, bytes);
-  buf[5] = kept, bytes[5] = heads * keep * sizeof(int32_t);
-  buf[6] = len_out, bytes[6] = B * sizeof(int32_t);
-  parts(*src, buf + 7, bytes + 7);
-  buf[12] = len, bytes[12] = B * sizeof(int32_t);
-  for (int i = 0; i < 7; ++i)
-    for (int j = i + 1; j < 13; ++j)
-      if (fc::overlap2(buf[i], bytes[i], buf[j], bytes[j]))
-        return fail(FC_ERR_INVALID_ARG, "%s: a buffer that is written overlaps another one (the two "
-                    "caches, kept, len and len_out must share no memory)", who);
+  QBuffers buf;
+  buf.add(*dst, B);
+  buf.add(kept, (size_t)B * src->n_kv_heads * keep * sizeof(int32_t));
+  buf.add(len_out, B * sizeof(int32_t));
+  buf.end_written();
+  buf.add(*src, B);
+  buf.add(len, B * sizeof(int32_t));
+  if (buf.clash())
+    return fail(FC_ERR_INVALID_ARG, "%s: a buffer that is written overlaps another one (the two caches, "
+                "kept, len and len_out must share no memory)", who);
   DeviceScope dev(ctx);
   if (dev.st != FC_OK) return dev.st;
   return fc::launch_qcache_evict(ctx, *src, *dst, len, keep, n_sink, n_recent, kept, len_out, B,

@@ -768,8 +768,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
       // S^T row x of tile t is key 32 t + x
       const u32x4 w = *reinterpret_cast<const u32x4 *>(
           a.k + ((long)hb * a.cap + (long)blk * kQBlock + 32 * t + l32) * HD + (2 * i + h) * 16);
-      k[t][2 * i] = dequant8(w[0], w[1], a.flip ? -ks : ks);
-      k[t][2 * i + 1] = dequant8(w[2], w[3], a.flip ? -ks : ks);
+      k[t][2 * i] = dequant8(w[0], w[1], ks);
+      k[t][2 * i + 1] = dequant8(w[2], w[3], ks);
     }
   // where each of this lane's pieces comes from: 32 rows on with each tile, over the other heads
   // wherever a token ends; rows behind the last one are read as the last one
@@ -803,6 +803,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
     dma4(lse + min(filled * 32 + l32, rows - 1), lds_addr(&sm_l[stage][wave][0]));
     ++filled;
   };
+  const float c = a.flip ? -a.c : a.c;   // the queries' signs are as they came
   f32x16 acc[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
@@ -857,14 +858,14 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], a.c, -sub));
+        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], c, -sub));
     } else {
       const int see = r < rows ? held + a.by_g(r) + 1 : 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float p = exp2_fast(fmaf(s[t][e], a.c, -sub));
+          const float p = exp2_fast(fmaf(s[t][e], c, -sub));
           acc[t][e] += w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4 < see ? p : 0.f;
         }
     }
@@ -912,8 +913,8 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
   // of at least two splits; else the weights compute them again from each row's sum
   const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
-  const long side = (!weigh ? 0 : logit ? per * a.cap : up4(per)) + up4(2L * a.B);
-  splits = std::max<long>(1, std::min<long>(splits, (ws - side) / (up4(2 * per) + per * HD)));
+  const long side = !weigh ? 0 : logit ? per * a.cap : up4(per), plan = up4(2L * a.B);
+  splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + per * HD)));
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   a.splits = (int)splits;
@@ -924,7 +925,8 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   else if (weigh) a.lse = at;
   at += side;
   if (splits > 1) {
-    a.plan = reinterpret_cast<int2 *>(at - up4(2L * a.B));
+    a.plan = reinterpret_cast<int2 *>(at);
+    at += plan;
     a.part = at;
     a.ml = reinterpret_cast<float2 *>(at + splits * per * HD);
   }
@@ -983,7 +985,7 @@ fc_status launch_qcache_attention(fc_ctx *ctx, const fc_qcache &c, const uint16_
   a.q = q, a.out = out, a.len = len, a.n_new = n_new, a.mask = key_mask;
   // a negative scale turns the queries' signs instead; scale 0: a number that leaves scores of any
   // ordinary size at 0 and hidden ones at -inf
-  a.c = std::max(std::fabs(scale) * kLog2e, 1.2e-38f);
+  a.c = std::min(std::max(std::fabs(scale) * kLog2e, 1.2e-38f), 3.4e38f);
   a.flip = scale < 0.f ? 0x80008000u : 0u;
   a.B = B, a.n = n, a.H = n_heads, a.KV = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.cap = c.capacity;
   a.by_g = quot_by(a.G);

@@ -71,9 +71,9 @@ __device__ __forceinline__ uniform_floats as_uniform(const float *p) {
   return (uniform_floats)(uintptr_t)p;
 }
 
-// Quotients of numbers up to 2^30 by a divisor d from 1 to 2^24: i / d = mulhi(4 i, magic) >> shift
-// with shift = ceil(log2 d), magic = ceil(2^(30 + shift) / d) <= 2^30 + ...: magic d - 2^(30 + shift) < d
-// <= 2^shift, so the error i (magic d - 2^(30 + shift)) / 2^(30 + shift) stays below 1 for i <= 2^30.
+// Quotients i / d for 0 <= i < 2^30 and 1 <= d <= 2^30: mulhi(4 i, magic) >> s with s = ceil(log2 d) and
+// magic = ceil(2^(30 + s) / d) < 2^32.  e = magic d - 2^(30 + s) < d <= 2^s, so i magic / 2^(30 + s)
+// exceeds i / d by i e / (d 2^(30 + s)) < 1 / d: not enough to reach the next integer.
 struct Quot {
   uint32_t magic;
   int shift;

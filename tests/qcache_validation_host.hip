@@ -101,6 +101,10 @@ int main() {
     fc_qcache odd = c;
     odd.k = c.k + 8;
     EXPECT(att(&odd), FC_ERR_INVALID_ARG);
+    odd = c;
+    odd.weight = c.weight + 1;
+    EXPECT(att(&odd), FC_ERR_INVALID_ARG);
+    EXPECT(ev(&c, &odd), FC_ERR_INVALID_ARG);
   }
   // rotary sections and theta
   for (fc_rope_axes r : {fc_rope_axes{1.0, {0, 0, 0}}, fc_rope_axes{NAN, {0, 0, 0}}, fc_rope_axes{INFINITY, {0, 0, 0}}, fc_rope_axes{1e6, {16, 24, 23}},
@@ -151,6 +155,28 @@ int main() {
     EXPECT(ev(&c, &y), FC_ERR_HIP);
     EXPECT(fc_qcache_attention(&ctx, &c, u16(14), i32(12), nullptr, nullptr, u16(14) + 8, 28, 1.f, 0, 1, 1, nullptr), FC_ERR_INVALID_ARG);
     EXPECT(fc_qcache_attention(&ctx, &c, u16(14), i32(12), nullptr, u8(15) + 1, u16(16), 28, 1.f, 0, 1, 1, nullptr), FC_ERR_INVALID_ARG);
+  }
+  // what is written shares memory with nothing else
+  {
+    const size_t k_bytes = (size_t)2 * 4 * 4224 * 128;
+    auto to = [&](const void *out) {
+      return fc_qcache_attention(&ctx, &c, u16(14), i32(12), i32(13), u8(15), reinterpret_cast<uint16_t *>((uintptr_t)out), 28, 1.f, 1, 2, 1, nullptr);
+    };
+    for (const void *p : {(const void *)(c.k + k_bytes - 16), (const void *)c.v, (const void *)c.k_scale, (const void *)c.v_scale, (const void *)c.weight,
+                          (const void *)u8(15), (const void *)i32(12), (const void *)i32(13)})
+      EXPECT(to(p), FC_ERR_INVALID_ARG);
+    EXPECT(to(c.k + k_bytes), FC_ERR_HIP);
+    fc_qcache y = c;
+    y.weight = reinterpret_cast<float *>(u8(15));
+    EXPECT(att(&y), FC_ERR_INVALID_ARG);                                 // over the mask
+    EXPECT(att(&y, 28, 0.1f, 0), FC_ERR_HIP);                            // not written
+    y = c;
+    y.v = c.k + k_bytes - 16;
+    EXPECT(app(&y, &rope, &x), FC_ERR_INVALID_ARG);
+    for (int i : {0, 1, 2, 3, 4, 11, 12, 13}) EXPECT(app(&c, &rope, &x, 2, 1, u16(i)), FC_ERR_INVALID_ARG);
+    fc_qkv_rows z = x;
+    z.k = reinterpret_cast<uint16_t *>(c.v);
+    EXPECT(app(&c, &rope, &z), FC_ERR_INVALID_ARG);
   }
   // evict
   EXPECT(ev(&c, &d, 0, 0, 0), FC_ERR_INVALID_ARG);

@@ -244,6 +244,56 @@ def test_attention_extreme_scores(fc, ctx):
     run_attention(fc, ctx, g, "qwen", 1, 3, 256, [180], None, cache=cache)
 
 
+@pytest.mark.parametrize("heads,n", [("toy", 1), ("qwen", 3), ("three", 9), ("toy", 66)])
+def test_attention_many_ragged_items(fc, ctx, heads, n):
+    """More items than a wave has lanes, of lengths from nothing to the whole cache, some without new
+    rows, the long ones at the end and in the middle."""
+    g = torch.Generator().manual_seed(20 + n)
+    B, cap = 133, 512
+    held = [(37 * b * b) % 200 for b in range(B)]
+    new = [(b * 7) % (n + 1) for b in range(B)]
+    held[3] = held[64] = held[129] = 0
+    new[3] = new[64] = n
+    held[63], held[130], new[130] = cap - n, cap - n, n
+    held[70] = cap                                      # full: its tokens are dropped
+    tail = slice(100, 110)
+    new[tail] = [0] * 10
+    run_attention(fc, ctx, g, heads, B, n, cap, held, [min(x, cap - h) for x, h in zip(new, held)])
+
+
+@pytest.mark.parametrize("heads,n", [("qwen", 1), ("three", 7), ("qwen", 9), ("three", 50), ("toy", 90)])
+def test_attention_masked_and_split(fc, ctx, heads, n):
+    """Hidden keys (NaN in their rows) and a NaN that some tokens see, over cache lengths that splits share."""
+    g = torch.Generator().manual_seed(30 + n)
+    H, kv, hd, _ = HEADS[heads]
+    B, cap, held = 3, 2048, [1900, 700, 64]
+    cache = filled(fc, g, B, kv, hd, cap)
+    mask = torch.rand(B, cap, generator=g) > 0.3
+    mask[0, 300:1200] = False
+    mask[2] = False
+    mask = mask.cuda()
+    cache.k.copy_(torch.where(~mask[:, None, :, None], torch.tensor(0x7F, dtype=torch.uint8, device="cuda"), cache.k))
+    cache.v.copy_(torch.where(~mask.view(B, 1, -1, 1, 64), torch.tensor(0xFF, dtype=torch.uint8, device="cuda"), cache.v))
+    j = held[0] + n // 2
+    mask[0, j] = True
+    cache.k[0, :, j] = 0x11
+    cache.v[0, :, j // 64, :, j % 64] = 0x22
+    cache.v[0, 0, j // 64, 5, j % 64] = 0x7F
+    _, out = run_attention(fc, ctx, g, heads, B, n, cap, held, [n, n, max(1, n - 1)], mask=mask.to(torch.uint8), cache=cache)
+    assert not out[2, :max(1, n - 1)].any()
+    assert out[0, n // 2:, 0].isnan().any(-1).all() and not out[0, :n // 2].isnan().any()
+
+
+@pytest.mark.parametrize("heads,n", [("qwen", 1), ("three", 9), ("qwen", 30)])
+def test_attention_other_scales(fc, ctx, heads, n):
+    """A negative scale turns the order of the keys; one that is huge leaves scores of 0 at 0."""
+    g = torch.Generator().manual_seed(40 + n)
+    H, kv, hd, _ = HEADS[heads]
+    run_attention(fc, ctx, g, heads, 2, n, 1024, [900, 70], None, scale=-0.2)
+    q = torch.zeros(2, n, H, hd, dtype=torch.bfloat16, device="cuda")
+    run_attention(fc, ctx, g, heads, 2, n, 1024, [900, 70], None, scale=3e38, q=q)
+
+
 def test_attention_few_heads_in_a_small_workspace(fc):
     """A context whose workspace holds no split's parts: one split, the same results."""
     g = torch.Generator().manual_seed(9)
@@ -322,6 +372,18 @@ def test_evict(fc, ctx, heads, held, keep, sink, recent):
     g = torch.Generator().manual_seed(keep)
     run_evict(fc, ctx, g, heads, 3, 320, held, keep, sink, recent)
     run_evict(fc, ctx, g, heads, 3, 320, held, keep, sink, recent, cap2=512, weight2=False)
+
+
+@pytest.mark.parametrize("cap,held,keep,sink,recent", [
+    (4160, [4160, 4097, 1000], 2100, 4, 128), (16384, [16384, 9000, 3001], 3000, 0, 700), (16448, [16448, 16385, 64], 1500, 64, 0),
+    (40000, [40000, 33333, 17000], 16900, 5, 77)])
+def test_evict_long_caches(fc, ctx, cap, held, keep, sink, recent):
+    """Caches of thousands of rows, with weights of few exponents and, for one item, few values."""
+    g = torch.Generator().manual_seed(cap)
+    B = len(held)
+    cache = filled(fc, g, B, 2, 64, cap)
+    cache.weight[1].copy_(torch.randint(0, 50, cache.weight[1].shape, generator=g).float().cuda() / 64)
+    run_evict(fc, ctx, g, "group2", B, cap, held, keep, sink, recent, cache=cache)
 
 
 def test_evict_ties_and_odd_weights(fc, ctx):
@@ -489,6 +551,24 @@ def test_same_inputs_same_bytes(fc, ctx):
         got.append((out, cache.weight.clone()))
     for o, x in got[1:]:
         assert torch.equal(o, got[0][0]) and torch.equal(x, got[0][1])
+
+
+def test_written_buffers_share_no_memory(fc, ctx):
+    H, kv, hd, sec = HEADS["toy"]
+    c, lens = qu.make(fc, 1, kv, hd, 128), ints([0])
+    x = torch.ones(1, 2, H, hd, dtype=torch.bfloat16, device="cuda")
+    over = c.k.view(-1)[:x.numel() * 2].view(torch.bfloat16).view(x.shape)
+    k = c.v.view(-1)[:2 * 2 * kv * hd].view(torch.bfloat16).view(1, 2, kv, hd)
+    one = torch.ones(1, 2, kv, hd, dtype=torch.bfloat16, device="cuda")
+    before = [c.k.clone(), c.v.clone()]
+    for f in (lambda: fc.fc_qcache_attention(ctx, c, x, lens, None, over),
+              lambda: fc.fc_qcache_append(ctx, c, fc.RopeAxes(1e6, sec), x, one, one, ints([[[0, 0]]] * 3), lens, None, over),
+              lambda: fc.fc_qcache_append(ctx, c, fc.RopeAxes(1e6, sec), None, k, one, ints([[[0, 0]]] * 3), lens, None, None)):
+        with pytest.raises(fc.FcError) as e:
+            f()
+        assert e.value.status == 1
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, before[0]) and torch.equal(c.v, before[1])
 
 
 def test_guards(fc, ctx):
