@@ -870,22 +870,24 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
         }
     }
   }
-  // over the 32 rows of a half wave: each step halves the registers that a lane still sums
-  const long out = (long)hb * a.cap;
+  // Summed over the 32 rows of a half wave: at each step a lane hands half of its keys' sums to the
+  // lane across and adds that one's other half, until it holds one key's.
+  float w[32];
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int e = 0; e < 32; ++e) w[e] = acc[e / 16][e % 16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float w = acc[t][e];
+  for (int o = 16; o; o >>= 1)
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) w += __shfl_xor(w, o);
-      const int j = w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4;
-      if (l32 == 0 && j < seen) {
-        if (a.mask && !a.mask[(long)b * a.cap + j]) w = 0.f;
-        if (wpart) wpart[(long)rs * P * a.cap + out + j] = w;
-        else a.weight[out + j] += w;
-      }
+    for (int e = 0; e < o; ++e) {
+      const bool up = l32 & o;
+      w[e] = (up ? w[e + o] : w[e]) + __shfl_xor(up ? w[e] : w[e + o], o);
     }
+  const int j = w0 + 32 * (l32 / 16) + 8 * (l32 % 16 / 4) + 4 * h + l32 % 4;
+  if (j >= seen) return;
+  const float x = a.mask && !a.mask[(long)b * a.cap + j] ? 0.f : w[0];
+  const long out = (long)hb * a.cap + j;
+  if (wpart) wpart[(long)rs * P * a.cap + out] = x;
+  else a.weight[out] += x;
 }
 
 __global__ __launch_bounds__(256) void k_qattn_weight_add(QAttnArgs a, const float *wpart, int row_splits) {
