@@ -647,16 +647,9 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x;
   // part s of row r: at + s step
-  long step, at0;
-  int used;
-  if (a.slots) {
-    const int2 sh = a.plan[b];        // not written for an item without rows, which returns below
-    step = R, at0 = ((long)kv * a.slots + sh.x) * R, used = sh.y;
-  } else {
-    const int rt = r / a.tile_rows * a.tile_rows;
-    step = (long)a.B * a.KV * R, at0 = (long)hb * R;
-    used = splits_used(held + a.by_g(min(rt + a.tile_rows, max(rows, 1)) - 1) + 1, a.splits);
-  }
+  const int2 sh = a.plan[b];          // not written for an item without rows, which returns below
+  const long step = R, at0 = ((long)kv * a.slots + sh.x) * R;
+  const int used = sh.y;
   if (r < join_rows) {
     if (r >= rows) return;
     const int sg = tid / TPR, d = tid % TPR * 4;
@@ -732,6 +725,51 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   } else {
     for (int e = 0; e < seen - j; ++e) to[e] += w[e];
   }
+}
+
+// The same for k_qattn_rows, whose rows are many and splits few: HD / 4 lanes for each row, eight
+// splits' parts in flight at a time.
+template <int HD>
+__global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
+  constexpr int TPR = HD / 4;
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, d = threadIdx.x % TPR * 4;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (r >= rows) return;
+  const int last = min(r / a.tile_rows * a.tile_rows + a.tile_rows, rows) - 1;
+  const int used = splits_used(held + a.by_g(last) + 1, a.splits);
+  const long step = (long)a.B * a.KV * R, at = (long)hb * R + r;
+  float mt = kNegInf, l = 0.f;
+  f32x4 y = {0, 0, 0, 0};
+  for (int s0 = 0; s0 < used; s0 += 8) {
+    float2 z[8];
+    f32x4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const long p = min(s0 + i, used - 1) * step + at;
+      z[i] = a.ml[p];
+      x[i] = *reinterpret_cast<const f32x4 *>(a.part + p * HD + d);
+    }
+    float mn = mt;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mn = fmaxf(mn, z[i].x);
+    const float ref = mn == kNegInf ? 0.f : mn, f = exp2_fast(mt - ref);
+    mt = mn;
+    l *= f;
+    y *= f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float h = exp2_fast(z[i].x - ref);
+      if (s0 + i >= used) break;
+      l += z[i].y * h;
+      y += x[i] * h;
+    }
+  }
+  y *= l == 0.f ? 0.f : 1.f / l;
+  const int tok = a.by_g(r);
+  const bf16x4 w = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+  *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + tok) * a.H + kv * a.G + r - tok * a.G) * HD + d) = w;
+  if (a.lse && d == 0) a.lse[at] = log_sum(mt, l);
 }
 
 // The weight that each key receives, from scores computed again: 4 waves hold 64 keys each in
@@ -950,9 +988,15 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   }
   if (splits > 1) {
     ProfScope ps(ctx, st, "fc_qattn_join");
-    const long more = logit ? (a.cap + kWeightKeys - 1) / kWeightKeys : 0;
-    hipLaunchKernelGGL(k_qattn_join<HD>, dim3((unsigned)(R + more), (unsigned)pairs), dim3(256), 0, st, a, (int)R);
-    FC_LAUNCH_OK(st, "k_qattn_join");
+    if (many) {
+      const int rpw = 1024 / HD;     // rows of a workgroup
+      hipLaunchKernelGGL(k_qattn_join_rows<HD>, dim3((unsigned)((R + rpw - 1) / rpw), (unsigned)pairs), dim3(256), 0, st, a);
+      FC_LAUNCH_OK(st, "k_qattn_join_rows");
+    } else {
+      const long more = logit ? (a.cap + kWeightKeys - 1) / kWeightKeys : 0;
+      hipLaunchKernelGGL(k_qattn_join<HD>, dim3((unsigned)(R + more), (unsigned)pairs), dim3(256), 0, st, a, (int)R);
+      FC_LAUNCH_OK(st, "k_qattn_join");
+    }
   }
   if (weigh && !logit) {
     const long groups = (a.cap + kGroupKeys - 1) / kGroupKeys, all = pairs * groups;
