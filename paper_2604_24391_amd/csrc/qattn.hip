@@ -39,8 +39,8 @@ struct QAttnArgs {
   const int32_t *len, *n_new;
   const uint8_t *mask;               // [B][cap], or null
   float2 *ml;                        // running maximum (log2) and sum of each split's rows,
-  float *part;                       // unnormalised outputs [..][hd]: k_qattn [KV][slots][R], k_qattn_rows
-                                     // [splits][B KV][R]
+  float *part;                       // unnormalised outputs: k_qattn [KV][slots][R][hd], k_qattn_rows as
+                                     // k_qattn_join_rows has it
   int2 *plan;                        // [B] k_qattn: an item's first slot and its slots
   float *lse;                        // [B KV][R] log2 of each row's sum, or null
   float *logit;                      // [B KV][R][cap] scores (log2), or null
@@ -611,12 +611,11 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   if (a.splits > 1) {
     const long to = (long)split * P * R + at;
     if (h == 0) a.ml[to] = make_float2(ref, sum);
-    float *dst = a.part + to * HD;
+    f32x4 *dst = reinterpret_cast<f32x4 *>(a.part) + (((long)split * P + hb) * ((R + 31) / 32) + w0 / 32) * (HD / 8) * 64 + lane;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4 *>(dst + 32 * d + 8 * j + 4 * h) = make_float4(o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]);
+      for (int j = 0; j < 4; ++j) dst[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
   } else {
     if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -727,18 +726,22 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   }
 }
 
-// The same for k_qattn_rows, whose rows are many and splits few: HD / 4 lanes for each row, eight
-// splits' parts in flight at a time.
+// The same for k_qattn_rows, whose rows are many and splits few: a workgroup joins 32 dims of 32 rows,
+// eight splits' parts in flight at a time.  Parts lie as that kernel's lanes hold them, [split][pair]
+// [32 rows][HD / 8][half wave][row] by four dims, so that both kernels move runs of 1 KB.
 template <int HD>
 __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
-  constexpr int TPR = HD / 4;
-  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, d = threadIdx.x % TPR * 4;
+  constexpr int DT = HD / 32;
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tile = blockIdx.x / DT, dt = blockIdx.x % DT;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = 32 * dt + 8 * wave + lane / 32 * 4;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int R = a.n * a.G, rows = m * a.G, r = tile * 32 + lane % 32;
   if (r >= rows) return;
   const int last = min(r / a.tile_rows * a.tile_rows + a.tile_rows, rows) - 1;
   const int used = splits_used(held + a.by_g(last) + 1, a.splits);
-  const long step = (long)a.B * a.KV * R, at = (long)hb * R + r;
+  const long step = (long)a.B * a.KV * R, at = (long)hb * R + r, R32 = (R + 31) / 32;
+  const long pstep = (long)a.B * a.KV * R32 * (HD / 8) * 64;
+  const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part) + ((hb * R32 + tile) * (HD / 8) + 4 * dt + wave) * 64 + lane;
   float mt = kNegInf, l = 0.f;
   f32x4 y = {0, 0, 0, 0};
   for (int s0 = 0; s0 < used; s0 += 8) {
@@ -746,9 +749,9 @@ __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
     f32x4 x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const long p = min(s0 + i, used - 1) * step + at;
-      z[i] = a.ml[p];
-      x[i] = *reinterpret_cast<const f32x4 *>(a.part + p * HD + d);
+      const int p = min(s0 + i, used - 1);
+      z[i] = a.ml[p * step + at];
+      x[i] = part[p * pstep];
     }
     float mn = mt;
 #pragma unroll
@@ -948,13 +951,13 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   // per wave of k_qattn)
   long splits = std::max<long>(1, ((many ? 2L : 1L) * ctx->num_cus + pairs * tiles - 1) / (pairs * tiles));
   splits = std::min<long>(splits, std::max(1, a.cap / kQBlock / 4));
-  const long per = pairs * R, ws = (long)ctx->part_elems;
+  const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
   // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
   // of at least two splits; else the weights compute them again from each row's sum
   const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
   const long side = !weigh ? 0 : logit ? per * a.cap : up4(per), plan = up4(2L * a.B);
-  splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + per * HD)));
+  splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   a.splits = (int)splits;
@@ -968,7 +971,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     a.plan = reinterpret_cast<int2 *>(at);
     at += plan;
     a.part = at;
-    a.ml = reinterpret_cast<float2 *>(at + splits * per * HD);
+    a.ml = reinterpret_cast<float2 *>(at + splits * padded * HD);
   }
   if (many) {
     if (pairs * tiles * splits > (1L << 24) - 1)
@@ -989,8 +992,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   if (splits > 1) {
     ProfScope ps(ctx, st, "fc_qattn_join");
     if (many) {
-      const int rpw = 1024 / HD;     // rows of a workgroup
-      hipLaunchKernelGGL(k_qattn_join_rows<HD>, dim3((unsigned)((R + rpw - 1) / rpw), (unsigned)pairs), dim3(256), 0, st, a);
+      hipLaunchKernelGGL(k_qattn_join_rows<HD>, dim3((unsigned)((R + 31) / 32 * (HD / 32)), (unsigned)pairs), dim3(256), 0, st, a);
       FC_LAUNCH_OK(st, "k_qattn_join_rows");
     } else {
       const long more = logit ? (a.cap + kWeightKeys - 1) / kWeightKeys : 0;
