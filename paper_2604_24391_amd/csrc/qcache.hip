@@ -284,91 +284,144 @@ __device__ __forceinline__ int pick_scan(int x, int *wsum, int &total) {
   return base + inc - x;
 }
 
-// The kept rows of one head in ascending order.  A radix select over 11, 11 and 10 bits of the
-// weights' keys finds the smallest kept key and how many rows of that key stay (the lowest ones);
-// then every wave counts, and writes down, what stays of its own run of rows.
+constexpr int kPickBins = 2048;
+// The digits of a key: bits 31-21, 20-10, 9-0.
+template <int STEP>
+struct Digit {
+  static constexpr int shift = STEP == 0 ? 21 : (STEP == 1 ? 10 : 0), bits = STEP == 2 ? 10 : 11;
+  __device__ static bool counts(uint32_t u, uint32_t prefix) {
+    if constexpr (STEP == 0) return u != 0u;
+    else return u >> (shift + bits) == prefix;
+  }
+  __device__ static int of(uint32_t u) { return u >> shift & ((1 << bits) - 1); }
+};
+// Places left in the selection: the digits of the smallest kept key found so far, and how many rows
+// of that prefix stay.
+struct Places {
+  uint32_t prefix;
+  int need;
+};
+// A digit more, from its counts: thread t holds those of bins 2047 - 2 t and 2046 - 2 t, so that a scan
+// runs from the largest key down.
+template <int STEP>
+__device__ __forceinline__ Places next_digit(Places p, int c0, int c1, int *wsum, int *found) {
+  int total;
+  const int bin = kPickBins - 1 - 2 * (int)threadIdx.x, before = pick_scan(c0 + c1, wsum, total);
+  if (before < p.need && before + c0 >= p.need) found[0] = bin, found[1] = p.need - before;
+  else if (before + c0 < p.need && before + c0 + c1 >= p.need) found[0] = bin - 1, found[1] = p.need - before - c0;
+  __syncthreads();
+  return Places{STEP == 0 ? (uint32_t)found[0] : p.prefix << Digit<STEP>::bits | (uint32_t)found[0], found[1]};
+}
+// f(row, its key) for the rows row0 + lane + 64 i, i < runs, of a wave.  Keys of rows that compete, [lo,
+// hi), are at least 0x00800000 (the lowest finite number's); the others, which stay whatever their
+// weight or lie behind the last row, get 0.  N loads at a time, the last ones repeated where the
+// run ends.
+template <int N, class F>
+__device__ __forceinline__ void each_key(const float *w, int row0, int runs, int lo, int hi, int cap, F f) {
+  const int lane = threadIdx.x & 63;
+  for (int i = 0; i < runs; i += N) {
+    const int j0 = row0 + 64 * i, j1 = row0 + 64 * runs;
+    float x[N];
+    if (j0 + 64 * N <= j1 && j0 >= lo && j0 + 64 * N <= hi) {      // all of them compete
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = w[j0 + lane + 64 * e];
+#pragma unroll
+      for (int e = 0; e < N; ++e) f(j0 + lane + 64 * e, weight_key(x[e]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = w[min(j0 + lane + 64 * e, cap - 1)];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int j = j0 + lane + 64 * e;
+        if (j0 + 64 * e < j1) f(j, j >= lo && j < hi ? weight_key(x[e]) : 0u);
+      }
+    }
+  }
+}
+// The kept ones of a workgroup's rows written down in order: those above the smallest kept key, those
+// that stay whatever their weight (key 0, below n), and of those that equal it what `need` leaves after
+// the `tie` before; `out` rows are kept before.  each(f) as each_key, a wave's rows behind those of the
+// waves before it.
+template <class Each>
+__device__ __forceinline__ void write_kept(Each each, Places p, int n, int keep, int out, int tie, int *wabove, int *wties,
+                                           int32_t *kept) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto stays = [&](int r, uint32_t u) { return u > p.prefix || (u == 0u && r < n); };
+  int above = 0, ties = 0;
+  each([&](int r, uint32_t u) {
+    above += __popcll(__ballot(stays(r, u)));
+    ties += __popcll(__ballot(u == p.prefix));
+  });
+  if (lane == 0) wabove[wave] = above, wties[wave] = ties;
+  __syncthreads();
+  for (int i = 0; i < wave; ++i) {
+    out += wabove[i] + min(max(p.need - tie, 0), wties[i]);
+    tie += wties[i];
+  }
+  const unsigned long long below = (1ull << lane) - 1ull;
+  each([&](int r, uint32_t u) {
+    const unsigned long long t = __ballot(u == p.prefix);
+    const bool stay = stays(r, u) || (u == p.prefix && tie + __popcll(t & below) < p.need);
+    tie += __popcll(t);
+    const unsigned long long k = __ballot(stay);
+    const int to = out + __popcll(k & below);
+    out += __popcll(k);
+    if (stay && to < keep) kept[to] = r;
+  });
+}
+
+// The kept rows of one head in ascending order, by one workgroup.  A radix select over 11, 11 and 10
+// bits of the weights' keys finds the smallest kept key and how many rows of that key stay (the lowest
+// ones); then every wave counts, and writes down, what stays of its own run of rows.
 // Weights share few exponents, so the first digit's counts stand in 16 copies, one for every
-// fourth lane: one copy had the lanes of a wave wait for each other (166 us for 65536 rows
-// against 27).  IT > 0: a lane holds IT keys in registers (up to 1024 IT rows); IT = 0 reads the
-// weights anew in each pass.
+// fourth lane: with one copy the lanes of a wave wait for each other.  IT > 0: a lane holds IT keys in
+// registers (up to 1024 IT rows); IT = 0 reads the weights anew in each pass.
 template <int IT>
 __global__ __launch_bounds__(kPickThreads) void k_qevict_pick(EvictArgs a) {
-  constexpr int BINS = 2048, COPIES = IT == 4 ? 4 : 16;   // fewer to clear and to add up for few rows
-  __shared__ __align__(16) int hist[BINS * COPIES];   // 128 KB of 16 copies: one workgroup on a CU
-  __shared__ int wsum[kPickWaves], wabove[kPickWaves], wties[kPickWaves];
-  __shared__ int s_digit, s_need;
+  constexpr int COPIES = IT == 4 ? 4 : 16;            // fewer to clear and to add up for few rows
+  __shared__ __align__(16) int hist[kPickBins * COPIES];  // 128 KB of 16 copies: one workgroup on a CU
+  __shared__ int wsum[kPickWaves], wabove[kPickWaves], wties[kPickWaves], found[2];
   const int b = blockIdx.x / a.KV, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = q_held(a.len, b, a.cap);
   const float *w = a.weight + (long)blockIdx.x * a.cap;
   int32_t *kept = a.kept + (long)blockIdx.x * a.keep;
-  const int left = min(n, a.keep);
-  if (a.left && tid == 0 && blockIdx.x % a.KV == 0) a.left[b] = left;
+  if (a.left && tid == 0 && blockIdx.x % a.KV == 0) a.left[b] = min(n, a.keep);
   if (n <= a.keep) {
     for (int j = tid; j < a.keep; j += kPickThreads) kept[j] = j < n ? j : -1;
     return;
   }
   const int lo = a.sink, hi = n - a.recent;              // rows that compete: [lo, hi)
   const int take = a.keep - a.sink - a.recent;           // < hi - lo
-
-  // Keys of rows that compete are at least 0x00800000 (the lowest finite number's); the others,
-  // which stay whatever their weight or lie behind the last row, get 0.
-  // a wave's run of rows: `runs` times 64, row = first + 64 i
-  const int runs = IT ? IT : (n + kPickThreads - 1) / kPickThreads;
-  const int first = wave * runs * 64 + lane;
-  auto load = [&](int i) {
-    const int j = first + 64 * i;
-    const uint32_t u = weight_key(w[min(j, a.cap - 1)]);   // no branch: the loads of a pass overlap
-    return j >= lo && j < hi ? u : 0u;
-  };
+  const int runs = IT ? IT : (n + kPickThreads - 1) / kPickThreads, row0 = wave * runs * 64;
   uint32_t key[IT ? IT : 1];
 #pragma unroll
-  for (int i = 0; i < IT; ++i) key[i] = load(i);
-  auto each = [&](auto f) {                    // f(row, its key)
+  for (int i = 0; i < IT; ++i) {
+    const int j = row0 + lane + 64 * i;
+    const uint32_t u = weight_key(w[min(j, a.cap - 1)]);   // no branch: the loads overlap
+    key[i] = j >= lo && j < hi ? u : 0u;
+  }
+  auto each = [&](auto f) {
     if constexpr (IT > 0) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) f(first + 64 * i, key[i]);
+      for (int i = 0; i < IT; ++i) f(row0 + lane + 64 * i, key[i]);
     } else {
-      // 16 loads at a time, the last ones repeated where the run ends
-      for (int i = 0; i < runs; i += 16) {
-        const int j0 = wave * runs * 64 + 64 * i, j1 = wave * runs * 64 + 64 * runs;
-        float x[16];
-        if (j0 + 1024 <= j1 && j0 >= lo && j0 + 1024 <= hi) {      // all of them compete
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = w[j0 + lane + 64 * e];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) f(j0 + lane + 64 * e, weight_key(x[e]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = w[min(j0 + lane + 64 * e, a.cap - 1)];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = j0 + lane + 64 * e;
-            if (j0 + 64 * e < j1) f(j, j >= lo && j < hi ? weight_key(x[e]) : 0u);
-          }
-        }
-      }
+      each_key<16>(w, row0, runs, lo, hi, a.cap, f);
     }
   };
-
-  uint32_t prefix = ~0u;               // no row competes for a place: none is above or ties
-  int need = take;
+  Places p{~0u, take};                 // take 0: no row is above or ties
   if (take > 0) {
     auto digit = [&](auto tag) {
-      constexpr int step = decltype(tag)::value;           // bits 31-21, 20-10, 9-0
-      constexpr int shift = step == 0 ? 21 : (step == 1 ? 10 : 0), copies = step == 0 ? COPIES : 1;
-      constexpr uint32_t mask = step == 2 ? 1023u : 2047u;
-      for (int x = tid; x < BINS * copies / 4; x += kPickThreads) reinterpret_cast<int4 *>(hist)[x] = make_int4(0, 0, 0, 0);
+      constexpr int step = decltype(tag)::value, copies = step == 0 ? COPIES : 1;
+      for (int x = tid; x < kPickBins * copies / 4; x += kPickThreads) reinterpret_cast<int4 *>(hist)[x] = make_int4(0, 0, 0, 0);
       __syncthreads();
       each([&](int, uint32_t u) {
-        if (step == 0 ? u != 0u : u >> (step == 1 ? 21 : 10) == prefix)
-          atomicAdd(&hist[(u >> shift & mask) * copies + (step == 0 ? lane & (COPIES - 1) : 0)], 1);
+        if (Digit<step>::counts(u, p.prefix)) atomicAdd(&hist[Digit<step>::of(u) * copies + (step == 0 ? lane & (COPIES - 1) : 0)], 1);
       });
       __syncthreads();
-      // thread t: bins 2047 - 2 t and 2046 - 2 t, so that a scan runs from the largest key down
       int c[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int bin = BINS - 1 - 2 * tid - e;
+        const int bin = kPickBins - 1 - 2 * tid - e;
         c[e] = 0;
         if constexpr (step == 0) {
 #pragma unroll
@@ -380,43 +433,133 @@ __global__ __launch_bounds__(kPickThreads) void k_qevict_pick(EvictArgs a) {
           c[e] = hist[bin];
         }
       }
-      int total;
-      const int before = pick_scan(c[0] + c[1], wsum, total);
-      if (before < need && before + c[0] >= need) s_digit = BINS - 1 - 2 * tid, s_need = need - before;
-      else if (before + c[0] < need && before + c[0] + c[1] >= need) s_digit = BINS - 2 - 2 * tid, s_need = need - before - c[0];
-      __syncthreads();
-      prefix = step == 0 ? (uint32_t)s_digit : prefix << (step == 1 ? 11 : 10) | (uint32_t)s_digit;
-      need = s_need;
+      p = next_digit<step>(p, c[0], c[1], wsum, found);
     };
     digit(std::integral_constant<int, 0>{});
     digit(std::integral_constant<int, 1>{});
     digit(std::integral_constant<int, 2>{});
   }
-  // rows above the smallest kept key, and the first `need` rows equal to it: counted for each wave's
-  // run, then written behind what the waves before keep
-  auto stays = [&](int r, uint32_t u) { return u > prefix || (u == 0u && r < n); };
-  int above = 0, ties = 0;
-  each([&](int r, uint32_t u) {
-    above += __popcll(__ballot(stays(r, u)));
-    ties += __popcll(__ballot(u == prefix));
-  });
-  if (lane == 0) wabove[wave] = above, wties[wave] = ties;
-  __syncthreads();
-  int out = 0, tie = 0;
-  for (int i = 0; i < wave; ++i) {
-    out += wabove[i] + min(max(need - tie, 0), wties[i]);
-    tie += wties[i];
+  write_kept(each, p, n, a.keep, 0, 0, wabove, wties, kept);
+}
+
+// The same by `parts` workgroups of each head, a kernel to a digit: each counts its own rows, the next
+// one adds the parts' counts up and finds the digit; the last one also finds from them how many rows
+// stay before its own.  The counts of a head are read by as many workgroups as it has, which share an
+// XCD's L2 where the heads are a multiple of 8 (heads fastest: workgroups go round the 8 in turn).
+constexpr int kMaxParts = 8;
+struct PickArgs {
+  EvictArgs e;
+  int *count;                          // [head][3 digits][part][kPickBins]
+  Places *places;                      // [head][2]: after the first and the second digit
+  int *above;                          // [head][part] rows above the prefix of the first two digits
+  int parts;
+};
+// Counts of a digit's bins 2046 - 2 t (x) and 2047 - 2 t (y) in every part.
+struct PartCounts {
+  int2 c[kMaxParts];
+  int c0 = 0, c1 = 0;                  // y and x summed
+};
+__device__ __forceinline__ int *part_bins(const PickArgs &a, int step, int part) {
+  return a.count + (((long)blockIdx.x * 3 + step) * a.parts + part) * kPickBins + kPickBins - 2 - 2 * (int)threadIdx.x;
+}
+__device__ __forceinline__ PartCounts all_parts(const PickArgs &a, int step) {
+  PartCounts p;
+#pragma unroll
+  for (int i = 0; i < kMaxParts; ++i) p.c[i] = *reinterpret_cast<const int2 *>(part_bins(a, step, min(i, a.parts - 1)));
+#pragma unroll
+  for (int i = 0; i < kMaxParts; ++i)
+    if (i < a.parts) p.c0 += p.c[i].y, p.c1 += p.c[i].x;
+  return p;
+}
+// A wave's rows: from row0 on, `runs` times 64; its workgroup's start at `start`.
+struct PartRows {
+  int start, row0, runs;
+};
+__device__ __forceinline__ PartRows part_rows(const PickArgs &a, int n) {
+  const int runs = (n + kPickThreads * a.parts - 1) / (kPickThreads * a.parts), start = blockIdx.y * runs * kPickThreads;
+  return PartRows{start, start + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * runs * 64, runs};
+}
+
+template <int STEP>
+__global__ __launch_bounds__(kPickThreads) void k_qevict_count(PickArgs a) {
+  constexpr int COPIES = STEP == 0 ? 4 : 1;
+  __shared__ __align__(16) int hist[kPickBins * COPIES];
+  __shared__ int wsum[kPickWaves], found[2];
+  const EvictArgs &e = a.e;
+  const int head = blockIdx.x, tid = threadIdx.x, n = q_held(e.len, head / e.KV, e.cap);
+  const int take = e.keep - e.sink - e.recent;
+  if (n <= e.keep || take == 0) return;
+  for (int x = tid; x < kPickBins * COPIES / 4; x += kPickThreads) reinterpret_cast<int4 *>(hist)[x] = make_int4(0, 0, 0, 0);
+  Places p{~0u, take};
+  if constexpr (STEP > 0) {
+    if (STEP == 2) p = a.places[head * 2];
+    const PartCounts c = all_parts(a, STEP - 1);
+    p = next_digit<STEP - 1>(p, c.c0, c.c1, wsum, found);
+    if (blockIdx.y == 0 && tid == 0) a.places[head * 2 + STEP - 1] = p;
   }
-  const unsigned long long below = (1ull << lane) - 1ull;
-  each([&](int r, uint32_t u) {
-    const unsigned long long t = __ballot(u == prefix);
-    const bool stay = stays(r, u) || (u == prefix && tie + __popcll(t & below) < need);
-    tie += __popcll(t);
-    const unsigned long long k = __ballot(stay);
-    const int to = out + __popcll(k & below);
-    out += __popcll(k);
-    if (stay && to < a.keep) kept[to] = r;
+  __syncthreads();
+  const PartRows rows = part_rows(a, n);
+  int above = 0;
+  each_key<8>(e.weight + (long)head * e.cap, rows.row0, rows.runs, e.sink, n - e.recent, e.cap, [&](int, uint32_t u) {
+    if (Digit<STEP>::counts(u, p.prefix)) atomicAdd(&hist[Digit<STEP>::of(u) * COPIES + (tid & (COPIES - 1))], 1);
+    if constexpr (STEP == 2) above += u >> Digit<2>::bits > p.prefix;
   });
+  __syncthreads();
+  int c[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int bin = kPickBins - 2 - 2 * tid + i;
+    if constexpr (COPIES == 4) {
+      const int4 y = reinterpret_cast<const int4 *>(hist)[bin];
+      c[i] = y.x + y.y + y.z + y.w;
+    } else {
+      c[i] = hist[bin];
+    }
+  }
+  *reinterpret_cast<int2 *>(part_bins(a, STEP, blockIdx.y)) = make_int2(c[0], c[1]);
+  if constexpr (STEP == 2) {
+    int total;
+    pick_scan(above, wsum, total);
+    if (tid == 0) a.above[head * a.parts + blockIdx.y] = total;
+  }
+}
+
+__global__ __launch_bounds__(kPickThreads) void k_qevict_write(PickArgs a) {
+  __shared__ int wsum[kPickWaves], wabove[kPickWaves], wties[kPickWaves], found[2];
+  const EvictArgs &e = a.e;
+  const int head = blockIdx.x, part = blockIdx.y, b = head / e.KV, tid = threadIdx.x, n = q_held(e.len, b, e.cap);
+  int32_t *kept = e.kept + (long)head * e.keep;
+  if (e.left && tid == 0 && head % e.KV == 0 && part == 0) e.left[b] = min(n, e.keep);
+  if (n <= e.keep) {
+    for (int j = part * kPickThreads + tid; j < e.keep; j += a.parts * kPickThreads) kept[j] = j < n ? j : -1;
+    return;
+  }
+  const int lo = e.sink, hi = n - e.recent, take = e.keep - e.sink - e.recent;
+  const PartRows rows = part_rows(a, n);
+  // rows kept before this part's: those whatever their weight, those above the smallest kept key, ties
+  int out = min(rows.start, lo) + max(min(rows.start, n) - hi, 0), tie = 0;
+  Places p{~0u, 0};
+  if (take > 0) {
+    const PartCounts c = all_parts(a, 2);
+    p = next_digit<2>(a.places[head * 2 + 1], c.c0, c.c1, wsum, found);
+    const int digit = p.prefix & 1023u, top = kPickBins - 1 - 2 * tid;
+    int above = 0, ties = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxParts; ++i)
+      if (i < part) {
+        above += (top > digit ? c.c[i].y : 0) + (top - 1 > digit ? c.c[i].x : 0);
+        ties += (top == digit ? c.c[i].y : 0) + (top - 1 == digit ? c.c[i].x : 0);
+      }
+    if (tid < part) above += a.above[head * a.parts + tid];
+    int total;
+    pick_scan(above, wsum, total);
+    out += total;
+    __syncthreads();
+    pick_scan(ties, wsum, tie);
+    out += min(p.need, tie);
+  }
+  const float *w = e.weight + (long)head * e.cap;
+  write_kept([&](auto f) { each_key<8>(w, rows.row0, rows.runs, lo, hi, e.cap, f); }, p, n, e.keep, out, tie, wabove, wties, kept);
 }
 
 // One block of 64 kept rows of one head: gathered, scaled anew, written.  Key rows are read alone;
@@ -572,9 +715,27 @@ fc_status launch_qcache_evict(fc_ctx *ctx, const fc_qcache &s, const fc_qcache &
   a.len = len, a.kept = kept, a.left = len_out;
   a.KV = s.n_kv_heads, a.cap = s.capacity, a.cap2 = d.capacity;
   a.keep = keep, a.sink = sink, a.recent = recent;
-  {
+  // the workgroups of a head: as many as run at once, each with 4096 rows at least, where their counts fit
+  const long heads = (long)B * a.KV;
+  long parts = std::min<long>(std::min<long>(kMaxParts, a.cap / 4096), std::max<long>(1, 2L * ctx->num_cus / heads));
+  parts = std::min<long>(parts, ((long)ctx->part_elems - (4 + kMaxParts) * heads) / (heads * 3 * kPickBins));
+  if (a.cap > 16 * kPickThreads && parts > 1) {
+    PickArgs p{a, reinterpret_cast<int *>(ctx->part), nullptr, nullptr, (int)parts};
+    p.places = reinterpret_cast<Places *>(p.count + heads * 3 * parts * kPickBins);
+    p.above = reinterpret_cast<int *>(p.places + 2 * heads);
+    const dim3 grid((unsigned)heads, (unsigned)parts), block(kPickThreads);
     ProfScope ps(ctx, st, "fc_qevict_pick");
-    const dim3 grid((unsigned)(B * a.KV)), block(kPickThreads);
+    hipLaunchKernelGGL(k_qevict_count<0>, grid, block, 0, st, p);
+    FC_LAUNCH_OK(st, "k_qevict_count");
+    hipLaunchKernelGGL(k_qevict_count<1>, grid, block, 0, st, p);
+    FC_LAUNCH_OK(st, "k_qevict_count");
+    hipLaunchKernelGGL(k_qevict_count<2>, grid, block, 0, st, p);
+    FC_LAUNCH_OK(st, "k_qevict_count");
+    hipLaunchKernelGGL(k_qevict_write, grid, block, 0, st, p);
+    FC_LAUNCH_OK(st, "k_qevict_write");
+  } else {
+    ProfScope ps(ctx, st, "fc_qevict_pick");
+    const dim3 grid((unsigned)heads), block(kPickThreads);
     if (a.cap <= 4 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<4>, grid, block, 0, st, a);
     else if (a.cap <= 16 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<16>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(k_qevict_pick<0>, grid, block, 0, st, a);
