@@ -786,9 +786,10 @@ constexpr int kWaveKeys = 64, kGroupKeys = 4 * kWaveKeys;
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpart, int row_splits) {
   constexpr int PC = HD / 8;                    // 16-byte pieces of a query row
-  constexpr int TILE = 32 * HD * 2, DMAS = TILE / 16 / 256;
+  constexpr int ROWS = 64;                      // of a stage: two products' worth between barriers
+  constexpr int TILE = ROWS * HD * 2, DMAS = TILE / 16 / 256;
   __shared__ __align__(1024) uint8_t sm[3][TILE];
-  __shared__ float sm_l[3][4][64];              // a wave's copy of the tile's row sums, twice
+  __shared__ float sm_l[3][4][ROWS];            // a wave's copy of the stage's row sums
   const int P = a.B * a.KV, R = a.n * a.G;
   const int hb = blockIdx.x % P, rest = blockIdx.x / P, rs = rest % row_splits, j0 = rest / row_splits * kGroupKeys;
   const int b = hb / a.KV, kv = hb % a.KV;
@@ -796,8 +797,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int rows = m * a.G, seen = held + m;
   if (m == 0 || j0 >= seen) return;
-  // row tiles that see a key of the group, and this workgroup's part of them
-  const int t0 = (int)((long)max(0, j0 - held) * a.G / 32), t1 = (rows + 31) / 32;
+  // stages of rows that see a key of the group, and this workgroup's part of them
+  const int t0 = (int)((long)max(0, j0 - held) * a.G / ROWS), t1 = (rows + ROWS - 1) / ROWS;
   const int lo = t0 + (int)((long)(t1 - t0) * rs / row_splits), hi = t0 + (int)((long)(t1 - t0) * (rs + 1) / row_splits);
 
   const int w0 = j0 + kWaveKeys * wave, blk = min(w0, a.cap - kQBlock) / kQBlock;
@@ -813,58 +814,41 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
       k[t][2 * i] = dequant8(w[0], w[1], ks);
       k[t][2 * i + 1] = dequant8(w[2], w[3], ks);
     }
-  // where each of this lane's pieces comes from: 32 rows on with each tile, over the other heads
-  // wherever a token ends; rows behind the last one are read as the last one
-  const uint16_t *qb = a.q + ((long)b * a.n * a.H + kv * a.G) * HD;
+  // a stage's rows lie over the tokens from that of its first row on; rows behind the last one are
+  // read as the last one
   const float *lse = a.lse + (long)hb * R;
-  const int step_t = a.by_g(32), step_g = 32 - step_t * a.G;
-  const long skip = (long)(a.H - a.G) * HD, step_p = 32L * HD + step_t * skip;
-  const uint16_t *src[DMAS];
-  int head[DMAS];
-#pragma unroll
-  for (int i = 0; i < DMAS; ++i) {
-    const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = lo * 32 + row, tok = a.by_g(r);
-    const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
-    head[i] = r - tok * a.G;
-    src[i] = qb + (long)tok * skip + (long)r * HD + piece * 8;
-  }
-  int filled = lo;                    // tile that the pointers stand at
-  auto fetch = [&](int stage) {
+  const int skip = (a.H - a.G) * HD;  // from a token's last head of the group to the next one's first
+  auto fetch = [&](int tile, int stage) {
+    const int t = __builtin_amdgcn_readfirstlane(a.by_g(tile * ROWS)), g = tile * ROWS - t * a.G, last = rows - 1 - tile * ROWS;
+    const uint16_t *qb = a.q + (((long)b * a.n + t) * a.H + kv * a.G) * HD;
 #pragma unroll
     for (int i = 0; i < DMAS; ++i) {
-      const uint16_t *at = src[i];
-      if (filled * 32 + 32 > rows) {
-        const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(filled * 32 + row, rows - 1);
-        at = qb + (long)a.by_g(r) * skip + (long)r * HD + ((p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) * 8;
-      }
-      dma16(at, lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
-      src[i] += step_p;
-      head[i] += step_g;
-      if (head[i] >= a.G) head[i] -= a.G, src[i] += skip;
+      const int p = (wave * DMAS + i) * 64 + lane, row = p / PC, r = min(row, last) + g;
+      const int piece = (p % PC) ^ (HD == 128 ? row & 15 : (row >> 1) & 7);
+      dma16(qb + (unsigned)(a.by_g(r) * skip + r * HD + piece * 8), lds_addr(&sm[stage][(wave * DMAS + i) * 1024]));
     }
-    dma4(lse + min(filled * 32 + l32, rows - 1), lds_addr(&sm_l[stage][wave][0]));
-    ++filled;
+    dma4(lse + min(tile * ROWS + lane, rows - 1), lds_addr(&sm_l[stage][wave][0]));
   };
-  const float c = a.flip ? -a.c : a.c;   // the queries' signs are as they came
   f32x16 acc[2];
+  const float c = a.flip ? -a.c : a.c;   // the queries' signs are as they came
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   loads_done();
-  if (lo < hi) fetch(0);
-  if (lo + 1 < hi) fetch(1);
+  if (lo < hi) fetch(lo, 0);
+  if (lo + 1 < hi) fetch(lo + 1, 1);
   const int qx = HD == 128 ? l32 & 15 : (l32 >> 1) & 7;
-  bf16x8 q[HD / 16];                  // the coming tile's rows, and their sums
+  bf16x8 q[HD / 16];                  // the coming 32 rows, and their sums
   float L = 0.f;
-  auto queries = [&](int st) {
-    const uint8_t *qt = sm[st] + l32 * HD * 2;
+  auto queries = [&](int st, int half) {
+    const uint8_t *qt = sm[st] + (32 * half + l32) * HD * 2;
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
       for (int x = 0; x < 2; ++x)     // piece of 8 elements: dims (2 i + h) 16 + 8 x
         q[2 * i + x] = *reinterpret_cast<const bf16x8 *>(qt + ((2 * (2 * i + h) + x) ^ qx) * 16);
-    return sm_l[st][wave][l32];
+    L = sm_l[st][wave][32 * half + l32];
   };
   auto arrived = [&](bool ahead) {
     if (ahead) wait_vm<DMAS + 1>();
@@ -873,44 +857,50 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   };
   if (lo < hi) {
     arrived(lo + 1 < hi);
-    L = queries(0);
+    queries(0, 0);
   }
   int stage = 0;
   for (int tile = lo; tile < hi; ++tile) {
     const int next = stage == 2 ? 0 : stage + 1;
-    if (tile + 2 < hi) fetch(next == 2 ? 0 : next + 1);
-    f32x16 s[2];
+    if (tile + 2 < hi) fetch(tile + 2, next == 2 ? 0 : next + 1);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int half = 0; half < 2; ++half) {
+      const int r0 = tile * ROWS + 32 * half;
+      f32x16 s[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < HD / 16; ++i) {
-      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][i], q[i], s[0], 0, 0, 0);
-      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][i], q[i], s[1], 0, 0, 0);
-    }
-    const float sub = L;
-    if (tile + 1 < hi) {
-      arrived(tile + 2 < hi);
-      L = queries(next);
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][i], q[i], s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][i], q[i], s[1], 0, 0, 0);
+      }
+      const float sub = L;
+      if (half == 0) {
+        queries(stage, 1);
+      } else if (tile + 1 < hi) {
+        arrived(tile + 2 < hi);
+        queries(next, 0);
+      }
+      const int r = r0 + l32;
+      if (r0 + 32 <= rows && w0 + kWaveKeys <= held + a.by_g(r0) + 1) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], c, -sub));
+      } else {
+        const int see = r < rows ? held + a.by_g(r) + 1 : 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float p = exp2_fast(fmaf(s[t][e], c, -sub));
+            acc[t][e] += w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4 < see ? p : 0.f;
+          }
+      }
     }
     stage = next;
-    const int r = tile * 32 + l32;
-    if (tile * 32 + 32 <= rows && w0 + kWaveKeys <= held + a.by_g(tile * 32) + 1) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[t][e] += exp2_fast(fmaf(s[t][e], c, -sub));
-    } else {
-      const int see = r < rows ? held + a.by_g(r) + 1 : 0;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = exp2_fast(fmaf(s[t][e], c, -sub));
-          acc[t][e] += w0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4 < see ? p : 0.f;
-        }
-    }
   }
   // Summed over the 32 rows of a half wave: at each step a lane hands half of its keys' sums to the
   // lane across and adds that one's other half, until it holds one key's.
