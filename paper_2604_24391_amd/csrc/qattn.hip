@@ -209,7 +209,11 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) vw[d] = load16<NT>(vbase + (long)blk * (HD * kQBlock) + 16 * d * kQBlock);
   };
+  // mask bytes of the lane's 16 keys, a block ahead as well
+  const uint8_t *mbase = a.mask ? a.mask + (long)b * a.cap + g * 16 : nullptr;
+  u32x4 mw = {~0u, ~0u, ~0u, ~0u};
   const int at0 = min(blo + wave, nblk - 1);
+  if (mbase) mw = *reinterpret_cast<const u32x4 *>(mbase + at0 * kQBlock);
   load_k(at0);
   load_v(at0);
   float ks = ksb[at0], vs = vsb[at0];
@@ -238,10 +242,10 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     const bool full = !a.mask && j0 + kQBlock <= kall;
     uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};      // the lane's 16 keys that some row may see, by bytes
     if (!full) {
-      if (a.mask) {
-        const u32x4 mw = *reinterpret_cast<const u32x4 *>(a.mask + (long)b * a.cap + j0 + g * 16);
+      if (mbase) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) vis[i] = set_bytes(mw[i]);
+        mw = *reinterpret_cast<const u32x4 *>(mbase + next * kQBlock);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -391,7 +395,6 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   }
   // one workgroup saw every key of these rows: their weights too (the scores it wrote above)
   if (MT == 1 && a.logit && a.splits == 1) {
-    __threadfence();
     __syncthreads();
     for (int j = tid; j < kmax; j += 256) {
       float w = 0.f;
