@@ -65,10 +65,9 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
-// Bytes of w that hold a NaN (0x7f or 0xff), as 0x01 each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
-}
+// Bytes of w that hold a NaN (0x7f or 0xff): their top bits, and as 0x01 each.
+__device__ __forceinline__ uint32_t nan_tops(uint32_t w) { return (w & 0x7F7F7F7Fu) + 0x01010101u; }
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return nan_tops(w) >> 7 & 0x01010101u; }
 // The four low bits of such bytes, side by side.
 __device__ __forceinline__ uint32_t byte_bits(uint32_t n) { return (n * 0x01020408u) >> 24 & 15u; }
 // The four low bits of b as bytes of 0xff.
@@ -259,20 +258,27 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     if (!full) {
       uint32_t any = 0;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        uint32_t bits = 0;
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           vw[d][i] &= vis[i];
-          const uint32_t n = nan_bytes(vw[d][i]);
-          vw[d][i] &= ~(n * 255u);
-          bits |= byte_bits(n) << (4 * i);
+          any |= nan_tops(vw[d][i]);
         }
-        reinterpret_cast<part16 *>(&sm_nan[wave][16 * d + l16])[g] = (uint16_t)bits;
-        any |= bits;
+      odd = __any((any & 0x80808080u) != 0);
+      if (odd) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t n = nan_bytes(vw[d][i]);
+            vw[d][i] &= ~(n * 255u);
+            bits |= byte_bits(n) << (4 * i);
+          }
+          reinterpret_cast<part16 *>(&sm_nan[wave][16 * d + l16])[g] = (uint16_t)bits;
+        }
+        wave_lds_order();
       }
-      odd = __any(any != 0);
-      wave_lds_order();
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -525,7 +531,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
       }
     const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
-    uint32_t mine = ~0u, any = 0;    // the lane's 32 keys that some row may see; NaN among them
+    uint32_t mine = ~0u;             // the lane's 32 keys that some row may see
+    uint32_t odd = 0;                // those of its halves where some value is NaN
     if (part) {
       mine = (uint32_t)(seen_bits(wmax - j0) >> (32 * h));
       if (a.mask) {
@@ -569,17 +576,29 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
       for (int d = 0; d < DT; ++d)
         vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + t) ^ vx) * 16)]);
       if (part) {                    // as in k_qattn
+        uint32_t any = 0;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          uint32_t bits = 0;
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t vis = bit_bytes(mine >> (16 * t + 4 * x));
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t w = vw[d][x] & bit_bytes(mine >> (16 * t + 4 * x)), n = nan_bytes(w);
-            vw[d][x] = w & ~(n * 255u);
-            bits |= byte_bits(n) << (4 * x);
+          for (int d = 0; d < DT; ++d) {
+            vw[d][x] &= vis;
+            any |= nan_tops(vw[d][x]);
           }
-          reinterpret_cast<part16 *>(&sm_nan[wave][32 * d + l32])[2 * h + t] = (uint16_t)bits;
-          any |= bits;
+        }
+        if (__any((any & 0x80808080u) != 0)) {
+          odd |= 0xFFFFu << (16 * t);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t n = nan_bytes(vw[d][x]);
+              vw[d][x] &= ~(n * 255u);
+              bits |= byte_bits(n) << (4 * x);
+            }
+            reinterpret_cast<part16 *>(&sm_nan[wave][32 * d + l32])[2 * h + t] = (uint16_t)bits;
+          }
         }
       }
 #pragma unroll
@@ -596,9 +615,9 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][2 * i], vw[d][2 * i + 1], vs), p, o[d], 0, 0, 0);
       }
     }
-    if (part && __any(any != 0)) {
-      const uint32_t other = __shfl_xor(mine, 32);
-      const uint64_t keys = ((uint64_t)(h ? mine : other) << 32 | (h ? other : mine)) & seen_bits(seen - j0);
+    if (odd) {
+      const uint32_t keep = mine & odd, other = __shfl_xor(keep, 32);
+      const uint64_t keys = ((uint64_t)(h ? keep : other) << 32 | (h ? other : keep)) & seen_bits(seen - j0);
       wave_lds_order();
 #pragma unroll
       for (int d = 0; d < DT; ++d)
