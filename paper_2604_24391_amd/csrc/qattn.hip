@@ -98,13 +98,17 @@ __device__ __forceinline__ int splits_used(int kmax, int splits) {
 }
 // k_qattn deals a.slots workgroups of each key-value head over the items by their lengths, `per`
 // blocks to each: with the same number for every item, the longest one of a ragged batch would
-// keep few CUs busy to the end.  Items take ceil(blocks / per) slots in order; per = ceil(all
-// blocks / (slots - items)) leaves room for what the quotients round up, and at least four blocks
-// (one per wave) to a slot.
+// keep few CUs busy to the end.  Items take ceil(blocks / per) slots in order; per is the smallest
+// number with which they suffice, but at least four blocks (one per wave).
 struct Share {
   int item, start, used, per;       // the item, its first slot, its slots, blocks of each
   int held, m;                      // its rows held and new
 };
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return __builtin_amdgcn_readfirstlane(x);
+}
 // The share of the item that slot `slot` falls to (item -1: none).
 __device__ __forceinline__ Share share_of(const QAttnArgs &a, int slot) {
   const int lane = threadIdx.x & 63;
@@ -115,21 +119,36 @@ __device__ __forceinline__ Share share_of(const QAttnArgs &a, int slot) {
     m = min(a.n_new ? min(max(a.n_new[j], 0), a.n) : a.n, a.cap - held);
     return i + lane < a.B && m > 0 ? (held + m + kQBlock - 1) / kQBlock : 0;
   };
-  const int room = max(1, a.slots - a.B);
+  if (a.slots == a.B) {               // one workgroup for each item
+    held = q_held(a.len, slot, a.cap), m = q_new(a.n_new, slot, a.n, held, a.cap);
+    return Share{m > 0 ? slot : -1, slot, 1, a.cap / kQBlock, held, m};
+  }
   int x = blocks(0);
   if (a.B == 1) {
     const int n = __builtin_amdgcn_readfirstlane(x), per = max(4, (n + a.slots - 1) / a.slots), used = (n + per - 1) / per;
     return Share{slot < used ? 0 : -1, 0, used, per, __builtin_amdgcn_readfirstlane(held), __builtin_amdgcn_readfirstlane(m)};
   }
-  unsigned all = (unsigned)x;         // below 2^30 for a cache of 2^42 bytes, the largest there is
-  for (int i = 64; i < a.B; i += 64) all += (unsigned)blocks(i);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
+  // (counts below 2^30: a cache of 2^42 bytes is the largest there is)
+  auto slots_of = [&](int per) {      // per 0: the blocks themselves
+    int all = 0;
+    for (int i = 0; i < a.B; i += 64) {
+      if (a.B > 64) x = blocks(i);
+      all += wave_sum(per ? (int)((unsigned)(x + per - 1) / (unsigned)per) : x);
+    }
+    return all;
+  };
+  const int all = slots_of(0);
+  int lo = max(4, (all + a.slots - 1) / a.slots), hi = max(lo, (all + a.slots - a.B - 1) / (a.slots - a.B));
+  while (lo < hi) {                   // hi suffices: the quotients round up by less than one each
+    const int mid = (lo + hi) / 2;
+    if (slots_of(mid) <= a.slots) hi = mid;
+    else lo = mid + 1;
+  }
+  const int per = lo;
   if (a.B > 64) x = blocks(0);
-  const unsigned per = a.slots > a.B ? max(4u, (all + room - 1) / (unsigned)room) : 1u << 30;
   int run = 0;
   for (int i = 0;;) {
-    const int u = (int)(((unsigned)x + per - 1) / per);
+    const int u = (int)((unsigned)(x + per - 1) / (unsigned)per);
     int inc = u;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -140,12 +159,12 @@ __device__ __forceinline__ Share share_of(const QAttnArgs &a, int slot) {
     const unsigned long long hit = __ballot(slot >= at && slot < at + u);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      return Share{i + l, __builtin_amdgcn_readlane(at, l), __builtin_amdgcn_readlane(u, l), (int)per,
+      return Share{i + l, __builtin_amdgcn_readlane(at, l), __builtin_amdgcn_readlane(u, l), per,
                    __builtin_amdgcn_readlane(held, l), __builtin_amdgcn_readlane(m, l)};
     }
     run += __builtin_amdgcn_readlane(inc, 63);
     i += 64;
-    if (i >= a.B) return Share{-1, 0, 0, (int)per, 0, 0};
+    if (i >= a.B) return Share{-1, 0, 0, per, 0, 0};
     x = blocks(i);
   }
 }
@@ -162,9 +181,9 @@ __device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 
 // several times what HBM delivers), so loads run ahead: each next block's keys are read when the
 // scores have used theirs, its values after the outputs.
 //
-// NT: loads without a place in the memory-side cache.  A cache larger than that (256 MB) is 76.6
-// instead of 83.8 us for eight items of 53 k rows; one that fits, and is there from the step before,
-// would be 26 instead of 22 us for sixteen of 3 k.
+// NT: loads without a place in the memory-side cache, for caches well beyond its 256 MB: 433 MB take
+// 75.6 us so and 83.6 otherwise, 337 MB 67.2 and 61.5, 54 MB 25.2 and 20.8 (part of what fits is
+// still there from the step before).
 template <bool NT>
 __device__ __forceinline__ u32x4 load16(const uint8_t *p) {
   const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
@@ -389,7 +408,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         y[e] = sm_o[0][row][d + e] + sm_o[1][row][d + e] + sm_o[2][row][d + e] + sm_o[3][row][d + e];
-      if (a.splits > 1) {
+      if (a.part) {
         *reinterpret_cast<float4 *>(a.part + (slot * R + r) * HD + d) =
             make_float4(y[0], y[1], y[2], y[3]);
       } else {
@@ -400,7 +419,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     }
   }
   // one workgroup saw every key of these rows: their weights too (the scores it wrote above)
-  if (MT == 1 && a.logit && a.splits == 1) {
+  if (MT == 1 && a.logit && !a.part) {
     __syncthreads();
     for (int j = tid; j < kmax; j += 256) {
       float w = 0.f;
@@ -960,31 +979,43 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const bool many = R > 64;
   const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4), tile = many ? 128 : 16 * MT;
   const long tiles = (R + tile - 1) / tile;
-  // k_qattn: workgroups for one on every CU, if that leaves four blocks (one per wave) to each;
-  // k_qattn_rows: as many as run at once, two on a CU
-  long splits = many ? 2L * ctx->num_cus / (pairs * tiles) : (ctx->num_cus + pairs * tiles - 1) / (pairs * tiles);
-  splits = std::min<long>(splits, a.cap / kQBlock / (many ? kRowsBlocks : 4));
   const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
   // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
-  // of at least two splits; else the weights compute them again from each row's sum
+  // of two slots an item; else the weights compute them again from each row's sum
   const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
   const long side = !weigh ? 0 : logit ? per * a.cap : up4(per), plan = up4(2L * a.B);
-  splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
+  long splits = 1, slots = a.B;
+  if (many) {
+    // as many workgroups as run at once, two on a CU
+    splits = std::min<long>(2L * ctx->num_cus / (pairs * tiles), a.cap / kQBlock / kRowsBlocks);
+    splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
+  } else {
+    // One workgroup's loads keep a CU's path to memory busy; two, where a mask adds vector work to
+    // each block, where head_dim 64 halves the loads in flight, or where an item would have fewer
+    // than four slots and their lengths come out uneven (long caches: 8 items of 4 heads 72.7 us
+    // with one, 75.6 with two; 19 of 8 heads 51.0 and 46.1, masked 69 and 50; 37 of 4 heads of 64
+    // dims 39.7 and 36.9).  Four blocks at least to a slot, one per wave.
+    slots = ctx->num_cus / a.KV;
+    if (a.mask || HD == 64 || slots < 4L * a.B) slots = 2L * ctx->num_cus / a.KV;
+    slots = std::min<long>(slots, a.cap / kQBlock / 4 * a.B);
+    slots = std::max<long>(a.B, std::min<long>(slots, (ws - side - plan - 4) / (a.KV * R * (HD + 2))));
+  }
+  const bool parts = many ? splits > 1 : slots > a.B;
   a.splits = (int)splits;
   a.tile_rows = tile;
-  a.slots = many ? 0 : (int)(splits * a.B);
+  a.slots = many ? 0 : (int)slots;
   float *at = ctx->part;
   if (logit) a.logit = at;
   else if (weigh) a.lse = at;
   at += side;
-  if (splits > 1) {
+  if (parts) {
     a.plan = reinterpret_cast<int2 *>(at);
     at += plan;
     a.part = at;
-    a.ml = reinterpret_cast<float2 *>(at + splits * padded * HD);
+    a.ml = reinterpret_cast<float2 *>(at + (many ? splits * padded : slots * a.KV * R) * HD);
   }
   if (many) {
     if (pairs * tiles * splits > (1L << 24) - 1)
@@ -995,14 +1026,14 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   } else {
     const dim3 grid((unsigned)a.slots, (unsigned)a.KV);
     ProfScope ps(ctx, st, "fc_qattn");
-    const bool big = pairs * a.cap * HD * 2 > (256L << 20);
+    const bool big = pairs * a.cap * HD * 2 > (384L << 20);
     if (MT == 1 && big) hipLaunchKernelGGL((k_qattn<HD, 1, true>), grid, dim3(256), 0, st, a);
     else if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1, false>), grid, dim3(256), 0, st, a);
     else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2, false>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_qattn<HD, 4, false>), grid, dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn");
   }
-  if (splits > 1) {
+  if (parts) {
     ProfScope ps(ctx, st, "fc_qattn_join");
     if (many) {
       hipLaunchKernelGGL(k_qattn_join_rows<HD>, dim3((unsigned)((R + 31) / 32 * (HD / 32)), (unsigned)pairs), dim3(256), 0, st, a);
