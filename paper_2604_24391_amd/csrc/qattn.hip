@@ -534,6 +534,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
     wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
     lds_barrier();                   // every wave has left the other stage
     if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1);
+    if (w0 >= rows) continue;        // it only brings its part of the blocks
     const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
     const float ks_next = ksb[ahead], vs_next = vsb[ahead];
     f32x16 s[2];
@@ -976,8 +977,8 @@ __global__ __launch_bounds__(256) void k_qattn_weight_add(QAttnArgs a, const flo
 template <int HD>
 fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const long R = (long)a.n * a.G, pairs = (long)a.B * a.KV;
-  const bool many = R > 64;
-  const int MT = R <= 16 ? 1 : (R <= 32 ? 2 : 4), tile = many ? 128 : 16 * MT;
+  const bool many = R > 32;
+  const int MT = R <= 16 ? 1 : 2, tile = many ? 128 : 16 * MT;
   const long tiles = (R + tile - 1) / tile;
   const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
@@ -1029,8 +1030,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     const bool big = pairs * a.cap * HD * 2 > (384L << 20);
     if (MT == 1 && big) hipLaunchKernelGGL((k_qattn<HD, 1, true>), grid, dim3(256), 0, st, a);
     else if (MT == 1) hipLaunchKernelGGL((k_qattn<HD, 1, false>), grid, dim3(256), 0, st, a);
-    else if (MT == 2) hipLaunchKernelGGL((k_qattn<HD, 2, false>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_qattn<HD, 4, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_qattn<HD, 2, false>), grid, dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn");
   }
   if (parts) {
