@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   constexpr int OS = HD + 4;
   __shared__ float sm_o[4][16][OS];
   __shared__ float2 sm_ml[4][16 * MT];
-  __shared__ float sm_l[16], sm_lse[16];
+  __shared__ float sm_l[16], sm_lse[16 * MT];
   __shared__ uint64_t sm_nan[4][HD];
   const Share sh = share_of(a, blockIdx.x);
   if (sh.item < 0) return;
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
           s[x][e] = y;
           top = fmaxf(top, y);
         }
-      if (MT == 1 && a.logit && seen[t]) {
+      if (a.logit && seen[t]) {
         float *to = a.logit + ((long)hb * R + 16 * t + l16) * a.cap + j0 + g * 16;
 #pragma unroll
         for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4 *>(to + 4 * x) = s[x];
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
       if (a.ml && rt + l16 < rows) a.ml[slot * R + rt + l16] = make_float2(mt, l);
       if (a.lse && rt + l16 < rows) a.lse[(long)hb * R + rt + l16] = log_sum(mt, l);
       sm_l[l16] = l;
-      sm_lse[l16] = log_sum(mt, l);
+      sm_lse[rt + l16] = log_sum(mt, l);
     }
     __syncthreads();
     for (int x = tid; x < 16 * HD / 4; x += 256) {
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
     }
   }
   // one workgroup saw every key of these rows: their weights too (the scores it wrote above)
-  if (MT == 1 && a.logit && !a.part) {
+  if (a.logit && !a.part) {
     __syncthreads();
     for (int j = tid; j < kmax; j += 256) {
       float w = 0.f;
@@ -674,17 +674,18 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
 }
 
 // The splits of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
-// by the sum.  With scores written down (R <= 16 rows), further workgroups turn them into the
+// by the sum.  With scores written down (R <= 32 rows), further workgroups turn them into the
 // weight that each key receives: 4 R bytes a key written and read, against the 2 R hd multiplications
 // and the hd bytes of the keys that computing them again costs.
-constexpr int kWeightKeys = 1024;
+constexpr int kWeightKeys = 256;
 
 template <int HD>
 __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) {
   constexpr int TPR = HD / 4, SG = 256 / TPR;
   __shared__ float sm_y[SG][HD];
   __shared__ float2 sm_ml[SG];
-  __shared__ float sm_lse[16];
+  __shared__ float sm_lse[32];
+  __shared__ f32x4 sm_w[4][kWeightKeys / 4];
   const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tid = threadIdx.x;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
   const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x;
@@ -732,35 +733,40 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
   const int j0 = (r - join_rows) * kWeightKeys, seen = held + m;
   if (m == 0 || j0 >= seen) return;
   {
-    // 16 threads to a row
-    const int row = tid / 16;
+    // 8 threads to a row
+    const int row = tid / 8;
     float mt = kNegInf, l = 0.f;
     if (row < rows)
-      for (int s = tid % 16; s < used; s += 16) {
+      for (int s = tid % 8; s < used; s += 8) {
         const float2 z = a.ml[s * step + at0 + row];
         const float mn = fmaxf(mt, z.x), ref = mn == kNegInf ? 0.f : mn;
         l = l * exp2_fast(mt - ref) + z.y * exp2_fast(z.x - ref);
         mt = mn;
       }
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
+    for (int o = 1; o < 8; o <<= 1) {
       const float m2 = __shfl_xor(mt, o), l2 = __shfl_xor(l, o);
       const float mn = fmaxf(mt, m2), ref = mn == kNegInf ? 0.f : mn;
       l = l * exp2_fast(mt - ref) + l2 * exp2_fast(m2 - ref);
       mt = mn;
     }
-    if (tid % 16 == 0) sm_lse[row] = log_sum(mt, l);
+    if (tid % 8 == 0) sm_lse[row] = log_sum(mt, l);
   }
   __syncthreads();
-  const int j = j0 + 4 * tid;
-  if (j >= seen) return;
+  // 64 threads of four keys each for every fourth row
+  const int lane = tid & 63, part = tid >> 6, j = j0 + 4 * lane;
   f32x4 w = {0, 0, 0, 0};
-  for (int i = 0; i < rows; ++i) {
-    const f32x4 y = *reinterpret_cast<const f32x4 *>(a.logit + ((long)hb * R + i) * a.cap + j);
-    const float L = sm_lse[i];
+  if (j < seen)
+    for (int i = part; i < rows; i += 4) {
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(a.logit + ((long)hb * R + i) * a.cap + j);
+      const float L = sm_lse[i];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] += prob(y[e], L);
-  }
+      for (int e = 0; e < 4; ++e) w[e] += prob(y[e], L);
+    }
+  sm_w[part][lane] = w;
+  __syncthreads();
+  if (part || j >= seen) return;
+  w = (w + sm_w[1][lane]) + (sm_w[2][lane] + sm_w[3][lane]);
   float *to = a.weight + (long)hb * a.cap + j;
   if (j + 4 <= seen) {
     *reinterpret_cast<f32x4 *>(to) += w;
@@ -982,9 +988,9 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const long tiles = (R + tile - 1) / tile;
   const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
-  // scores of 16 rows or fewer are written down for the weights, where they fit beside the parts
+  // scores of 32 rows or fewer are written down for the weights, where they fit beside the parts
   // of two slots an item; else the weights compute them again from each row's sum
-  const bool logit = weigh && MT == 1 && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
+  const bool logit = weigh && !many && per * a.cap + 2 * up4(2 * per) + 2 * per * HD + up4(2L * a.B) <= ws;
   const long side = !weigh ? 0 : logit ? per * a.cap : up4(per), plan = up4(2L * a.B);
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
