@@ -175,11 +175,13 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 }
 __device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 0.f : exp2_fast(y - L); }
 
-// All rows of an item (MT tiles of 16) against a run of its key blocks, which go round the 4 waves;
-// these are joined in LDS.  One split writes the outputs, several their parts.
+// All rows of an item (MT tiles of 16: up to 32) against a run of its key blocks, which go round the 4
+// waves; these are joined in LDS.  An item's only slot writes the outputs, several their parts.
 // Memory bounds it (MT = 1: about 1000 vector cycles for a block's 16 KB, at 8 waves on a CU
 // several times what HBM delivers), so loads run ahead: each next block's keys are read when the
-// scores have used theirs, its values after the outputs.
+// scores have used theirs, its values after the outputs.  Eight items of 40000 to 65535 rows (433 MB)
+// 70 us, 6.1 TB/s; sixteen of 2200 to 4200 (54 MB, in the memory-side cache) 16 us; one of 2176 7 us,
+// most of it the launch and one pass of latencies.
 //
 // NT: loads without a place in the memory-side cache, for caches well beyond its 256 MB: 433 MB take
 // 75.6 us so and 83.6 otherwise, 337 MB 67.2 and 61.5, 54 MB 25.2 and 20.8 (part of what fits is
@@ -429,10 +431,16 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   }
 }
 
-// Many rows: 4 waves of 32 rows each share the key blocks, which the DMA brings into LDS a block
+// More than 32 rows: 4 waves of 32 each share the key blocks, which the DMA brings into LDS a block
 // ahead (16 KB each at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
 // back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
 // a lane holds one row and, of a block's keys, the 32 of its half wave.
+// Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 PFLOP) take 638 us, the
+// first call after a pause 800: the card's power bounds it.  Blocks converted once per workgroup
+// (689), scores a block ahead of the softmax, three waves on a SIMD or 64 rows in a wave come out
+// the same or slower: what they save in cycles goes in clock (without the exponentials, 8 % of it;
+// without the keys' conversion, 5).  256 tokens over 2176 rows: 23 us of latencies, a block after the
+// other in each workgroup.
 //
 // LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks.
@@ -673,8 +681,8 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   }
 }
 
-// The splits of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
-// by the sum.  With scores written down (R <= 32 rows), further workgroups turn them into the
+// The parts of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
+// by the sum; 4 to 5 us beside a launch's 3.6.  With scores written down (R <= 32 rows), further workgroups turn them into the
 // weight that each key receives: 4 R bytes a key written and read, against the 2 R hd multiplications
 // and the hd bytes of the keys that computing them again costs.
 constexpr int kWeightKeys = 256;
@@ -777,7 +785,8 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
 
 // The same for k_qattn_rows, whose rows are many and splits few: a workgroup joins 32 dims of 32 rows,
 // eight splits' parts in flight at a time.  Parts lie as that kernel's lanes hold them, [split][pair]
-// [32 rows][HD / 8][half wave][row] by four dims, so that both kernels move runs of 1 KB.
+// [32 rows][HD / 8][half wave][row] by four dims, so that both kernels move runs of 1 KB (7168 rows of
+// four parts, 15 MB: 5.8 us; that kernel writes rows of 512 bytes 3 us slower).
 template <int HD>
 __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
   constexpr int DT = HD / 32;
@@ -825,10 +834,13 @@ __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
 }
 
 // The weight that each key receives, from scores computed again: 4 waves hold 64 keys each in
-// registers, as bfloat16, and the rows' queries pass by in tiles of 32 through LDS.  S^T puts the
-// keys in a lane's registers, so its sums over rows stay there until the end.  One exponential
-// for every two matrix cycles: the vector unit bounds it.  Row ranges are dealt over
-// `row_splits` workgroups, whose sums the next kernel adds up in order.
+// registers, as bfloat16, and the rows' queries pass by through LDS, 64 between barriers (32: 10 %
+// slower).  S^T puts the keys in a lane's registers, so its sums over rows stay there until the end.
+// Row ranges are dealt over `row_splits` workgroups, whose sums the next kernel adds up in order.
+// A prompt of 8192 rows (0.24 PFLOP) takes 311 us, 38 % of the matrix unit's cycles: the other terms,
+// an exponential and two more vector instructions for 32 matrix cycles, and one barrier for 64 rows,
+// add to the products rather than hide behind them at two waves on a SIMD (254 registers: the keys
+// are 64, scores and sums 64); without the exponentials it is a tenth faster.
 constexpr int kWaveKeys = 64, kGroupKeys = 4 * kWaveKeys;
 
 template <int HD>
