@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kPickThreads) void k_qevict_write(PickArgs a) {
 // One block of 64 kept rows of one head: gathered, scaled anew, written.  Key rows are read alone;
 // values lie by columns, so each source block with a kept row in it is read whole (8 KB at hd
 // 128), four at a time through LDS, where single bytes cost nothing.  Memory bounds it: 32 heads,
-// 16384 of 62000 rows each (the values whole, 254 MB, keys 67, written 134) 123 us, 3.7 TB/s.  Two
+// 16384 of 62000 rows each (400 MB read, by the counters, and 137 written) 123 us, 4.4 TB/s.  Two
 // blocks at a time 142, eight 156 (LDS leaves fewer workgroups); neighbours on one XCD, or loads past
 // the memory-side cache: no gain.
 template <int HD>
