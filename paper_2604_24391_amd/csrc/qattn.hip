@@ -46,6 +46,7 @@ struct QAttnArgs {
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, tile_rows, slots;
+  int *queue, pieces;                // k_qattn_rows: [8] pieces of work taken behind the first ones, or null
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
 };
@@ -464,8 +465,28 @@ __device__ __forceinline__ void dma4(const void *gp, uint32_t lds) {
       : "memory");
 }
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
+// The kernel's arguments read anew, which keeps no register between two reads.
+__device__ __forceinline__ QAttnArgs args_again() {
+  typedef const __attribute__((address_space(4))) uint32_t *Words;
+  Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  struct { uint32_t w[sizeof(QAttnArgs) / 4]; } x;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(QAttnArgs) / 4); ++i) x.w[i] = p[i];
+  return __builtin_bit_cast(QAttnArgs, x);
+}
+
+// Pieces of work are numbered by pairs (item and key-value head), then splits, then tiles of rows, the
+// last rows, which see most keys, first.  Workgroups go round the 8 XCDs in turn and start in order:
+// an XCD that kept to its pairs, as P is often a multiple of 8, would make the others wait whenever its
+// items are the longer ones, so the pairs move on by one with each round of them (8 items of 10 to
+// 4000 rows: 244 to 135 us; all of one length: up to 1 % slower).
+// QUEUE: as many workgroups as run at once, each going on with the next piece of its XCD's pairs, whose
+// keys are in its L2, then with the others' (queue[8]: pieces taken).  Sixteen frames of 704 to 1024
+// tokens, seven rounds: 548 us, 587 without; but a last round that is not full falls to few CUs (equal
+// items, 3.5 rounds: 392 and 357), so only ragged batches of four rounds or more go this way.
+template <int HD, bool QUEUE>
+__global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs args) {
   constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
   constexpr int DT = HD / 32;                   // output tiles of 32 dims
   constexpr int TILE = kQBlock * HD;            // bytes of a block's keys, and of its values
@@ -474,212 +495,233 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs a) {
   __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
   __shared__ uint64_t sm_nan[4][HD];
   __shared__ __align__(16) uint8_t sm_mask[STAGES][4][256];
-  // pairs fastest: an XCD (workgroups go round the 8 in turn) keeps to few pairs' keys; the
-  // longest rows first
-  const int P = a.B * a.KV, R = a.n * a.G;
-  const int hb = blockIdx.x % P, rest = blockIdx.x / P, split = rest % a.splits;
-  const int r0 = ((R + 127) / 128 - 1 - rest / a.splits) * 128;
-  const int b = hb / a.KV, kv = hb % a.KV;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
-  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
-  const int rows = m * a.G;
-  if (r0 >= rows) return;
-  const int kmax = held + a.by_g(min(r0 + 128, rows) - 1) + 1;
-  const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
-  if (split >= used) return;
-  const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
+  auto work = [&](const QAttnArgs &a, int id) {
+    const int P = a.B * a.KV, R = a.n * a.G;
+    const int rest = id / P, hb = QUEUE ? id % P : (id % P + rest) % P, split = rest % a.splits;
+    const int r0 = ((R + 127) / 128 - 1 - rest / a.splits) * 128;
+    const int b = hb / a.KV, kv = hb % a.KV;
+    const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+    const int rows = m * a.G;
+    if (r0 >= rows) return;
+    const int kmax = held + a.by_g(min(r0 + 128, rows) - 1) + 1;
+    const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
+    if (split >= used) return;
+    const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
-  const long nblk = a.cap / kQBlock;
-  const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
-  const uniform_floats ksb = as_uniform(a.ks + hb * nblk), vsb = as_uniform(a.vs + hb * nblk);
-  int ksrc[DMAS], vsrc[DMAS];
+    const long nblk = a.cap / kQBlock;
+    const uint8_t *kbase = a.k + (long)hb * a.cap * HD, *vbase = a.v + (long)hb * a.cap * HD;
+    const uniform_floats ksb = as_uniform(a.ks + hb * nblk), vsb = as_uniform(a.vs + hb * nblk);
+    int ksrc[DMAS], vsrc[DMAS];
 #pragma unroll
-  for (int i = 0; i < DMAS; ++i) {
-    const int p = (wave * DMAS + i) * 64 + lane, kr = p / PC, vr = p / 4;
-    ksrc[i] = kr * HD + ((p % PC) ^ key_swz<HD>(kr)) * 16;
-    vsrc[i] = vr * kQBlock + ((p & 3) ^ val_swz(vr)) * 16;
-  }
-  auto fetch = [&](int blk, int stage) {
-    const long at = (long)blk * TILE;
-#pragma unroll
-    for (int i = 0; i < DMAS; ++i) dma16(kbase + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
-#pragma unroll
-    for (int i = 0; i < DMAS; ++i) dma16(vbase + at + vsrc[i], lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
-    // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
-    if (a.mask) dma4(a.mask + (long)b * a.cap + blk * kQBlock + (lane & 15) * 4, lds_addr(&sm_mask[stage][wave][0]));
-  };
-
-  const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
-  const int seen = r < rows ? held + tok + 1 : 0;                              // keys that the lane's row sees
-  const int wmax = w0 < rows ? held + a.by_g(min(w0 + 32, rows) - 1) + 1 : 0;  // that any row of the wave sees
-  const int wall = held + a.by_g(w0) + 1;                                      // that every one does
-  const long at_q = (((long)b * a.n + tok) * a.H + head) * HD;
-  bf16x8 q[HD / 16];
-  {
-    const uint16_t *src = a.q + at_q;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i) {
-      q[2 * i] = load_q(src + (2 * i + h) * 16, a.flip);
-      q[2 * i + 1] = load_q(src + (2 * i + h) * 16 + 8, a.flip);
+    for (int i = 0; i < DMAS; ++i) {
+      const int p = (wave * DMAS + i) * 64 + lane, kr = p / PC, vr = p / 4;
+      ksrc[i] = kr * HD + ((p % PC) ^ key_swz<HD>(kr)) * 16;
+      vsrc[i] = vr * kQBlock + ((p & 3) ^ val_swz(vr)) * 16;
     }
-  }
-  loads_done();
-  fetch(blo, 0);
+    auto fetch = [&](int blk, int stage) {
+      const long at = (long)blk * TILE;
+#pragma unroll
+      for (int i = 0; i < DMAS; ++i) dma16(kbase + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
+#pragma unroll
+      for (int i = 0; i < DMAS; ++i) dma16(vbase + at + vsrc[i], lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
+      // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
+      if (a.mask) dma4(a.mask + (long)b * a.cap + blk * kQBlock + (lane & 15) * 4, lds_addr(&sm_mask[stage][wave][0]));
+    };
 
-  // S^T row x of tile t is key ((x / 4) % 2) 32 + 16 t + x / 8 4 + x % 4
-  const int kr = ((l32 >> 2) & 1) * 32 + (l32 >> 3) * 4 + (l32 & 3);
-  const int koff = kr * HD, kx = key_swz<HD>(kr), voff = l32 * kQBlock, vx = val_swz(l32);
-  f32x16 o[DT];
+    const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
+    const int seen = r < rows ? held + tok + 1 : 0;                              // keys that the lane's row sees
+    const int wmax = w0 < rows ? held + a.by_g(min(w0 + 32, rows) - 1) + 1 : 0;  // that any row of the wave sees
+    const int wall = held + a.by_g(w0) + 1;                                      // that every one does
+    const long at_q = (((long)b * a.n + tok) * a.H + head) * HD;
+    bf16x8 q[HD / 16];
+    {
+      const uint16_t *src = a.q + at_q;
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-  float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
+      for (int i = 0; i < HD / 32; ++i) {
+        q[2 * i] = load_q(src + (2 * i + h) * 16, a.flip);
+        q[2 * i + 1] = load_q(src + (2 * i + h) * 16 + 8, a.flip);
+      }
+    }
+    loads_done();
+    fetch(blo, 0);
 
-  int stage = 0;
-  float ks = ksb[blo], vs = vsb[blo];
-  for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
-    wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
-    lds_barrier();                   // every wave has left the other stage
-    if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1);
-    if (w0 >= rows) continue;        // it only brings its part of the blocks
-    const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
-    const float ks_next = ksb[ahead], vs_next = vsb[ahead];
-    f32x16 s[2];
+    // S^T row x of tile t is key ((x / 4) % 2) 32 + 16 t + x / 8 4 + x % 4
+    const int kr = ((l32 >> 2) & 1) * 32 + (l32 >> 3) * 4 + (l32 & 3);
+    const int koff = kr * HD, kx = key_swz<HD>(kr), voff = l32 * kQBlock, vx = val_swz(l32);
+    f32x16 o[DT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(&sm[stage][0][koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16)]);
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
-      }
-    const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
-    uint32_t mine = ~0u;             // the lane's 32 keys that some row may see
-    uint32_t odd = 0;                // those of its halves where some value is NaN
-    if (part) {
-      mine = (uint32_t)(seen_bits(wmax - j0) >> (32 * h));
-      if (a.mask) {
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const u32x4 mw = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16 * i]);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) bits |= byte_bits(set_bytes(mw[x]) & 0x01010101u) << (16 * i + 4 * x);
-        }
-        mine &= bits;
-      }
-      const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
+
+    int stage = 0;
+    float ks = ksb[blo], vs = vsb[blo];
+    for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
+      wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
+      lds_barrier();                   // every wave has left the other stage
+      if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1);
+      if (w0 >= rows) continue;        // it only brings its part of the blocks
+      const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
+      const float ks_next = ksb[ahead], vs_next = vsb[ahead];
+      f32x16 s[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
-    }
-    float top = kNegInf;
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
-    // the reference follows the maximum only where it is 2^8 behind: no sum comes near
-    // float32's limits, and most blocks need not touch O
-    if (__any(top > ref + 8.f)) {
-      const float mn = fmaxf(ref, top), corr = exp2_fast(ref - (mn == kNegInf ? 0.f : mn));
-      ref = mn;
-      sum *= corr;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= corr;
-    }
-    const float sub = ref == kNegInf ? 0.f : ref;
-    // 16 keys of the lane at a time: their values, their exponentials, their products
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      u32x4 vw[DT];
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + t) ^ vx) * 16)]);
-      if (part) {                    // as in k_qattn
-        uint32_t any = 0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t vis = bit_bytes(mine >> (16 * t + 4 * x));
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            vw[d][x] &= vis;
-            any |= nan_tops(vw[d][x]);
-          }
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 w = *reinterpret_cast<const u32x4 *>(&sm[stage][0][koff + t * 16 * HD + (((2 * i + h) ^ kx) * 16)]);
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
         }
-        if (__any((any & 0x80808080u) != 0)) {
-          odd |= 0xFFFFu << (16 * t);
+      const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
+      uint32_t mine = ~0u;             // the lane's 32 keys that some row may see
+      uint32_t odd = 0;                // those of its halves where some value is NaN
+      if (part) {
+        mine = (uint32_t)(seen_bits(wmax - j0) >> (32 * h));
+        if (a.mask) {
+          uint32_t bits = 0;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            uint32_t bits = 0;
+          for (int i = 0; i < 2; ++i) {
+            const u32x4 mw = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16 * i]);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t n = nan_bytes(vw[d][x]);
-              vw[d][x] &= ~(n * 255u);
-              bits |= byte_bits(n) << (4 * x);
-            }
-            reinterpret_cast<part16 *>(&sm_nan[wave][32 * d + l32])[2 * h + t] = (uint16_t)bits;
+            for (int x = 0; x < 4; ++x) bits |= byte_bits(set_bytes(mw[x]) & 0x01010101u) << (16 * i + 4 * x);
           }
+          mine &= bits;
         }
+        const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
       }
+      float top = kNegInf;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        bf16x8 p;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float y = exp2_fast(fmaf(s[t][8 * i + e], a.c, -sub));
-          sum += y;
-          p[e] = (__bf16)y;
-        }
+        for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
+      // the reference follows the maximum only where it is 2^8 behind: no sum comes near
+      // float32's limits, and most blocks need not touch O
+      if (__any(top > ref + 8.f)) {
+        const float mn = fmaxf(ref, top), corr = exp2_fast(ref - (mn == kNegInf ? 0.f : mn));
+        ref = mn;
+        sum *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= corr;
+      }
+      const float sub = ref == kNegInf ? 0.f : ref;
+      // 16 keys of the lane at a time: their values, their exponentials, their products
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        u32x4 vw[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][2 * i], vw[d][2 * i + 1], vs), p, o[d], 0, 0, 0);
+          vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][voff + d * 32 * kQBlock + (((2 * h + t) ^ vx) * 16)]);
+        if (part) {                    // as in k_qattn
+          uint32_t any = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t vis = bit_bytes(mine >> (16 * t + 4 * x));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              vw[d][x] &= vis;
+              any |= nan_tops(vw[d][x]);
+            }
+          }
+          if (__any((any & 0x80808080u) != 0)) {
+            odd |= 0xFFFFu << (16 * t);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              uint32_t bits = 0;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t n = nan_bytes(vw[d][x]);
+                vw[d][x] &= ~(n * 255u);
+                bits |= byte_bits(n) << (4 * x);
+              }
+              reinterpret_cast<part16 *>(&sm_nan[wave][32 * d + l32])[2 * h + t] = (uint16_t)bits;
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          bf16x8 p;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float y = exp2_fast(fmaf(s[t][8 * i + e], a.c, -sub));
+            sum += y;
+            p[e] = (__bf16)y;
+          }
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(vw[d][2 * i], vw[d][2 * i + 1], vs), p, o[d], 0, 0, 0);
+        }
       }
+      if (odd) {
+        const uint32_t keep = mine & odd, other = __shfl_xor(keep, 32);
+        const uint64_t keys = ((uint64_t)(h ? keep : other) << 32 | (h ? other : keep)) & seen_bits(seen - j0);
+        wave_lds_order();
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (sm_nan[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4] & keys) o[d][e] = __builtin_nanf("");
+      }
+      ks = ks_next, vs = vs_next;
     }
-    if (odd) {
-      const uint32_t keep = mine & odd, other = __shfl_xor(keep, 32);
-      const uint64_t keys = ((uint64_t)(h ? keep : other) << 32 | (h ? other : keep)) & seen_bits(seen - j0);
-      wave_lds_order();
+
+    sum += __shfl_xor(sum, 32);
+    if (r >= rows) return;
+    const long at = (long)hb * R + r;
+    if (a.splits > 1) {
+      const long to = (long)split * P * R + at;
+      if (h == 0) a.ml[to] = make_float2(ref, sum);
+      f32x4 *dst = reinterpret_cast<f32x4 *>(a.part) + (((long)split * P + hb) * ((R + 31) / 32) + w0 / 32) * (HD / 8) * 64 + lane;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (sm_nan[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4] & keys) o[d][e] = __builtin_nanf("");
+        for (int j = 0; j < 4; ++j) dst[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    } else {
+      if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t *dst = a.out + at_q;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x4 w = {(__bf16)(o[d][4 * j] * inv), (__bf16)(o[d][4 * j + 1] * inv), (__bf16)(o[d][4 * j + 2] * inv), (__bf16)(o[d][4 * j + 3] * inv)};
+          *reinterpret_cast<bf16x4 *>(dst + 32 * d + 8 * j + 4 * h) = w;
+        }
     }
-    ks = ks_next, vs = vs_next;
-  }
-
-  sum += __shfl_xor(sum, 32);
-  if (r >= rows) return;
-  const long at = (long)hb * R + r;
-  if (a.splits > 1) {
-    const long to = (long)split * P * R + at;
-    if (h == 0) a.ml[to] = make_float2(ref, sum);
-    f32x4 *dst = reinterpret_cast<f32x4 *>(a.part) + (((long)split * P + hb) * ((R + 31) / 32) + w0 / 32) * (HD / 8) * 64 + lane;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) dst[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+  };
+  if constexpr (!QUEUE) {
+    work(args, blockIdx.x);
   } else {
-    if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t *dst = a.out + at_q;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x4 w = {(__bf16)(o[d][4 * j] * inv), (__bf16)(o[d][4 * j + 1] * inv), (__bf16)(o[d][4 * j + 2] * inv), (__bf16)(o[d][4 * j + 3] * inv)};
-        *reinterpret_cast<bf16x4 *>(dst + 32 * d + 8 * j + 4 * h) = w;
+    __shared__ int sm_next;
+    int id = blockIdx.x, from = blockIdx.x % 8;
+    for (int done = 0;;) {             // queues found empty
+      const QAttnArgs a = args_again();
+      work(a, id);
+      for (;;) {
+        __syncthreads();
+        if (tid == 0) sm_next = (int)gridDim.x + 8 * atomicAdd(&a.queue[from], 1) + from;
+        __syncthreads();
+        id = __builtin_amdgcn_readfirstlane(sm_next);
+        if (id < a.pieces) break;
+        if (++done == 8) return;
+        from = (from + 1) % 8;
       }
+    }
   }
 }
+
+__global__ void k_qattn_queue(int *queue) { queue[threadIdx.x] = 0; }
 
 // The parts of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
 // by the sum; 4 to 5 us beside a launch's 3.6.  With scores written down (R <= 32 rows), further workgroups turn them into the
@@ -851,7 +893,7 @@ __global__ __launch_bounds__(256, 2) void k_qattn_weight(QAttnArgs a, float *wpa
   __shared__ __align__(1024) uint8_t sm[3][TILE];
   __shared__ float sm_l[3][4][ROWS];            // a wave's copy of the stage's row sums
   const int P = a.B * a.KV, R = a.n * a.G;
-  const int hb = blockIdx.x % P, rest = blockIdx.x / P, rs = rest % row_splits, j0 = rest / row_splits * kGroupKeys;
+  const int rest = blockIdx.x / P, hb = (blockIdx.x % P + rest) % P, rs = rest % row_splits, j0 = rest / row_splits * kGroupKeys;
   const int b = hb / a.KV, kv = hb % a.KV;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
@@ -1039,8 +1081,16 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   if (many) {
     if (pairs * tiles * splits > (1L << 24) - 1)
       return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
+    a.pieces = (int)(pairs * tiles * splits);
+    const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;   // workgroups that run at once
+    if (a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
+      a.queue = reinterpret_cast<int *>(at);
+      hipLaunchKernelGGL(k_qattn_queue, dim3(1), dim3(8), 0, st, a.queue);
+      FC_LAUNCH_OK(st, "k_qattn_queue");
+    }
     ProfScope ps(ctx, st, "fc_qattn_rows");
-    hipLaunchKernelGGL(k_qattn_rows<HD>, dim3((unsigned)(pairs * tiles * splits)), dim3(256), 0, st, a);
+    if (a.queue) hipLaunchKernelGGL((k_qattn_rows<HD, true>), dim3((unsigned)once), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_qattn_rows<HD, false>), dim3((unsigned)a.pieces), dim3(256), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn_rows");
   } else {
     const dim3 grid((unsigned)a.slots, (unsigned)a.KV);

@@ -261,6 +261,54 @@ def test_attention_many_ragged_items(fc, ctx, heads, n):
     run_attention(fc, ctx, g, heads, B, n, cap, held, [min(x, cap - h) for x, h in zip(new, held)])
 
 
+@pytest.mark.parametrize("heads,n,B,cap", [("qwen", 20, 300, 192), ("wide", 26, 400, 128)])
+def test_attention_many_rounds_of_workgroups(fc, ctx, heads, n, B, cap):
+    """Ragged batches of several times the workgroups that run at once: every item against products in
+    64 bits (the tolerance of check_attention), tokens that do not count left alone, replays equal."""
+    g = torch.Generator().manual_seed(50)
+    H, kv, hd, _ = HEADS[heads]
+    cache = filled(fc, g, B, kv, hd, cap)
+    q = randn(g, B, n, H, hd)
+    new = [(b * 5) % (n + 1) for b in range(B)]
+    held = [0 if b % 50 == 7 else (b * b * 3) % (cap - n) for b in range(B)]
+    before, k, v = cache.weight.clone(), cache.rows().double(), cache.rows(values=True).double()
+    lens, m_new, out = ints(held), ints(new), torch.full_like(q, 9.0)
+    call = lambda: fc.fc_qcache_attention(ctx, cache, q, lens, m_new, out, accumulate=True)  # noqa: E731
+    call()
+    first, weight = out.clone(), cache.weight.clone()
+    for b in range(B):
+        m, rows, G = new[b], held[b] + new[b], H // kv
+        assert bool((out[b, m:] == 9.0).all())
+        if m == 0:
+            assert torch.equal(weight[b], before[b])
+            continue
+        kk, vv = k[b, :, :rows].repeat_interleave(G, 0), v[b, :, :rows].repeat_interleave(G, 0)
+        qq = q[b, :m].double().transpose(0, 1).contiguous()
+        hide = torch.arange(rows, device="cuda")[None] > held[b] + torch.arange(m, device="cuda")[:, None]
+        p = (torch.matmul(qq, kk.transpose(1, 2).contiguous()) * hd ** -0.5).masked_fill(hide, float("-inf")).softmax(-1)
+        mass = float((torch.matmul(qq.abs(), kk.abs().transpose(1, 2).contiguous()) * hd ** -0.5).max())
+        rel = 4 * (hd + 4) * 2.0 ** -24 * mass + 2.0 ** -22 + rows * 2.0 ** -24
+        want, absv = torch.matmul(p, vv).transpose(0, 1), torch.matmul(p, vv.abs()).transpose(0, 1)
+        assert bool(((out[b, :m].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + rel) * absv).all()), b
+        add = p.sum(1).view(kv, G, rows).sum(1)
+        w = before[b, :, :rows].double() + add
+        assert bool(((weight[b, :, :rows].double() - w).abs() <= (rel + m * G * 2.0 ** -24) * add + 2.0 ** -24 * w.abs() + 1e-30).all()), b
+        assert torch.equal(weight[b, :, rows:], before[b, :, rows:])
+    for _ in range(3):
+        cache.weight.copy_(before)
+        call()
+        assert torch.equal(out, first) and torch.equal(cache.weight, weight)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        cache.weight.copy_(before)
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first) and torch.equal(cache.weight, weight)
+
+
 @pytest.mark.parametrize("heads,n", [("qwen", 1), ("three", 7), ("qwen", 9), ("three", 50), ("toy", 90)])
 def test_attention_masked_and_split(fc, ctx, heads, n):
     """Hidden keys (NaN in their rows) and a NaN that some tokens see, over cache lengths that splits share."""
