@@ -436,12 +436,14 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 // ahead (16 KB each at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
 // back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
 // a lane holds one row and, of a block's keys, the 32 of its half wave.
-// Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 PFLOP) take 638 us, the
-// first call after a pause 800: the card's power bounds it.  Blocks converted once per workgroup
-// (689), scores a block ahead of the softmax, three waves on a SIMD or 64 rows in a wave come out
-// the same or slower: what they save in cycles goes in clock (without the exponentials, 8 % of it;
-// without the keys' conversion, 5).  256 tokens over 2176 rows: 23 us of latencies, a block after the
-// other in each workgroup.
+// Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 PFLOP) take 548 us, 0.94
+// PFLOP/s; the first calls after a pause are slower.  The card's power bounds it: a plain matrix
+// product of these operations takes 370 us at the clock that is left to it, and the exponentials and
+// conversions, which hide behind the products in cycles, cost the rest in power.  Scores a block
+// ahead of the softmax (two ways), three waves on a SIMD or prefetched operands come out the same;
+// 64 rows in a wave, or blocks converted once per workgroup, slower (by half, by a tenth); without the
+// exponentials it is 8 % faster, without the keys' conversion 5.  256 tokens over 2176 rows: 23 us of
+// latencies, a block after the other in each workgroup.
 //
 // LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks.
