@@ -274,18 +274,15 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
         vis[i] &= left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
       }
     }
-    // What no row sees may hold anything, NaN among it, and 0 x NaN is NaN: such values become 0.  A
-    // NaN that some rows see becomes 0 too, and NaN is what these rows get for it afterwards.
+    // 0 x NaN is NaN, so where some row may not see the block whole (what none sees may hold anything)
+    // a NaN becomes 0, and NaN is what the rows that see it get for it afterwards.
     bool odd = false;
     if (!full) {
       uint32_t any = 0;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          vw[d][i] &= vis[i];
-          any |= nan_tops(vw[d][i]);
-        }
+        for (int i = 0; i < 4; ++i) any |= nan_tops(vw[d][i]);
       odd = __any((any & 0x80808080u) != 0);
       if (odd) {
 #pragma unroll
@@ -580,27 +577,33 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs args) {
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[0], w[1], ks), q[2 * i], s[t], 0, 0, 0);
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dequant8(w[2], w[3], ks), q[2 * i + 1], s[t], 0, 0, 0);
         }
-      const bool part = a.mask || j0 + kQBlock > wall;   // some row of the wave may not see it whole
+      // the keys that the mask shows, and whether some row of the wave may not see the block whole
+      uint64_t shown = ~0ull;
+      if (a.mask) shown = __ballot(sm_mask[stage][wave][lane] != 0);
+      const bool later = j0 + kQBlock > wall, part = later || shown != ~0ull;
       uint32_t mine = ~0u;             // the lane's 32 keys that some row may see
       uint32_t odd = 0;                // those of its halves where some value is NaN
       if (part) {
-        mine = (uint32_t)(seen_bits(wmax - j0) >> (32 * h));
-        if (a.mask) {
-          uint32_t bits = 0;
+        const uint64_t some = shown & seen_bits(wmax - j0);
+        mine = (uint32_t)(some >> (32 * h));
+        if (later) {
+          const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const u32x4 mw = *reinterpret_cast<const u32x4 *>(&sm_mask[stage][wave][h * 32 + 16 * i]);
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) bits |= byte_bits(set_bytes(mw[x]) & 0x01010101u) << (16 * i + 4 * x);
-          }
-          mine &= bits;
+            for (int e = 0; e < 16; ++e)
+              if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
+        } else {                       // the same keys for every row: the scalar unit spreads them over the halves
+          const uint32_t lo = (uint32_t)some, hi = (uint32_t)(some >> 32);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint64_t lanes = (uint64_t)(uint32_t)((int)(hi << (31 - 16 * t - e)) >> 31) << 32 |
+                                     (uint32_t)((int)(lo << (31 - 16 * t - e)) >> 31);
+              s[t][e] = __builtin_amdgcn_inverse_ballot_w64(lanes) ? s[t][e] : kNegInf;
+            }
         }
-        const uint32_t sees = mine & (uint32_t)(seen_bits(seen - j0) >> (32 * h));
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
       }
       float top = kNegInf;
 #pragma unroll
@@ -628,14 +631,9 @@ __global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs args) {
         if (part) {                    // as in k_qattn
           uint32_t any = 0;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t vis = bit_bytes(mine >> (16 * t + 4 * x));
+          for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              vw[d][x] &= vis;
-              any |= nan_tops(vw[d][x]);
-            }
-          }
+            for (int x = 0; x < 4; ++x) any |= nan_tops(vw[d][x]);
           if (__any((any & 0x80808080u) != 0)) {
             odd |= 0xFFFFu << (16 * t);
 #pragma unroll
