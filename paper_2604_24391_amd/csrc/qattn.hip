@@ -484,26 +484,27 @@ __device__ __forceinline__ QAttnArgs args_again() {
 // keys are in its L2, then with the others' (queue[8]: pieces taken).  Sixteen frames of 704 to 1024
 // tokens, seven rounds: 548 us, 587 without; but a last round that is not full falls to few CUs (equal
 // items, 3.5 rounds: 392 and 357), so only ragged batches of four rounds or more go this way.
-template <int HD, bool QUEUE>
-__global__ __launch_bounds__(256, 2) void k_qattn_rows(QAttnArgs args) {
+template <int HD, int NW, bool QUEUE>
+__global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
   constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
   constexpr int DT = HD / 32;                   // output tiles of 32 dims
   constexpr int TILE = kQBlock * HD;            // bytes of a block's keys, and of its values
-  constexpr int DMAS = TILE / 16 / 256;         // DMA instructions of a wave for either
+  constexpr int DMAS = TILE / 1024 / NW;        // DMA instructions of a wave for either
+  constexpr int ROWS = 32 * NW;
   constexpr int STAGES = 2;
   __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
-  __shared__ uint64_t sm_nan[4][HD];
-  __shared__ __align__(16) uint8_t sm_mask[STAGES][4][256];
+  __shared__ uint64_t sm_nan[NW][HD];
+  __shared__ __align__(16) uint8_t sm_mask[STAGES][NW][256];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   auto work = [&](const QAttnArgs &a, int id) {
     const int P = a.B * a.KV, R = a.n * a.G;
     const int rest = id / P, hb = QUEUE ? id % P : (id % P + rest) % P, split = rest % a.splits;
-    const int r0 = ((R + 127) / 128 - 1 - rest / a.splits) * 128;
+    const int r0 = ((R + ROWS - 1) / ROWS - 1 - rest / a.splits) * ROWS;
     const int b = hb / a.KV, kv = hb % a.KV;
     const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
     const int rows = m * a.G;
     if (r0 >= rows) return;
-    const int kmax = held + a.by_g(min(r0 + 128, rows) - 1) + 1;
+    const int kmax = held + a.by_g(min(r0 + ROWS, rows) - 1) + 1;
     const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
     if (split >= used) return;
     const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
@@ -1038,7 +1039,7 @@ template <int HD>
 fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const long R = (long)a.n * a.G, pairs = (long)a.B * a.KV;
   const bool many = R > 32;
-  const int MT = R <= 16 ? 1 : 2, tile = many ? 128 : 16 * MT;
+  const int MT = R <= 16 ? 1 : 2, NW = R <= 64 ? 2 : 4, tile = many ? 32 * NW : 16 * MT;
   const long tiles = (R + tile - 1) / tile;
   const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
   auto up4 = [](long x) { return (x + 3) / 4 * 4; };
@@ -1050,8 +1051,8 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   long splits = 1, slots = a.B;
   if (many) {
-    // as many workgroups as run at once, two on a CU
-    splits = std::min<long>(2L * ctx->num_cus / (pairs * tiles), a.cap / kQBlock / kRowsBlocks);
+    // as many workgroups as run at once, eight waves on a CU
+    splits = std::min<long>(8L / NW * ctx->num_cus / (pairs * tiles), a.cap / kQBlock / kRowsBlocks);
     splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
   } else {
     // One workgroup's loads keep a CU's path to memory busy; two, where a mask adds vector work to
@@ -1083,14 +1084,15 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
       return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
     a.pieces = (int)(pairs * tiles * splits);
     const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;   // workgroups that run at once
-    if (a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
+    if (NW == 4 && a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
       a.queue = reinterpret_cast<int *>(at);
       hipLaunchKernelGGL(k_qattn_queue, dim3(1), dim3(8), 0, st, a.queue);
       FC_LAUNCH_OK(st, "k_qattn_queue");
     }
     ProfScope ps(ctx, st, "fc_qattn_rows");
-    if (a.queue) hipLaunchKernelGGL((k_qattn_rows<HD, true>), dim3((unsigned)once), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_qattn_rows<HD, false>), dim3((unsigned)a.pieces), dim3(256), 0, st, a);
+    if (a.queue) hipLaunchKernelGGL((k_qattn_rows<HD, 4, true>), dim3((unsigned)once), dim3(256), 0, st, a);
+    else if (NW == 4) hipLaunchKernelGGL((k_qattn_rows<HD, 4, false>), dim3((unsigned)a.pieces), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_qattn_rows<HD, 2, false>), dim3((unsigned)a.pieces), dim3(128), 0, st, a);
     FC_LAUNCH_OK(st, "k_qattn_rows");
   } else {
     const dim3 grid((unsigned)a.slots, (unsigned)a.KV);
