@@ -45,7 +45,7 @@ struct QAttnArgs {
   float *lse;                        // [B KV][R] log2 of each row's sum, or null
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
-  int B, n, H, KV, G, cap, splits, tile_rows, slots;
+  int B, n, H, KV, G, cap, splits, least, tile_rows, slots;
   int *queue, pieces;                // k_qattn_rows: [8] pieces of work taken behind the first ones, or null
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
@@ -92,10 +92,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // Splits that the key blocks of one tile of rows are dealt over (k_qattn_rows): lengths are known on
 // the device only, so the grid has room for `splits`, and a short item uses no more than leaves
-// each of them eight blocks (256 rows of 7 heads over 2176 keys: 42.5 us; four 44.3, twelve 47.9).
-constexpr int kRowsBlocks = 8;
-__device__ __forceinline__ int splits_used(int kmax, int splits) {
-  return max(1, min(splits, (kmax + kRowsBlocks * kQBlock - 1) / (kRowsBlocks * kQBlock)));
+// each of them `least` blocks.
+__device__ __forceinline__ int splits_used(int kmax, const QAttnArgs &a) {
+  return max(1, min(a.splits, (kmax + a.least * kQBlock - 1) / (a.least * kQBlock)));
 }
 // k_qattn deals a.slots workgroups of each key-value head over the items by their lengths, `per`
 // blocks to each: with the same number for every item, the longest one of a ragged batch would
@@ -505,7 +504,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
     const int rows = m * a.G;
     if (r0 >= rows) return;
     const int kmax = held + a.by_g(min(r0 + ROWS, rows) - 1) + 1;
-    const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a.splits);
+    const int blocks = (kmax + kQBlock - 1) / kQBlock, used = splits_used(kmax, a);
     if (split >= used) return;
     const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
@@ -839,7 +838,7 @@ __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
   const int R = a.n * a.G, rows = m * a.G, r = tile * 32 + lane % 32;
   if (r >= rows) return;
   const int last = min(r / a.tile_rows * a.tile_rows + a.tile_rows, rows) - 1;
-  const int used = splits_used(held + a.by_g(last) + 1, a.splits);
+  const int used = splits_used(held + a.by_g(last) + 1, a);
   const long step = (long)a.B * a.KV * R, at = (long)hb * R + r, R32 = (R + 31) / 32;
   const long pstep = (long)a.B * a.KV * R32 * (HD / 8) * 64;
   const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part) + ((hb * R32 + tile) * (HD / 8) + 4 * dt + wave) * 64 + lane;
@@ -1051,8 +1050,14 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
   long splits = 1, slots = a.B;
   if (many) {
-    // as many workgroups as run at once, eight waves on a CU
-    splits = std::min<long>(8L / NW * ctx->num_cus / (pairs * tiles), a.cap / kQBlock / kRowsBlocks);
+    // Workgroups for every CU, as long as each has four blocks; as many as run at once (eight waves on a
+    // CU), as long as each has eight, for what its part of the outputs costs (63 rows of 4 heads over
+    // 4000 keys 15.0 us so, with two 16.5, with eight 17.8; 1792 rows over 2176 42.5, with four to fill
+    // all places 44.3, with twelve 47.9).
+    const long units = pairs * tiles, blocks = a.cap / kQBlock, spread = std::min<long>(ctx->num_cus / units, blocks / 4);
+    splits = std::min<long>(8L / NW * ctx->num_cus / units, blocks / 8);
+    a.least = spread >= splits ? 4 : 8;
+    splits = std::max(spread, splits);
     splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
   } else {
     // One workgroup's loads keep a CU's path to memory busy; two, where a mask adds vector work to
