@@ -376,14 +376,14 @@ __device__ __forceinline__ void write_kept(Each each, Places p, int n, int keep,
 // The kept rows of one head in ascending order, by one workgroup.  A radix select over 11, 11 and 10
 // bits of the weights' keys finds the smallest kept key and how many rows of that key stay (the lowest
 // ones); then every wave counts, and writes down, what stays of its own run of rows.
-// Weights share few exponents, so the first digit's counts stand in 16 copies, one for every
-// fourth lane: with one copy the lanes of a wave wait for each other.  IT > 0: a lane holds IT keys in
+// Weights share few exponents, so the first digit's counts stand in 4 copies, one for every fourth
+// lane (16 where there are more rows to count): with one the lanes of a wave wait for each other.  IT > 0: a lane holds IT keys in
 // registers (up to 1024 IT rows; 64 of them spill: 90 us for 65536 rows against 57); IT = 0 reads
 // the weights anew in each pass, where the workspace has no room for the counts of several
 // workgroups.  Latency bounds it, a chain of passes and barriers: 7.5 us for 2176 rows.
 template <int IT>
 __global__ __launch_bounds__(kPickThreads) void k_qevict_pick(EvictArgs a) {
-  constexpr int COPIES = IT == 4 ? 4 : 16;            // fewer to clear and to add up for few rows
+  constexpr int COPIES = IT ? 4 : 16;                 // fewer to clear and to add up for few rows
   __shared__ __align__(16) int hist[kPickBins * COPIES];  // 128 KB of 16 copies: one workgroup on a CU
   __shared__ int wsum[kPickWaves], wabove[kPickWaves], wties[kPickWaves], found[2];
   const int b = blockIdx.x / a.KV, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -582,6 +582,7 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
   constexpr int GROUP = 4, VSTR = kQBlock + 4;               // source blocks at a time; off the bank period
   constexpr int CPT = HD * kQBlock / 16 / kQThreads;         // 16-byte pieces of a block for each thread
   __shared__ int src[kQBlock];
+  __shared__ float scale[2][kQBlock];                        // of each row's keys and values
   __shared__ float red[2][kQThreads / 64];
   __shared__ __align__(16) uint8_t vt[GROUP][HD * VSTR];
   const int hb = blockIdx.y, b = hb / a.KV, blk = blockIdx.x, j0 = blk * kQBlock, tid = threadIdx.x;
@@ -595,20 +596,17 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
   const int sub = tid % TPR, row = tid / TPR;
   uint4 kr[KP];
   float kmul[KP], kmax = 0.f;
+  float mul = 0.f;
+  if (tid < 2 * kQBlock) mul = (tid < kQBlock ? ks : vs)[src[tid % kQBlock] / kQBlock];
 #pragma unroll
-  for (int p = 0; p < KP; ++p) {
-    const int s = src[p * RPP + row];
-    kr[p] = *reinterpret_cast<const uint4 *>(a.k + ((long)hb * a.cap + s) * HD + sub * 16);
-    kmul[p] = ks[s / kQBlock];
-  }
+  for (int p = 0; p < KP; ++p)
+    kr[p] = *reinterpret_cast<const uint4 *>(a.k + ((long)hb * a.cap + src[p * RPP + row]) * HD + sub * 16);
   const int d = tid / TPD, v0 = tid % TPD * KPT;
   const uint8_t *vb = a.v + (long)hb * a.cap * HD;
   uint32_t vc[KPT / 4];                 // codes of the thread's keys of its column
   float vmul[KPT], vmax = 0.f;
 #pragma unroll
   for (int i = 0; i < KPT / 4; ++i) vc[i] = 0;
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) vmul[i] = vs[src[v0 + i] / kQBlock];
   const int b0 = src[0] / kQBlock, b1 = src[cnt - 1] / kQBlock;
   for (int g = b0; g <= b1; g += GROUP) {
     uint4 x[GROUP][CPT];
@@ -618,6 +616,7 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
       for (int c = 0; c < CPT; ++c)
         x[i][c] = *reinterpret_cast<const uint4 *>(vb + (long)min(g + i, b1) * (HD * kQBlock) + (c * kQThreads + tid) * 16);
     if (g > b0) __syncthreads();        // the group before has been read
+    else if (tid < 2 * kQBlock) scale[tid / kQBlock][tid % kQBlock] = mul;
 #pragma unroll
     for (int i = 0; i < GROUP; ++i)
 #pragma unroll
@@ -634,7 +633,10 @@ __global__ __launch_bounds__(kQThreads) void k_qevict_move(EvictArgs a) {
     }
   }
 #pragma unroll
+  for (int i = 0; i < KPT; ++i) vmul[i] = scale[1][v0 + i];
+#pragma unroll
   for (int p = 0; p < KP; ++p) {
+    kmul[p] = scale[0][p * RPP + row];
     const uint32_t w[4] = {kr[p].x, kr[p].y, kr[p].z, kr[p].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -748,6 +750,7 @@ fc_status launch_qcache_evict(fc_ctx *ctx, const fc_qcache &s, const fc_qcache &
     ProfScope ps(ctx, st, "fc_qevict_pick");
     const dim3 grid((unsigned)heads), block(kPickThreads);
     if (a.cap <= 4 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<4>, grid, block, 0, st, a);
+    else if (a.cap <= 8 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<8>, grid, block, 0, st, a);
     else if (a.cap <= 16 * kPickThreads) hipLaunchKernelGGL(k_qevict_pick<16>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(k_qevict_pick<0>, grid, block, 0, st, a);
     FC_LAUNCH_OK(st, "k_qevict_pick");
