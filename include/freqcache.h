@@ -263,7 +263,7 @@ typedef struct {
   const uint16_t *q, *k, *v;
   int64_t q_row, k_row, v_row;
   int64_t q_item, k_item, v_item;
-  int32_t n_heads;          /* query heads, a multiple of the cache's n_kv_heads */
+  int32_t n_heads;          /* query heads, a multiple of the cache's n_kv_heads, up to 65535 */
 } fc_qkv_rows;
 
 /* Library version string. */
@@ -543,7 +543,8 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
  *             dst->weight may be NULL; dst->capacity >= keep;
  *   keep:     rows kept, >= n_sink + n_recent;
  *   kept:     [B][n_kv][keep] int32 source rows, ascending, -1 behind the last;
- *   len_out:  [B] int32 min(len[b], keep), or NULL; not len itself. */
+ *   len_out:  [B] int32 min(len[b], keep), or NULL; not len itself.
+ * The selection may use the context's partial-sum workspace. */
 fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *dst,
                           const int32_t *len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           int32_t *kept, int32_t *len_out, int32_t B, void *stream);

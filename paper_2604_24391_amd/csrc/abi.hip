@@ -777,6 +777,7 @@ static fc_status check_qrows(const fc_qcache &c, int n_heads, int B, int n, cons
   if (n_heads < 1 || n_heads % c.n_kv_heads)
     return fail(FC_ERR_SHAPE, "%s: n_kv_heads %d does not divide n_heads %d", who, c.n_kv_heads, n_heads);
   if (n < 1 || n > c.capacity) return fail(FC_ERR_SHAPE, "%s: n=%d tokens, capacity %d", who, n, c.capacity);
+  if (n_heads > 65535) return fail(FC_ERR_UNSUPPORTED, "%s: %d heads (at most 65535)", who, n_heads);
   if ((long)n * n_heads > (1L << 30))
     return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens of %d heads (at most 2^30 rows an item)", who, n, n_heads);
   return FC_OK;

@@ -94,6 +94,7 @@ int main() {
     EXPECT(att(&c, 28, 0.1f, 1, 2, n), FC_ERR_SHAPE);
   }
   for (int H : {0, -4, 3, 30, INT_MAX}) EXPECT(att(&c, H), FC_ERR_SHAPE);
+  for (int H : {65536, 1 << 28}) EXPECT(att(&c, H), FC_ERR_UNSUPPORTED);
   {
     fc_qcache big = c;
     big.capacity = 1 << 30;
