@@ -428,10 +428,11 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   }
 }
 
-// More than 32 rows: 4 waves of 32 each share the key blocks, which the DMA brings into LDS a block
-// ahead (16 KB each at hd 128), in e4m3: half of the bytes that bfloat16 tiles would be read
-// back as, at the price that every wave converts them for itself.  32 x 32 matrix instructions;
-// a lane holds one row and, of a block's keys, the 32 of its half wave.
+// More than 32 rows: 4 waves of 32 each (2 up to 64 rows, where the others would hold places and idle:
+// 46 us against 32 for sixteen items of 52 rows of 8 heads over 5000 keys) share the key blocks,
+// which the DMA brings into LDS a block ahead (16 KB each at hd 128), in e4m3: half of the bytes that
+// bfloat16 tiles would be read back as, at the price that every wave converts them for itself.  32 x
+// 32 matrix instructions; a lane holds one row and, of a block's keys, the 32 of its half wave.
 // Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 PFLOP) take 548 us, 0.94
 // PFLOP/s; the first calls after a pause are slower.  The card's power bounds it: a plain matrix
 // product of these operations takes 370 us at the clock that is left to it, and the exponentials and

@@ -434,6 +434,13 @@ def test_evict_long_caches(fc, ctx, cap, held, keep, sink, recent):
     run_evict(fc, ctx, g, "group2", B, cap, held, keep, sink, recent, cache=cache)
 
 
+def test_evict_long_cache_in_a_small_workspace(fc):
+    """A context without room for the counts of several workgroups selects by one a head."""
+    g = torch.Generator().manual_seed(60)
+    with fc.Context(fc.Caps(max_batch=1, max_height=28, max_width=28, max_tokens=4, max_seq=8, max_d_model=64, max_ffn=64, max_qkv=192)) as small:
+        run_evict(fc, small, g, "group2", 2, 16448, [16448, 16000], 4000, 9, 100)
+
+
 def test_evict_ties_and_odd_weights(fc, ctx):
     """Few distinct weights (ties to the lower row), zeros of both signs, NaN, infinities, negative and
     subnormal weights."""
