@@ -1056,9 +1056,17 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     // 4000 keys 15.0 us so, with two 16.5, with eight 17.8; 1792 rows over 2176 42.5, with four to fill
     // all places 44.3, with twelve 47.9).
     const long units = pairs * tiles, blocks = a.cap / kQBlock, spread = std::min<long>(ctx->num_cus / units, blocks / 4);
-    splits = std::min<long>(8L / NW * ctx->num_cus / units, blocks / 8);
+    const long places = 8L / NW * ctx->num_cus;
+    splits = std::min<long>(places / units, blocks / 8);
     a.least = spread >= splits ? 4 : 8;
-    splits = std::max(spread, splits);
+    splits = std::max<long>(1, std::max(spread, splits));
+    // Where they do not fill the places once, more, of 16 blocks at least, if these fill their last round
+    // better by a tenth (360 tiles over 4600 keys in four splits 122 us, 142 in one; 200 over 7400 in
+    // five 116, in two 124; 336 over 3200 in three 105, 103 in one).
+    auto filled = [&](long s) { return (double)(units * s) / ((units * s + places - 1) / places * places); };
+    if (units < places)
+      for (long s = splits + 1; s <= 8 && blocks / s >= 16; ++s)
+        if (filled(s) > filled(splits) + 0.1) splits = s;
     splits = std::max<long>(1, std::min<long>(splits, (ws - side - plan) / (up4(2 * per) + padded * HD)));
   } else {
     // One workgroup's loads keep a CU's path to memory busy; two, where a mask adds vector work to
@@ -1090,7 +1098,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
       return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
     a.pieces = (int)(pairs * tiles * splits);
     const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;   // workgroups that run at once
-    if (NW == 4 && a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
+    if (NW == 4 && !parts && a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
       a.queue = reinterpret_cast<int *>(at);
       hipLaunchKernelGGL(k_qattn_queue, dim3(1), dim3(8), 0, st, a.queue);
       FC_LAUNCH_OK(st, "k_qattn_queue");
