@@ -859,7 +859,7 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
   if (accumulate) buf.add(c.weight, (size_t)B * c.n_kv_heads * c.capacity * sizeof(float));
   buf.end_written();
   fc_qcache read = c;
-  read.weight = nullptr;
+  if (accumulate) read.weight = nullptr;
   buf.add(read, B);
   buf.add(q, qb);
   buf.add(key_mask, (size_t)B * c.capacity);

@@ -1049,6 +1049,8 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   const long side = !weigh ? 0 : logit ? per * a.cap : up4(per), plan = up4(2L * a.B);
   if (side > ws)
     return fail(FC_ERR_CAPACITY, "fc_qcache_attention: the sums of %ld rows exceed the context's workspace", per);
+  if (weigh && !logit && (a.cap + kGroupKeys - 1L) / kGroupKeys * pairs > (1L << 24) - 1)
+    return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: weights of %ld heads of %d rows in one call", pairs, a.cap);
   long splits = 1, slots = a.B;
   if (many) {
     // Workgroups for every CU, as long as each has four blocks; as many as run at once (eight waves on a
@@ -1094,7 +1096,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
     a.ml = reinterpret_cast<float2 *>(at + (many ? splits * padded : slots * a.KV * R) * HD);
   }
   if (many) {
-    if (pairs * tiles * splits > (1L << 24) - 1)
+    if (pairs * tiles * splits > (1L << 24) - 1)   // nothing has been launched yet
       return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
     a.pieces = (int)(pairs * tiles * splits);
     const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;   // workgroups that run at once
@@ -1130,11 +1132,9 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
   }
   if (weigh && !logit) {
     const long groups = (a.cap + kGroupKeys - 1) / kGroupKeys, all = pairs * groups;
-    // workgroups for four on every CU, each with eight row tiles at least, where their sums fit
+    // workgroups for four on every CU, each with 256 rows at least, where their sums fit
     long rs = std::max<long>(1, std::min(4L * ctx->num_cus / all, (R + 255) / 256));
     rs = std::max<long>(1, std::min<long>(rs, (ws - up4(per)) / (pairs * a.cap)));
-    if (all * rs > (1L << 24) - 1)
-      return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: weights of %ld heads of %d rows in one call", pairs, a.cap);
     float *wpart = rs > 1 ? ctx->part + up4(per) : nullptr;   // the splits' parts are joined by now
     {
       ProfScope ps(ctx, st, "fc_qattn_weight");

@@ -167,6 +167,8 @@ int main() {
                           (const void *)u8(15), (const void *)i32(12), (const void *)i32(13)})
       EXPECT(to(p), FC_ERR_INVALID_ARG);
     EXPECT(to(c.k + k_bytes), FC_ERR_HIP);
+    EXPECT(fc_qcache_attention(&ctx, &c, u16(14), i32(12), i32(13), nullptr, reinterpret_cast<uint16_t *>(c.weight), 28, 1.f, 0, 2, 1, nullptr),
+           FC_ERR_INVALID_ARG);                                      // nor over weights that stay as they are
     fc_qcache y = c;
     y.weight = reinterpret_cast<float *>(u8(15));
     EXPECT(att(&y), FC_ERR_INVALID_ARG);                                 // over the mask
