@@ -524,7 +524,10 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  *   scale:    finite, usually 1 / sqrt(head_dim);
  *   accumulate: 1: weight[b][h][j] += the sum of the probabilities that row j has received
  *             from the tokens and the query heads of its group (cache->weight is needed).
- * What is hidden from a token has no effect on it, whatever its bytes.  The partial results
+ * What is hidden from a token has no effect on it, whatever its bytes.  Outputs are summed in
+ * float32, which holds every mean of finite numbers while the rows that a token sees times the
+ * largest of their values are below 2^137 (any number of rows up to values of 1e32, 512 of the
+ * largest of bfloat16).  The partial results
  * use the context's partial-sum workspace: fewer splits where it is small, and
  * FC_ERR_CAPACITY when accumulate needs more rows than it holds (one float for each of the
  * B n n_heads rows). */

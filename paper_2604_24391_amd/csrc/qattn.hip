@@ -59,6 +59,15 @@ __device__ __forceinline__ bf16x8 dequant8(uint32_t w0, uint32_t w1, float s) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// Values enter the products 2^-17 smaller than they are, and an output's last factor makes up for
+// it.  Scales reach 2^120, where codes of 256 and more stand for numbers beyond bfloat16 and 0 times
+// one (a hidden row's) would be NaN, and outputs are sums of up to 2^8 |v| a row before their division.
+// 17 is as far as the least number, 2^-109, stays a normal bfloat16; powers of two round nothing.
+constexpr uint32_t kValueDown = 17;
+constexpr float kValueUp = 131072.f;
+__device__ __forceinline__ float value_scale(float s) { return __uint_as_float(__float_as_uint(s) - (kValueDown << 23)); }
+// What an unnormalised output is multiplied with, from its row's sum (a row that sees no key: 0).
+__device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : kValueUp / l; }
 // LDS words that lanes of one wave write in parts and read whole, and the order between the two.
 typedef uint16_t __attribute__((may_alias)) part16;
 typedef uint32_t __attribute__((may_alias)) part32;
@@ -236,7 +245,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
   if (mbase) mw = *reinterpret_cast<const u32x4 *>(mbase + at0 * kQBlock);
   load_k(at0);
   load_v(at0);
-  float ks = ksb[at0], vs = vsb[at0];
+  float ks = ksb[at0], vs = value_scale(vsb[at0]);
   bf16x8 q[MT][2 * KC];
   int seen[MT];                                 // keys that the lane's row sees
   f32x4 o[MT][DT];
@@ -258,7 +267,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 
   for (int blk = blo + wave; blk < bhi; blk += 4) {
     const int j0 = blk * kQBlock, next = min(blk + 4, nblk - 1);
-    const float ks_next = ksb[next], vs_next = vsb[next];
+    const float ks_next = ksb[next], vs_next = value_scale(vsb[next]);
     const bool full = !a.mask && j0 + kQBlock <= kall;
     uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};      // the lane's 16 keys that some row may see, by bytes
     if (!full) {
@@ -411,7 +420,7 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
         *reinterpret_cast<float4 *>(a.part + (slot * R + r) * HD + d) =
             make_float4(y[0], y[1], y[2], y[3]);
       } else {
-        const float inv = sm_l[row] == 0.f ? 0.f : 1.f / sm_l[row];
+        const float inv = output_factor(sm_l[row]);
         const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
         *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
       }
@@ -557,14 +566,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
     float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
 
     int stage = 0;
-    float ks = ksb[blo], vs = vsb[blo];
+    float ks = ksb[blo], vs = value_scale(vsb[blo]);
     for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
       wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
       lds_barrier();                   // every wave has left the other stage
       if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1);
       if (w0 >= rows) continue;        // it only brings its part of the blocks
       const int j0 = blk * kQBlock, ahead = min(blk + 1, bhi - 1);
-      const float ks_next = ksb[ahead], vs_next = vsb[ahead];
+      const float ks_next = ksb[ahead], vs_next = value_scale(vsb[ahead]);
       f32x16 s[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -612,8 +621,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
       top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
-      // the reference follows the maximum only where it is 2^8 behind: no sum comes near
-      // float32's limits, and most blocks need not touch O
+      // the reference follows the maximum only where it is 2^8 behind: most blocks need not touch O,
+      // and its sums stay within float32 while rows times their largest value are below 2^137
       if (__any(top > ref + 8.f)) {
         const float mn = fmaxf(ref, top), corr = exp2_fast(ref - (mn == kNegInf ? 0.f : mn));
         ref = mn;
@@ -690,7 +699,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
         for (int j = 0; j < 4; ++j) dst[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
     } else {
       if (a.lse && h == 0) a.lse[at] = log_sum(ref, sum);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const float inv = output_factor(sum);
       uint16_t *dst = a.out + at_q;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
@@ -774,7 +783,7 @@ __global__ __launch_bounds__(256) void k_qattn_join(QAttnArgs a, int join_rows) 
       f32x4 t = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < SG; ++i) t += *reinterpret_cast<const f32x4 *>(&sm_y[i][d]);
-      t *= sum == 0.f ? 0.f : 1.f / sum;
+      t *= output_factor(sum);
       const bf16x4 w = {(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
       *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
       if (a.lse && tid == 0) a.lse[(long)hb * R + r] = log_sum(top, sum);
@@ -869,7 +878,7 @@ __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
       y += x[i] * h;
     }
   }
-  y *= l == 0.f ? 0.f : 1.f / l;
+  y *= output_factor(l);
   const int tok = a.by_g(r);
   const bf16x4 w = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
   *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + tok) * a.H + kv * a.G + r - tok * a.G) * HD + d) = w;
