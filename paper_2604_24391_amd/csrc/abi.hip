@@ -811,7 +811,7 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
   buf.add(c, B);
   buf.add(q_out, qb);
   buf.end_written();
-  buf.add(pos, axes * n * ib);
+  buf.add(pos, (size_t)axes * n * ib);
   buf.add(len, ib);
   buf.add(n_new, ib);
   if ((uintptr_t)q_out % 16) return fail(FC_ERR_INVALID_ARG, "%s: q_out must be 16-byte aligned", who);
