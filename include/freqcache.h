@@ -257,7 +257,8 @@ typedef struct {
 
 /* Rows of queries, keys and values of new tokens, e.g. the parts of one projection's rows:
  * element (b, i, h, x) of q lies at q[b q_item + i q_row + h head_dim + x] (bf16, device;
- * strides in elements, multiples of 8, not negative; pointers 16-byte aligned).
+ * strides in elements, multiples of 8, from 0 to 2^40, a row stride times n up to 2^60;
+ * pointers 16-byte aligned).
  * q may be NULL (keys and values only).  (host struct) */
 typedef struct {
   const uint16_t *q, *k, *v;

@@ -818,9 +818,9 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
   for (int i = 0; i < 3; ++i) {
     if (!in[i]) continue;
     if ((uintptr_t)in[i] % 16 || row[i] < 0 || item[i] < 0 || row[i] % 8 || item[i] % 8 ||
-        row[i] > (1L << 40) || item[i] > (1L << 40))
+        row[i] > (1L << 40) || item[i] > (1L << 40) || (n > 1 && row[i] > (1L << 60) / (n - 1)))
       return fail(FC_ERR_INVALID_ARG, "%s: q, k and v must be 16-byte aligned, with strides that are "
-                  "multiples of 8 elements and not negative", who);
+                  "multiples of 8 elements, not negative and up to 2^40 (2^60 over a call's tokens)", who);
     const int width = (i ? c.n_kv_heads : x.n_heads) * c.head_dim;
     const size_t bytes = ((size_t)(B - 1) * item[i] + (size_t)(n - 1) * row[i] + width) * 2;
     const bool same = i == 0 && x.q == q_out && (n == 1 || row[0] == width) &&

@@ -43,6 +43,24 @@ int main() {
     EXPECT(app(x, reinterpret_cast<int32_t *>(at(0) - bytes + 4), n), FC_ERR_INVALID_ARG);   // their last one is the keys' first
     EXPECT(app(x, reinterpret_cast<int32_t *>(at(0) + (64L << 30) - 4), n), FC_ERR_INVALID_ARG);
   }
+  // strides whose rows end beyond 64 bits: (n - 1) k_row is 2^64 elements here, and 2^63 bytes
+  for (int n : {(1 << 24) + 1, (1 << 22) + 1, kRows - 200}) {
+    for (int64_t s : {(int64_t)1 << 40, ((int64_t)1 << 40) - 8}) {
+      fc_qkv_rows y = x;
+      y.k_row = s;
+      EXPECT(app(y, i32(12), n), FC_ERR_INVALID_ARG);
+      y = x;
+      y.v_row = s;
+      EXPECT(app(y, i32(12), n), FC_ERR_INVALID_ARG);
+    }
+    fc_qkv_rows y = x;
+    y.k_row = y.v_row = 64;
+    EXPECT(app(y, i32(12), n), FC_ERR_HIP);
+  }
+  // a stride that no token takes says nothing
+  fc_qkv_rows one = x;
+  one.k_row = one.v_row = one.k_item = one.v_item = (int64_t)1 << 40;
+  EXPECT(app(one, i32(12), 1), FC_ERR_HIP);
   std::printf(g_fail ? "%d failed\n" : "OK (%d failed expectations)\n", g_fail);
   return g_fail != 0;
 }
