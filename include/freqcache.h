@@ -506,7 +506,8 @@ fc_status fc_phase_correlate_rotation(fc_ctx *ctx, const float *frames_prev,
  * grows).  Numbers are rounded to nearest even from float32; an infinity is held as
  * +-448 s, a NaN as a NaN, and neither sets the scale.  The new rows' weights are set to 0.
  * Rows past the capacity are dropped, their q_out (and out, in the attention) left as it is.
- * Counts outside their ranges are clamped. */
+ * Counts outside their ranges are clamped.  FC_ERR_UNSUPPORTED for more than 2^30 - 127 tokens or
+ * 2^30 rows (tokens times heads) an item. */
 fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_axes *rope,
                            const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
                            const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
@@ -531,7 +532,10 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  * largest of bfloat16).  The partial results
  * use the context's partial-sum workspace: fewer splits where it is small, and
  * FC_ERR_CAPACITY when accumulate needs more rows than it holds (one float for each of the
- * B n n_heads rows). */
+ * B n n_heads rows).  FC_ERR_UNSUPPORTED, before anything is launched, for more than 2^30 rows
+ * (tokens times heads) an item, and for calls that need 2^24 workgroups or more: one for each 128
+ * rows of each item's key-value heads and each of their splits, and, where accumulate computes the
+ * scores again, one for each 256 rows of capacity. */
 fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_t *q,
                               const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
                               uint16_t *out, int32_t n_heads, float scale, int32_t accumulate,
@@ -548,7 +552,8 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
  *   keep:     rows kept, >= n_sink + n_recent;
  *   kept:     [B][n_kv][keep] int32 source rows, ascending, -1 behind the last;
  *   len_out:  [B] int32 min(len[b], keep), or NULL; not len itself.
- * The selection may use the context's partial-sum workspace. */
+ * The selection may use the context's partial-sum workspace.  FC_ERR_UNSUPPORTED for keep above
+ * 2^30 - 64. */
 fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *dst,
                           const int32_t *len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           int32_t *kept, int32_t *len_out, int32_t B, void *stream);

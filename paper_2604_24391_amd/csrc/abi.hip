@@ -750,6 +750,9 @@ static fc_status check_qcache(fc_ctx *ctx, const fc_qcache *c, int B, const char
   return FC_OK;
 }
 
+// Blocks of rows that a call's grid holds, a workgroup of 256 threads each: fewer than 2^32 threads.
+constexpr long kQGridBlocks = (1L << 24) - 1;
+
 // Buffers of one call: the first `written` are written, and share memory with no other one.
 struct QBuffers {
   const void *p[16];
@@ -796,6 +799,8 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
                 "one of q and q_out", who);
   const fc_qkv_rows &x = *rows;
   if ((st = check_qrows(c, x.n_heads, B, n, who)) != FC_OK) return st;
+  if ((n + 2L * FC_QCACHE_BLOCK - 2) / FC_QCACHE_BLOCK > kQGridBlocks)   // they may start inside a block
+    return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens in one call (at most 2^30 - 127)", who, n);
   const int *sec = rope->section;
   if (!(rope->theta > 1) || !std::isfinite(rope->theta))
     return fail(FC_ERR_INVALID_ARG, "%s: theta must be above 1", who);
@@ -890,6 +895,8 @@ fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *ds
                 who, keep, n_sink, n_recent);
   if (keep > dst->capacity)
     return fail(FC_ERR_SHAPE, "%s: keep %d above the destination's capacity %d", who, keep, dst->capacity);
+  if ((keep + FC_QCACHE_BLOCK - 1L) / FC_QCACHE_BLOCK > kQGridBlocks)
+    return fail(FC_ERR_UNSUPPORTED, "%s: keep %d (at most 2^30 - 64)", who, keep);
   QBuffers buf;
   buf.add(*dst, B);
   buf.add(kept, (size_t)B * src->n_kv_heads * keep * sizeof(int32_t));

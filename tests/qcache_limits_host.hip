@@ -61,6 +61,13 @@ int main() {
   fc_qkv_rows one = x;
   one.k_row = one.v_row = one.k_item = one.v_item = (int64_t)1 << 40;
   EXPECT(app(one, i32(12), 1), FC_ERR_HIP);
+  // a grid holds fewer than 2^32 threads: 2^24 - 1 workgroups of 256, 64 rows each, one more block
+  // where the rows start inside one
+  for (int n : {kRows, kRows - 64, kRows - 126}) EXPECT(app(x, i32(12), n), FC_ERR_UNSUPPORTED);
+  EXPECT(app(x, i32(12), kRows - 127), FC_ERR_HIP);
+  auto ev = [&](int keep) { return fc_qcache_evict(&ctx, &c, &d, i32(13), keep, 0, 0, i32(14), nullptr, 1, nullptr); };
+  for (int keep : {kRows, kRows - 63}) EXPECT(ev(keep), FC_ERR_UNSUPPORTED);
+  EXPECT(ev(kRows - 64), FC_ERR_HIP);
   std::printf(g_fail ? "%d failed\n" : "OK (%d failed expectations)\n", g_fail);
   return g_fail != 0;
 }
