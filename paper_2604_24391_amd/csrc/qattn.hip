@@ -46,7 +46,7 @@ struct QAttnArgs {
   float *logit;                      // [B KV][R][cap] scores (log2), or null
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, least, tile_rows, slots;
-  int *queue, pieces;                // k_qattn_rows: [8] pieces of work taken behind the first ones, or null
+  int *queue, pieces;                // k_qattn_rows: 8 counts of pieces taken behind the first ones, or null
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
 };
@@ -490,9 +490,18 @@ __device__ __forceinline__ QAttnArgs args_again() {
 // items are the longer ones, so the pairs move on by one with each round of them (8 items of 10 to
 // 4000 rows: 244 to 135 us; all of one length: up to 1 % slower).
 // QUEUE: as many workgroups as run at once, each going on with the next piece of its XCD's pairs, whose
-// keys are in its L2, then with the others' (queue[8]: pieces taken).  Sixteen frames of 704 to 1024
-// tokens, seven rounds: 548 us, 587 without; but a last round that is not full falls to few CUs (equal
-// items, 3.5 rounds: 392 and 357), so only ragged batches of four rounds or more go this way.
+// keys are in its L2, then with the others' (queue: pieces taken of each).  Batches whose items bring
+// different numbers of tokens (n_new is given; what it holds the host does not know) go this way from
+// four rounds of workgroups on, counted as if every token were there; in fewer a last round that is not
+// full falls to few CUs (3.5 rounds of equal items: 392 us so, 357 without).  With the queue and without:
+// sixteen frames of 704 to 1024 tokens, seven rounds, 522 and 541 us, with a key mask 608 and 665; of
+// 1024 each 624 and 660; 48 items of 171 to 256 tokens 345 and 348; 300 of 64 over 1000 keys 406 and 403;
+// where most tokens are missing the pieces without rows cost more so: 200 of 1024 tokens 127 and 129, 60
+// of them 89 and 55.
+// Counts lie 256 bytes apart: side by side their atomics wait for one another (1 token of 256 in 64
+// items 114 us instead of 60, 40 items of 300 over 500 keys 174 instead of 148).
+constexpr int kQueueStep = 64;
+
 template <int HD, int NW, bool QUEUE>
 __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
   constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
@@ -720,7 +729,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
       work(a, id);
       for (;;) {
         __syncthreads();
-        if (tid == 0) sm_next = (int)gridDim.x + 8 * atomicAdd(&a.queue[from], 1) + from;
+        if (tid == 0) sm_next = (int)gridDim.x + 8 * atomicAdd(&a.queue[kQueueStep * from], 1) + from;
         __syncthreads();
         id = __builtin_amdgcn_readfirstlane(sm_next);
         if (id < a.pieces) break;
@@ -731,7 +740,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
   }
 }
 
-__global__ void k_qattn_queue(int *queue) { queue[threadIdx.x] = 0; }
+__global__ void k_qattn_queue(int *queue) { queue[kQueueStep * threadIdx.x] = 0; }
 
 // The parts of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided
 // by the sum; 4 to 5 us beside a launch's 3.6.  With scores written down (R <= 32 rows), further workgroups turn them into the
@@ -1109,7 +1118,7 @@ fc_status run_qattn(fc_ctx *ctx, QAttnArgs &a, bool weigh, hipStream_t st) {
       return fail(FC_ERR_UNSUPPORTED, "fc_qcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
     a.pieces = (int)(pairs * tiles * splits);
     const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;   // workgroups that run at once
-    if (NW == 4 && !parts && a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 <= ws) {
+    if (NW == 4 && !parts && a.B > 1 && a.n_new && a.pieces >= 4 * once && at - ctx->part + 8 * kQueueStep <= ws) {
       a.queue = reinterpret_cast<int *>(at);
       hipLaunchKernelGGL(k_qattn_queue, dim3(1), dim3(8), 0, st, a.queue);
       FC_LAUNCH_OK(st, "k_qattn_queue");
