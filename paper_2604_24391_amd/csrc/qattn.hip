@@ -632,9 +632,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
       top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
       // the reference follows the maximum only where it is 2^8 behind: most blocks need not touch O,
       // and its sums stay within float32 while rows times their largest value are below 2^137
+      // (each row's by its own scores alone: another row's may come from keys that are hidden from it)
       if (__any(top > ref + 8.f)) {
-        const float mn = fmaxf(ref, top), corr = exp2_fast(ref - (mn == kNegInf ? 0.f : mn));
-        ref = mn;
+        const bool up = top > ref + 8.f;
+        const float corr = up ? exp2_fast(ref - top) : 1.f;
+        ref = up ? top : ref;
         sum *= corr;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= corr;

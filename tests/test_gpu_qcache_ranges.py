@@ -185,3 +185,40 @@ def test_many_rounds_masked(fc, ctx, heads, B, n, cap, odd):  # noqa: F811
         some = list(range(0, B, 9)) + [1, 5, B - 1]
         part = fc.QCache(*(t[some].contiguous() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.weight)))
         check_on_device(part, before[some], q[some], out[some], [held[b] for b in some], [new[b] for b in some], mask[some])
+
+
+@pytest.mark.parametrize("heads,n,cap,held", [("qwen", 1, 256, [130, 60]), ("toy", 6, 256, [130, 60]), ("qwen", 5, 2048, [1900, 700]), ("three", 40, 256, [130, 60]),
+                                              ("toy", 70, 256, [130, 60]), ("three", 40, 2048, [1900, 700]), ("qwen", 70, 512, [300, 64])])
+@pytest.mark.parametrize("masked", [False, True])
+def test_hidden_rows_leave_no_bit(fc, ctx, heads, n, cap, held, masked):  # noqa: F811
+    """A token's output and the weights of what it sees keep every bit whatever stands in rows that are
+    hidden from it: masked ones, those behind the last, and, for all but the last token, that one's
+    own (its key far above all others for some queries)."""
+    g = torch.Generator().manual_seed(100 + n)
+    H, kv, hd, _ = HEADS[heads]
+    cache = filled(fc, g, 2, kv, hd, cap)
+    q = randn(g, 2, n, H, hd)
+    mask = (torch.rand(2, cap, generator=g) > 0.3).to(torch.uint8).cuda() if masked else None
+    lens, w0 = ints(held), cache.weight.clone()
+    got = []
+    for change in (False, True):
+        for b in range(2) if change else ():
+            last = held[b] + n - 1
+            hide = torch.arange(cap, device="cuda") > last
+            if masked:
+                hide |= mask[b] == 0
+            junk = codes((torch.randn(cache.k[b].shape, generator=g) * 200).clamp(-448, 448)).cuda()
+            cache.k[b] = torch.where(hide[None, :, None], junk, cache.k[b])
+            junk = codes((torch.randn(cache.v[b].shape, generator=g) * 200).clamp(-448, 448)).cuda()
+            cache.v[b] = torch.where(hide.view(-1, 64)[None, :, None], junk, cache.v[b])
+            if n > 1:
+                cache.k[b, :, last] = codes((torch.randn(kv, hd, generator=g) * 400).clamp(-448, 448)).cuda()
+                cache.v[b, :, last // 64, :, last % 64] = codes((torch.randn(kv, hd, generator=g) * 400).clamp(-448, 448)).cuda()
+        cache.weight.copy_(w0)
+        out = torch.full_like(q, 9.0)
+        fc.fc_qcache_attention(ctx, cache, q, lens, None, out, key_mask=mask, accumulate=n == 1)
+        got.append((out, cache.weight.clone()))
+    seen = slice(0, n - 1) if n > 1 else slice(0, 1)
+    a, c = got[0][0][:, seen], got[1][0][:, seen]
+    assert torch.equal(a.view(torch.int16), c.view(torch.int16)), f"{int((a != c).sum())} outputs of {a.numel()} changed"
+    assert torch.equal(got[0][1], got[1][1])
