@@ -157,6 +157,22 @@ def test_numbers_of_splits(fc, wide_ctx, heads, B, n, cap, masked):  # noqa: F81
         assert torch.equal(out, first) and torch.equal(cache.weight, weight)
 
 
+@pytest.mark.parametrize("heads,B,n,cap,masked", [("qwen", 2, 2, 131072, False), ("wide", 1, 1, 524288, True), ("three", 4, 10, 65536, False)])
+def test_few_rows_whose_scores_do_not_fit(fc, ctx, heads, B, n, cap, masked):  # noqa: F811
+    """Weighed calls of a few rows over caches so large that the workspace has no room for their scores:
+    the weights compute them again."""
+    g = torch.Generator().manual_seed(60 + n)
+    H, kv, hd, _ = HEADS[heads]
+    cache = filled(fc, g, B, kv, hd, cap)
+    q = randn(g, B, n, H, hd)
+    held = [cap - n - 1000 * b - 17 if b < 3 else 5 for b in range(B)]
+    new = [max(1, n - b) for b in range(B)]
+    mask = (torch.rand(B, cap, generator=g) > 0.3).to(torch.uint8).cuda() if masked else None
+    before, out = cache.weight.clone(), torch.full_like(q, 9.0)
+    fc.fc_qcache_attention(ctx, cache, q, ints(held), ints(new), out, key_mask=mask, accumulate=True)
+    check_on_device(cache, before, q, out, held, new, mask)
+
+
 @pytest.mark.parametrize("heads,B,n,cap", [("qwen", 300, 20, 192), ("wide", 400, 26, 128)])
 @pytest.mark.parametrize("odd", [False, True])
 def test_many_rounds_masked(fc, ctx, heads, B, n, cap, odd):  # noqa: F811
