@@ -232,8 +232,10 @@ typedef struct {
  * what the tokens of an answer attend to.  Keys are held rotated, so rows may be dropped
  * without moving the others' positions.  Numbers are e4m3 (OCP, 0x7f / 0xff NaN); a number
  * stands for its code times the scale of its block of FC_QCACHE_BLOCK rows and key-value
- * head.  Scales are powers of two, at least 2^-100.  Rows behind those held are never read
- * for a result and may hold anything; every call leaves them as they are.  (host struct) */
+ * head.  Scales are powers of two from 2^-100 to 2^120 (there codes of 256 and more stand for
+ * numbers beyond float32: a key with one gives the tokens that see it no finite score).  Rows
+ * behind those held are never read for a result and may hold anything; every call leaves them
+ * as they are.  fc_layer_forward does not read this cache.  (host struct) */
 #define FC_QCACHE_BLOCK 64
 typedef struct {
   uint8_t *k;               /* [B][n_kv][capacity][head_dim]                               */
@@ -497,6 +499,7 @@ fc_status fc_phase_correlate_rotation(fc_ctx *ctx, const float *frames_prev,
  *   pos:   [axes][B][n] int32 positions (axes: 3, or 1 when every section is 0);
  *   len:   [B] int32 rows held before this call, the same for every layer's cache of a step
  *          (no call advances it: the caller adds n_new after the step's last layer);
+ *   n:     tokens of an item in the buffers, up to the capacity;
  *   n_new: [B] int32 rows that item b brings, its first n_new[b] of the n; NULL: all n;
  *   q_out: [B][n][n_heads][head_dim] bf16 rotated queries (NULL with q NULL); it may be q
  *          itself in that layout; no other buffer overlaps it or the cache's.  Rows from
@@ -506,8 +509,8 @@ fc_status fc_phase_correlate_rotation(fc_ctx *ctx, const float *frames_prev,
  * grows).  Numbers are rounded to nearest even from float32; an infinity is held as
  * +-448 s, a NaN as a NaN, and neither sets the scale.  The new rows' weights are set to 0.
  * Rows past the capacity are dropped, their q_out (and out, in the attention) left as it is.
- * Counts outside their ranges are clamped.  FC_ERR_UNSUPPORTED for more than 2^30 - 127 tokens or
- * 2^30 rows (tokens times heads) an item. */
+ * Counts outside their ranges are clamped.  FC_ERR_UNSUPPORTED for more than 65535 heads,
+ * 2^30 - 127 tokens or 2^30 rows (tokens times heads) an item. */
 fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_axes *rope,
                            const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
                            const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
@@ -520,22 +523,23 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  *   q:        [B][n][n_heads][head_dim] bf16, rotated (q_out of the append);
  *   len, n_new: as given to the append;
  *   key_mask: [B][capacity] uint8 (16-byte aligned), or NULL: every row is seen;
- *   out:      [B][n][n_heads][head_dim] bf16: softmax(scale q k) v; a token that sees no
- *             row gets 0; tokens from n_new[b] on are left as they are; no other buffer
- *             overlaps it;
+ *   out:      [B][n][n_heads][head_dim] bf16: softmax(scale q k) v, its probabilities rounded
+ *             to bf16 before the product with v (their sum and the weights not); a token
+ *             that sees no row gets 0; tokens from n_new[b] on are left as they are; no
+ *             other buffer overlaps it;
  *   scale:    finite, usually 1 / sqrt(head_dim);
  *   accumulate: 1: weight[b][h][j] += the sum of the probabilities that row j has received
  *             from the tokens and the query heads of its group (cache->weight is needed).
  * What is hidden from a token has no effect on it, whatever its bytes.  Outputs are summed in
  * float32, which holds every mean of finite numbers while the rows that a token sees times the
  * largest of their values are below 2^137 (any number of rows up to values of 1e32, 512 of the
- * largest of bfloat16).  The partial results
- * use the context's partial-sum workspace: fewer splits where it is small, and
- * FC_ERR_CAPACITY when accumulate needs more rows than it holds (one float for each of the
- * B n n_heads rows).  FC_ERR_UNSUPPORTED, before anything is launched, for more than 2^30 rows
- * (tokens times heads) an item, and for calls that need 2^24 workgroups or more: one for each 128
- * rows of each item's key-value heads and each of their splits, and, where accumulate computes the
- * scores again, one for each 256 rows of capacity. */
+ * largest of bfloat16).
+ * The partial results use the context's partial-sum workspace: fewer splits where it is small,
+ * and FC_ERR_CAPACITY when accumulate needs more rows than it holds (one float for each of the
+ * B n n_heads rows).  FC_ERR_UNSUPPORTED, before anything is launched, for more than 65535 heads
+ * or 2^30 rows (tokens times heads) an item, and for calls that need 2^24 workgroups or more:
+ * one for each 128 rows of each item's key-value heads and each of their splits, and, where
+ * accumulate computes the scores again, one for each 256 rows of capacity. */
 fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_t *q,
                               const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
                               uint16_t *out, int32_t n_heads, float scale, int32_t accumulate,
@@ -545,7 +549,11 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
  * first n_sink, the last n_recent and, of those between, the keep - n_sink - n_recent of
  * largest weight (equal weights: the lower row; -0 equals 0, a NaN counts as the lowest
  * finite number) go into dst in their order, with their weights; every row when
- * len[b] <= keep.  dst's blocks get the smallest scale for their rows.
+ * len[b] <= keep.  dst's blocks get the smallest scale for their rows.  There is no key mask
+ * here: rows that one has hidden from the attention compete like others, and count among the
+ * first and the last.  Heads keep rows of their own, so that afterwards a row's number means
+ * another token in each head, and a key_mask, which has no head axis, cannot hide a token any
+ * more: what is to stay hidden is kept out of the cache (n_new), not masked in it.
  *   src, dst: caches of the same heads and head_dim that share no memory (callers alternate
  *             two caches, or pass one spare on from layer to layer); src->weight is needed,
  *             dst->weight may be NULL; dst->capacity >= keep;

@@ -186,11 +186,13 @@ __device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 
 
 // All rows of an item (MT tiles of 16: up to 32) against a run of its key blocks, which go round the 4
 // waves; these are joined in LDS.  An item's only slot writes the outputs, several their parts.
-// Memory bounds it (MT = 1: about 1000 vector cycles for a block's 16 KB, at 8 waves on a CU
-// several times what HBM delivers), so loads run ahead: each next block's keys are read when the
+// HBM bounds it over long caches (MT = 1: about 1000 vector cycles for a block's 16 KB, at 8 waves on
+// a CU several times what HBM delivers), so loads run ahead: each next block's keys are read when the
 // scores have used theirs, its values after the outputs.  Eight items of 40000 to 65535 rows (433 MB)
-// 70 us, 6.1 TB/s; sixteen of 2200 to 4200 (54 MB, in the memory-side cache) 16 us; one of 2176 7 us,
-// most of it the launch and one pass of latencies.
+// take 70 us, 6.1 TB/s.  Short shares are bound by latency: sixteen items of 2200 to 4200 rows (54 MB, in
+// the memory-side cache) 16 us, 3.4 TB/s, where a wave has three or four blocks and reads one more that
+// it does not use; one of 2176 6.5 us, most of it the launch and one pass.  Two tiles (17 to 32 rows)
+// take 366 registers at hd 128, one wave on a SIMD: 4 tokens of those sixteen items 30 us with the join.
 //
 // NT: loads without a place in the memory-side cache, for caches well beyond its 256 MB: 433 MB take
 // 75.6 us so and 83.6 otherwise, 337 MB 67.2 and 61.5, 54 MB 25.2 and 20.8 (part of what fits is
@@ -442,14 +444,15 @@ __global__ __launch_bounds__(256) void k_qattn(QAttnArgs a) {
 // which the DMA brings into LDS a block ahead (16 KB each at hd 128), in e4m3: half of the bytes that
 // bfloat16 tiles would be read back as, at the price that every wave converts them for itself.  32 x
 // 32 matrix instructions; a lane holds one row and, of a block's keys, the 32 of its half wave.
-// Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 PFLOP) take 548 us, 0.94
-// PFLOP/s; the first calls after a pause are slower.  The card's power bounds it: a plain matrix
-// product of these operations takes 370 us at the clock that is left to it, and the exponentials and
-// conversions, which hide behind the products in cycles, cost the rest in power.  Scores a block
-// ahead of the softmax (two ways), three waves on a SIMD or prefetched operands come out the same;
-// 64 rows in a wave, or blocks converted once per workgroup, slower (by half, by a tenth); without the
-// exponentials it is 8 % faster, without the keys' conversion 5.  256 tokens over 2176 rows: 23 us of
-// latencies, a block after the other in each workgroup.
+// Sixteen frames of up to 1024 tokens, 28 heads, over 2200 to 4200 rows (0.51 TFLOP) take 542 us, 0.95
+// PFLOP/s (564 on another box), a prompt of 8192 (0.48 TFLOP) 472.  Matrix instructions take 41 and 45 %
+// of a SIMD's cycles and vector ones (softmax, conversions) 60 and 64: together the whole, so at two waves
+// on a SIMD little of the one runs under the other.  The clock is 2.2 GHz of 2.4, in the first launches
+// after a pause 2.0 (595 us).  Scores a block ahead of the softmax (two ways), three waves on a SIMD or
+// prefetched operands come out the same; 64 rows in a wave, or blocks converted once per workgroup, slower
+// (by half, by a tenth); without the exponentials it is 8 % faster, without the keys' conversion 5.  256
+// tokens over 2176 rows: 22 us, eight or nine blocks one after the other on 224 workgroups, and their
+// start and end.
 //
 // LDS rows are 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks.
@@ -900,10 +903,11 @@ __global__ __launch_bounds__(256) void k_qattn_join_rows(QAttnArgs a) {
 // registers, as bfloat16, and the rows' queries pass by through LDS, 64 between barriers (32: 10 %
 // slower).  S^T puts the keys in a lane's registers, so its sums over rows stay there until the end.
 // Row ranges are dealt over `row_splits` workgroups, whose sums the next kernel adds up in order.
-// A prompt of 8192 rows (0.24 PFLOP) takes 311 us, 38 % of the matrix unit's cycles: the other terms,
-// an exponential and two more vector instructions for 32 matrix cycles, and one barrier for 64 rows,
-// add to the products rather than hide behind them at two waves on a SIMD (254 registers: the keys
-// are 64, scores and sums 64); without the exponentials it is a tenth faster.
+// A prompt of 8192 rows (0.24 TFLOP) takes 278 us (306 in the first launches after a pause), 38 % of the
+// matrix unit's cycles: the other terms, an exponential and two more vector instructions for 32 matrix
+// cycles, and one barrier for 64 rows, add to the products (53 % of cycles) rather than hide behind them
+// at two waves on a SIMD (252 registers: the keys are 64, scores and sums 64); without the exponentials
+// it is a tenth faster.
 constexpr int kWaveKeys = 64, kGroupKeys = 4 * kWaveKeys;
 
 template <int HD>

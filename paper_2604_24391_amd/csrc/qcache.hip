@@ -703,8 +703,8 @@ fc_status launch_qcache_append(fc_ctx *ctx, const fc_qcache &c, const fc_rope_ax
   const bool one = !(rope.section[0] || rope.section[1] || rope.section[2]);
   a.sec0 = one ? half : rope.section[0];
   a.sec1 = one ? half : rope.section[0] + rope.section[1];
-  // two powers and products of them (within 8 2^-53, as pow itself is within one; sixteen calls of
-  // pow take as long as a small launch)
+  // two powers and products of them (sixteen calls of pow take as long as a small launch): with pow
+  // within one unit in the last place, 2 2^-53, a factor is within 23 2^-53 and their product within 44
   const double r = std::pow(rope.theta, -2.0 / c.head_dim), r8 = std::pow(rope.theta, -16.0 / c.head_dim);
   a.lo[0] = 1.0 / (2.0 * M_PI), a.hi[0] = 1.0;
   for (int i = 1; i < 8; ++i) a.lo[i] = a.lo[i - 1] * r, a.hi[i] = a.hi[i - 1] * r8;

@@ -1021,7 +1021,9 @@ def fc_qcache_evict(ctx: Context, src: QCache, dst: QCache, lens: torch.Tensor, 
                     stream=None):
     """Of each item's lens[b] rows, head by head, the first `sink`, the last `recent` and those of
     largest weight between, `keep` in all, into dst in their order; their numbers go to kept
-    [B, n_kv, keep] int32 (-1 behind the last), min(lens, keep) to lens_out."""
+    [B, n_kv, keep] int32 (-1 behind the last), min(lens, keep) to lens_out.  Rows hidden by a
+    key_mask compete like others, and as each head keeps rows of its own, dst has no key_mask
+    that could hide them."""
     dev = ctx.device
     B, kv = src.k.shape[:2]
     if dst.k.shape[0] != B:
