@@ -530,7 +530,8 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
  *   scale:    finite, usually 1 / sqrt(head_dim);
  *   accumulate: 1: weight[b][h][j] += the sum of the probabilities that row j has received
  *             from the tokens and the query heads of its group (cache->weight is needed).
- * What is hidden from a token has no effect on it, whatever its bytes.  Outputs are summed in
+ * What is hidden from a token has no effect on it, whatever its bytes, nor have the scales of
+ * blocks all of whose rows are hidden.  Outputs are summed in
  * float32, which holds every mean of finite numbers while the rows that a token sees times the
  * largest of their values are below 2^137 (any number of rows up to values of 1e32, 512 of the
  * largest of bfloat16).

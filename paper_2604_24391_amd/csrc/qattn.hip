@@ -63,9 +63,12 @@ __device__ __forceinline__ bf16x8 dequant8(uint32_t w0, uint32_t w1, float s) {
 // it.  Scales reach 2^120, where codes of 256 and more stand for numbers beyond bfloat16 and 0 times
 // one (a hidden row's) would be NaN, and outputs are sums of up to 2^8 |v| a row before their division.
 // 17 is as far as the least number, 2^-109, stays a normal bfloat16; powers of two round nothing.
+// Blocks that nobody sees may hold any scale: what comes out is finite.
 constexpr uint32_t kValueDown = 17;
 constexpr float kValueUp = 131072.f;
-__device__ __forceinline__ float value_scale(float s) { return __uint_as_float(__float_as_uint(s) - (kValueDown << 23)); }
+__device__ __forceinline__ float value_scale(float s) {
+  return __uint_as_float((max(__float_as_uint(s) & 0x7FFFFFFFu, (127u + kQLowExp) << 23)) - (kValueDown << 23));
+}
 // What an unnormalised output is multiplied with, from its row's sum (a row that sees no key: 0).
 __device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : kValueUp / l; }
 // LDS words that lanes of one wave write in parts and read whole, and the order between the two.

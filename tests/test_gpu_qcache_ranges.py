@@ -238,3 +238,31 @@ def test_hidden_rows_leave_no_bit(fc, ctx, heads, n, cap, held, masked):  # noqa
     a, c = got[0][0][:, seen], got[1][0][:, seen]
     assert torch.equal(a.view(torch.int16), c.view(torch.int16)), f"{int((a != c).sum())} outputs of {a.numel()} changed"
     assert torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("heads,n,cap,held", [("qwen", 1, 512, [400, 300]), ("toy", 6, 512, [400, 300]), ("qwen", 2, 2048, [1900, 700]), ("three", 40, 512, [400, 300]),
+                                              ("toy", 70, 512, [400, 300]), ("three", 40, 2048, [1900, 700])])
+def test_hidden_blocks_of_any_scale(fc, ctx, heads, n, cap, held):  # noqa: F811
+    """Whole blocks hidden by the mask (rows counted as held that nothing was written to): neither their
+    codes nor their scales have an effect, whatever they hold."""
+    g = torch.Generator().manual_seed(110 + n)
+    H, kv, hd, _ = HEADS[heads]
+    cache = filled(fc, g, 2, kv, hd, cap)
+    q = randn(g, 2, n, H, hd)
+    mask = torch.ones(2, cap, dtype=torch.uint8, device="cuda")
+    mask[0, :128], mask[1, 64:256] = 0, 0
+    w0, lens, got = cache.weight.clone(), ints(held), []
+    odd = [float("nan"), float("inf"), float("-inf"), 0.0, -1.0, 3.4e38, 1e-44, 5.0, 2.0 ** -111, -2.0 ** -111]
+    for junk in (None, *odd):
+        if junk is not None:
+            for b, blocks in ((0, (0, 1)), (1, (1, 2, 3))):
+                for blk in blocks:
+                    cache.k_scale[b, :, blk] = cache.v_scale[b, :, blk] = junk
+                    cache.k[b, :, 64 * blk:64 * blk + 64] = codes((torch.randn(kv, 64, hd, generator=g) * 200).clamp(-448, 448)).cuda()
+                    cache.v[b, :, blk] = codes((torch.randn(kv, hd, 64, generator=g) * 200).clamp(-448, 448)).cuda()
+        cache.weight.copy_(w0)
+        out = torch.full_like(q, 9.0)
+        fc.fc_qcache_attention(ctx, cache, q, lens, None, out, key_mask=mask, accumulate=True)
+        got.append((out.view(torch.int16), cache.weight.clone()))
+    for junk, (o, w) in zip(odd, got[1:]):
+        assert torch.equal(o, got[0][0]) and torch.equal(w, got[0][1]), f"scale {junk}"
