@@ -21,14 +21,12 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attn_dev.h"
 #include "fc_internal.h"
 #include "qcache.h"
 
 namespace fc {
 namespace {
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kNegInf = -__builtin_inff();
 
 struct QAttnArgs {
   const uint8_t *k, *v;
@@ -71,13 +69,6 @@ __device__ __forceinline__ float value_scale(float s) {
 }
 // What an unnormalised output is multiplied with, from its row's sum (a row that sees no key: 0).
 __device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : kValueUp / l; }
-// LDS words that lanes of one wave write in parts and read whole, and the order between the two.
-typedef uint16_t __attribute__((may_alias)) part16;
-typedef uint32_t __attribute__((may_alias)) part32;
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
 // Bytes of w that hold a NaN (0x7f or 0xff): their top bits, and as 0x01 each.
 __device__ __forceinline__ uint32_t nan_tops(uint32_t w) { return (w & 0x7F7F7F7Fu) + 0x01010101u; }
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return nan_tops(w) >> 7 & 0x01010101u; }
@@ -85,100 +76,9 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return nan_tops(w) >
 __device__ __forceinline__ uint32_t byte_bits(uint32_t n) { return (n * 0x01020408u) >> 24 & 15u; }
 // The four low bits of b as bytes of 0xff.
 __device__ __forceinline__ uint32_t bit_bytes(uint32_t b) { return ((b & 15u) * 0x00204081u & 0x01010101u) * 255u; }
-// The bits of a block's 64 keys below `seen` (relative to the block's first).
-__device__ __forceinline__ uint64_t seen_bits(int seen) {
-  return seen >= 64 ? ~0ull : (seen <= 0 ? 0ull : (1ull << seen) - 1ull);
-}
 // Bytes of w that are not zero, as 0xff each.
 __device__ __forceinline__ uint32_t set_bytes(uint32_t w) {
   return ((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) >> 7 & 0x01010101u) * 255u;
-}
-// Eight query elements, their signs turned where the scale is negative.
-__device__ __forceinline__ bf16x8 load_q(const uint16_t *src, uint32_t flip) {
-  u32x4 w = *reinterpret_cast<const u32x4 *>(src);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] ^= flip;
-  return __builtin_bit_cast(bf16x8, w);
-}
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Splits that the key blocks of one tile of rows are dealt over (k_qattn_rows): lengths are known on
-// the device only, so the grid has room for `splits`, and a short item uses no more than leaves
-// each of them `least` blocks.
-__device__ __forceinline__ int splits_used(int kmax, const QAttnArgs &a) {
-  return max(1, min(a.splits, (kmax + a.least * kQBlock - 1) / (a.least * kQBlock)));
-}
-// k_qattn deals a.slots workgroups of each key-value head over the items by their lengths, `per`
-// blocks to each: with the same number for every item, the longest one of a ragged batch would
-// keep few CUs busy to the end.  Items take ceil(blocks / per) slots in order; per is the smallest
-// number with which they suffice, but at least four blocks (one per wave).
-struct Share {
-  int item, start, used, per;       // the item, its first slot, its slots, blocks of each
-  int held, m;                      // its rows held and new
-};
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return __builtin_amdgcn_readfirstlane(x);
-}
-// The share of the item that slot `slot` falls to (item -1: none).
-__device__ __forceinline__ Share share_of(const QAttnArgs &a, int slot) {
-  const int lane = threadIdx.x & 63;
-  int held = 0, m = 0;                // of item i + lane
-  auto blocks = [&](int i) {
-    const int j = min(i + lane, a.B - 1);
-    held = min(max(a.len[j], 0), a.cap);
-    m = min(a.n_new ? min(max(a.n_new[j], 0), a.n) : a.n, a.cap - held);
-    return i + lane < a.B && m > 0 ? (held + m + kQBlock - 1) / kQBlock : 0;
-  };
-  if (a.slots == a.B) {               // one workgroup for each item
-    held = q_held(a.len, slot, a.cap), m = q_new(a.n_new, slot, a.n, held, a.cap);
-    return Share{m > 0 ? slot : -1, slot, 1, a.cap / kQBlock, held, m};
-  }
-  int x = blocks(0);
-  if (a.B == 1) {
-    const int n = __builtin_amdgcn_readfirstlane(x), per = max(4, (n + a.slots - 1) / a.slots), used = (n + per - 1) / per;
-    return Share{slot < used ? 0 : -1, 0, used, per, __builtin_amdgcn_readfirstlane(held), __builtin_amdgcn_readfirstlane(m)};
-  }
-  // (counts below 2^30: a cache of 2^42 bytes is the largest there is)
-  auto slots_of = [&](int per) {      // per 0: the blocks themselves
-    int all = 0;
-    for (int i = 0; i < a.B; i += 64) {
-      if (a.B > 64) x = blocks(i);
-      all += wave_sum(per ? (int)((unsigned)(x + per - 1) / (unsigned)per) : x);
-    }
-    return all;
-  };
-  const int all = slots_of(0);
-  int lo = max(4, (all + a.slots - 1) / a.slots), hi = max(lo, (all + a.slots - a.B - 1) / (a.slots - a.B));
-  while (lo < hi) {                   // hi suffices: the quotients round up by less than one each
-    const int mid = (lo + hi) / 2;
-    if (slots_of(mid) <= a.slots) hi = mid;
-    else lo = mid + 1;
-  }
-  const int per = lo;
-  if (a.B > 64) x = blocks(0);
-  int run = 0;
-  for (int i = 0;;) {
-    const int u = (int)((unsigned)(x + per - 1) / (unsigned)per);
-    int inc = u;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o);
-      if (lane >= o) inc += y;
-    }
-    const int at = run + inc - u;
-    const unsigned long long hit = __ballot(slot >= at && slot < at + u);
-    if (hit) {
-      const int l = __ffsll((long long)hit) - 1;
-      return Share{i + l, __builtin_amdgcn_readlane(at, l), __builtin_amdgcn_readlane(u, l), per,
-                   __builtin_amdgcn_readlane(held, l), __builtin_amdgcn_readlane(m, l)};
-    }
-    run += __builtin_amdgcn_readlane(inc, 63);
-    i += 64;
-    if (i >= a.B) return Share{-1, 0, 0, per, 0, 0};
-    x = blocks(i);
-  }
 }
 // log2 of the sum of 2^S of a row from its maximum and sum: the probability of key j is 2^(S_j - L).
 // A row that sees no key gets +inf (every weight 0).
@@ -465,31 +365,6 @@ __device__ __forceinline__ int key_swz(int row) {
 }
 __device__ __forceinline__ int val_swz(int dim) { return (dim >> 2) & 3; }
 
-// LDS DMA of 4 B per lane to lds + 4 * lane (lds must be wave-uniform), as dma16.
-__device__ __forceinline__ void dma4(const void *gp, uint32_t lds) {
-  const uint32_t l = __builtin_amdgcn_readfirstlane(lds);
-  uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %2\n\t"
-      "global_load_lds_dword %1, off\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(gp), "s"(l)
-      : "memory");
-}
-
-// The kernel's arguments read anew, which keeps no register between two reads.
-__device__ __forceinline__ QAttnArgs args_again() {
-  typedef const __attribute__((address_space(4))) uint32_t *Words;
-  Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(p));
-  struct { uint32_t w[sizeof(QAttnArgs) / 4]; } x;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(QAttnArgs) / 4); ++i) x.w[i] = p[i];
-  return __builtin_bit_cast(QAttnArgs, x);
-}
-
 // Pieces of work are numbered by pairs (item and key-value head), then splits, then tiles of rows, the
 // last rows, which see most keys, first.  Workgroups go round the 8 XCDs in turn and start in order:
 // an XCD that kept to its pairs, as P is often a multiple of 8, would make the others wait whenever its
@@ -504,10 +379,6 @@ __device__ __forceinline__ QAttnArgs args_again() {
 // 1024 each 624 and 660; 48 items of 171 to 256 tokens 345 and 348; 300 of 64 over 1000 keys 406 and 403;
 // where most tokens are missing the pieces without rows cost more so: 200 of 1024 tokens 127 and 129, 60
 // of them 89 and 55.
-// Counts lie 256 bytes apart: side by side their atomics wait for one another (1 token of 256 in 64
-// items 114 us instead of 60, 40 items of 300 over 500 keys 174 instead of 148).
-constexpr int kQueueStep = 64;
-
 template <int HD, int NW, bool QUEUE>
 __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
   constexpr int PC = HD / 16;                   // 16-byte pieces of a key row
@@ -733,7 +604,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_qattn_rows(QAttnArgs args) {
     __shared__ int sm_next;
     int id = blockIdx.x, from = blockIdx.x % 8;
     for (int done = 0;;) {             // queues found empty
-      const QAttnArgs a = args_again();
+      const QAttnArgs a = args_again<QAttnArgs>();
       work(a, id);
       for (;;) {
         __syncthreads();
