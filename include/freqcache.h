@@ -21,7 +21,10 @@
  *
  * Beside it, for what an episode keeps beyond the frame window and for the tokens of an
  * answer: a token cache in 8 bits, written, attended to and cut down by fc_qcache_append,
- * fc_qcache_attention and fc_qcache_evict.
+ * fc_qcache_attention and fc_qcache_evict.  Where several answers or rollouts go on from one
+ * history, or episodes of unlike length share the memory, there is a token cache in pages, in
+ * bfloat16: fc_pcache_append, fc_pcache_attention, fc_pcache_step (pages for new rows, forks,
+ * rows given up) and fc_pcache_compact.
  *
  * Conventions for every call:
  *   - Pointers are DEVICE pointers unless marked (host).  The caller allocates
@@ -247,6 +250,30 @@ typedef struct {
   int32_t head_dim;         /* 64 or 128 */
   int32_t capacity;         /* rows of each item and head; a multiple of 64, up to 2^30 */
 } fc_qcache;
+
+/* The paged token cache: rows of keys (rotated) and values in bfloat16, in pages that items
+ * share a pool of.  One state serves every layer: which page holds an item's rows, and how many
+ * items hold a page.  Row j of item b lies in page table[b][j / page_rows], at row j mod
+ * page_rows; several items may hold a page (answers that go on from one history), which then
+ * none of them may write: fc_pcache_step sees to it.  An entry outside 0 .. n_pages - 1 is no
+ * page: its rows are dropped when written, and hidden.  Rows of a page that no item has written
+ * may hold anything.  The number of rows that each item holds is the caller's, as with
+ * fc_qcache.  fc_layer_forward does not read this cache.  (host struct) */
+#define FC_PCACHE_TILE 8
+typedef struct {
+  uint16_t *k;              /* [n_pages][n_kv][page_rows][head_dim]                        */
+  uint16_t *v;              /* [n_pages][n_kv][page_rows / 8][head_dim][8]: by columns of
+                               eight rows; like k 16-byte aligned                       */
+  int32_t *state;           /* fc_pcache_state_bytes bytes, 16-byte aligned: table
+                               [B][max_pages], zeros up to a multiple of four numbers, and
+                               holders [n_pages] (table entries that name each page)    */
+  int32_t n_kv_heads;
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t page_rows;        /* a power of two from 16 to 1024 */
+  int32_t n_pages;
+  int32_t max_pages;        /* of an item; max_pages page_rows up to 2^30, with the items of a
+                               call B max_pages up to 2^28 and 2^36 rows                */
+} fc_pcache;
 
 /* Rotary positions on up to three axes (time, row, column): the rotary pairs
  * (i, i + head_dim / 2) are split into sections of section[0..2] pairs (sum head_dim / 2),
@@ -566,6 +593,76 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
 fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *dst,
                           const int32_t *len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           int32_t *kept, int32_t *len_out, int32_t B, void *stream);
+
+/* Bytes of the state of B items of up to max_pages pages each and a pool of n_pages (0 for counts
+ * below 1 and for B max_pages above 2^30).  (host function, no device work) */
+size_t fc_pcache_state_bytes(int32_t B, int32_t max_pages, int32_t n_pages);
+
+/* An empty state: every table entry -1, no page held.  Stream-ordered. */
+fc_status fc_pcache_init(fc_ctx *ctx, const fc_pcache *cache, int32_t B, void *stream);
+
+/* New rows into the paged cache: queries and keys rotated by their positions (float32, rounded to
+ * nearest even), keys and values into their rows' pages, for item b the rows len[b] .. len[b] +
+ * n_new[b] - 1.  Arguments and their limits as in fc_qcache_append, with max_pages page_rows as
+ * the capacity.  Rows without a page are dropped (their q_out is written), rows past the capacity
+ * too (their q_out left as it is).  The pages must be the item's own where rows are written
+ * (fc_pcache_step has granted them): of two items that write one row either may win. */
+fc_status fc_pcache_append(fc_ctx *ctx, const fc_pcache *cache, const fc_rope_axes *rope,
+                           const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
+                           const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
+                           void *stream);
+
+/* Attention of n tokens per item over the paged cache, their own rows (appended before) among it:
+ * token i of item b, i < n_new[b], attends to the rows j <= len[b] + i that have a page and, with
+ * a key_mask, key_mask[b][j] not 0.  One token, a chunk or a whole prompt; the work is split over
+ * the keys where there are few rows.
+ *   q, out:   [B][n][n_heads][head_dim] bf16; out is softmax(scale q k) v, its probabilities
+ *             rounded to bf16 before the product with v (their sum not); a token that sees no row
+ *             gets 0; tokens from n_new[b] on are left as they are; no other buffer overlaps out;
+ *   key_mask: [B][max_pages page_rows] uint8 (16-byte aligned), or NULL: every row is seen;
+ *   scale:    finite, usually 1 / sqrt(head_dim).
+ * What is hidden from a token has no effect on it, whatever its bytes.  Outputs are summed in
+ * float32, which holds every mean of finite numbers while the rows that a token sees times the
+ * largest of their values are below 2^137; a probability below 2^-100 of the token's largest may
+ * count as 0.  The output of a token that sees a value that is not finite is not finite there.
+ * The partial results use the context's partial-sum workspace: fewer splits where it is small.
+ * FC_ERR_UNSUPPORTED, before anything is launched, for more than 65535 heads, 2^30 rows (tokens
+ * times heads) an item, or 2^24 workgroups (one for each 128 rows of each item's key-value heads
+ * and each of their splits). */
+fc_status fc_pcache_attention(fc_ctx *ctx, const fc_pcache *cache, const uint16_t *q,
+                              const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
+                              uint16_t *out, int32_t n_heads, float scale, int32_t B, int32_t n,
+                              void *stream);
+
+/* The state's step, before the rows of a step are appended, for the caches of n_layers layers
+ * at once (host array; same state and sizes, else FC_ERR_SHAPE; no two pools overlap): item b goes
+ * on from the first len[b] rows of item src[b], and gets pages for n_new[b] more.
+ *   src:     [B] int32 or NULL (every item goes on from its own rows).  Items that take the same
+ *            src share its pages.  A source outside 0 .. B - 1 is none: the item holds no page;
+ *   len:     [B] int32 rows that the item keeps (0 ends it); pages behind them are let go;
+ *   n_new:   [B] int32 rows that it is about to append, from 0 to n, or NULL: n;
+ *   granted: [B] int32 receives how many of them have a page of the item's own: n_new[b], or
+ *            fewer where pages run out (or where max_pages page_rows rows are full, or the last
+ *            kept row's place has no page: 0).
+ * Table entries behind the item's rows become -1, the holders are counted anew.  New pages are the
+ * free ones of lowest number, given to the items in order, first for a copy, then behind the kept
+ * rows.  A partly filled last page that several table entries hold is copied, in every layer, for
+ * each item about to write it, but for the last one where all its holders write: the copy's rows
+ * are those held, rounded up to a multiple of eight.  Where a
+ *            copy finds no page, its item is granted 0, and so is every later one that would
+ *            write that page.
+ * Uses the context's partial-sum workspace (FC_ERR_CAPACITY when B max_pages + 4 B + 4 n_pages
+ * numbers exceed it); allocates nothing. */
+fc_status fc_pcache_step(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers,
+                         const int32_t *src, const int32_t *len, const int32_t *n_new, int32_t n,
+                         int32_t *granted, int32_t B, void *stream);
+
+/* Live pages (those with holders, L of them) moved to the numbers below L, in every layer: the
+ * k-th live page from number L on goes to the k-th free page below it; the table and the holders
+ * follow, and *live (device, may be NULL) receives L.  Pages from L on are then free, and their
+ * memory can be given to something else.  Limits as for fc_pcache_step. */
+fc_status fc_pcache_compact(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers, int32_t *live,
+                            int32_t B, void *stream);
 
 /* Debug mode (process-wide): after every kernel launch the library waits for the
  * launch stream and reports an error raised while the kernel ran as FC_ERR_HIP from

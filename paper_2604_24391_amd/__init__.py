@@ -15,4 +15,6 @@ from .freqcache import (  # noqa: F401
     MergerDesc, VitCache, VitDesc,
     select_state_bytes, select_state_alloc, fc_slot_map_init, slot_state_alloc,
     slot_state_bytes, fc_version, lib, token_grid,
-    fc_qcache_append, fc_qcache_attention, fc_qcache_evict, QCACHE_BLOCK, QCache, RopeAxes)
+    fc_qcache_append, fc_qcache_attention, fc_qcache_evict, QCACHE_BLOCK, QCache, RopeAxes,
+    fc_pcache_append, fc_pcache_attention, fc_pcache_compact, fc_pcache_init, fc_pcache_step,
+    pcache_state_bytes, PCACHE_TILE, PageState, PCache)

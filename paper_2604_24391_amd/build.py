@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libfreqcache.so")
 SOURCES = ["abi.hip", "select.hip", "pixpc.hip", "layer.hip", "slotmap.hip", "vit.hip", "qcache.hip",
-           "qattn.hip"]
+           "qattn.hip", "pcache.hip", "pattn.hip"]
 
 # gfx950 only.  Packed-FP32 instructions are disabled for all device code.
 FLAGS = [

@@ -776,13 +776,57 @@ struct QBuffers {
   }
 };
 
-static fc_status check_qrows(const fc_qcache &c, int n_heads, int B, int n, const char *who) {
-  if (n_heads < 1 || n_heads % c.n_kv_heads)
-    return fail(FC_ERR_SHAPE, "%s: n_kv_heads %d does not divide n_heads %d", who, c.n_kv_heads, n_heads);
-  if (n < 1 || n > c.capacity) return fail(FC_ERR_SHAPE, "%s: n=%d tokens, capacity %d", who, n, c.capacity);
+static fc_status check_qrows(int n_kv_heads, int capacity, int n_heads, int n, const char *who) {
+  if (n_heads < 1 || n_heads % n_kv_heads)
+    return fail(FC_ERR_SHAPE, "%s: n_kv_heads %d does not divide n_heads %d", who, n_kv_heads, n_heads);
+  if (n < 1 || n > capacity) return fail(FC_ERR_SHAPE, "%s: n=%d tokens, capacity %d", who, n, capacity);
   if (n_heads > 65535) return fail(FC_ERR_UNSUPPORTED, "%s: %d heads (at most 65535)", who, n_heads);
   if ((long)n * n_heads > (1L << 30))
     return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens of %d heads (at most 2^30 rows an item)", who, n, n_heads);
+  return FC_OK;
+}
+
+static fc_status check_rope(const fc_rope_axes &rope, int hd, const char *who) {
+  const int *sec = rope.section;
+  if (!(rope.theta > 1) || !std::isfinite(rope.theta))
+    return fail(FC_ERR_INVALID_ARG, "%s: theta must be above 1", who);
+  if ((sec[0] || sec[1] || sec[2]) &&
+      (sec[0] < 0 || sec[1] < 0 || sec[2] < 0 || (long)sec[0] + sec[1] + sec[2] != hd / 2))
+    return fail(FC_ERR_INVALID_ARG, "%s: rotary sections %d/%d/%d must sum to head_dim/2 = %d", who,
+                sec[0], sec[1], sec[2], hd / 2);
+  return FC_OK;
+}
+
+// The rows of an append and what goes with them, beside the cache's buffers in buf.
+static fc_status check_appended(QBuffers &buf, const fc_qkv_rows &x, const fc_rope_axes &rope, int n_kv, int hd,
+                                const int32_t *pos, const int32_t *len, const int32_t *n_new, uint16_t *q_out,
+                                int B, int n, const char *who) {
+  const uint16_t *in[3] = {x.q, x.k, x.v};
+  const int64_t row[3] = {x.q_row, x.k_row, x.v_row}, item[3] = {x.q_item, x.k_item, x.v_item};
+  const size_t qb = (size_t)B * n * x.n_heads * hd * 2, ib = (size_t)B * sizeof(int32_t);
+  const int32_t *sec = rope.section;
+  const int axes = sec[0] || sec[1] || sec[2] ? 3 : 1;
+  buf.add(q_out, qb);
+  buf.end_written();
+  buf.add(pos, (size_t)axes * n * ib);
+  buf.add(len, ib);
+  buf.add(n_new, ib);
+  if ((uintptr_t)q_out % 16) return fail(FC_ERR_INVALID_ARG, "%s: q_out must be 16-byte aligned", who);
+  for (int i = 0; i < 3; ++i) {
+    if (!in[i]) continue;
+    if ((uintptr_t)in[i] % 16 || row[i] < 0 || item[i] < 0 || row[i] % 8 || item[i] % 8 ||
+        row[i] > (1L << 40) || item[i] > (1L << 40) || (n > 1 && row[i] > (1L << 60) / (n - 1)))
+      return fail(FC_ERR_INVALID_ARG, "%s: q, k and v must be 16-byte aligned, with strides that are "
+                  "multiples of 8 elements, not negative and up to 2^40 (2^60 over a call's tokens)", who);
+    const int width = (i ? n_kv : x.n_heads) * hd;
+    const size_t bytes = ((size_t)(B - 1) * item[i] + (size_t)(n - 1) * row[i] + width) * 2;
+    const bool same = i == 0 && x.q == q_out && (n == 1 || row[0] == width) &&
+                      (B == 1 || item[0] == (int64_t)n * width);
+    if (!same) buf.add(in[i], bytes);
+  }
+  if (buf.clash())
+    return fail(FC_ERR_INVALID_ARG, "%s: q_out or a buffer of the cache overlaps another one (q_out may "
+                "be q itself in the same layout)", who);
   return FC_OK;
 }
 
@@ -798,43 +842,14 @@ fc_status fc_qcache_append(fc_ctx *ctx, const fc_qcache *cache, const fc_rope_ax
     return fail(FC_ERR_INVALID_ARG, "%s: null rotary description, rows, positions or lengths, or only "
                 "one of q and q_out", who);
   const fc_qkv_rows &x = *rows;
-  if ((st = check_qrows(c, x.n_heads, B, n, who)) != FC_OK) return st;
+  if ((st = check_qrows(c.n_kv_heads, c.capacity, x.n_heads, n, who)) != FC_OK) return st;
   if ((n + 2L * FC_QCACHE_BLOCK - 2) / FC_QCACHE_BLOCK > kQGridBlocks)   // they may start inside a block
     return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens in one call (at most 2^30 - 127)", who, n);
-  const int *sec = rope->section;
-  if (!(rope->theta > 1) || !std::isfinite(rope->theta))
-    return fail(FC_ERR_INVALID_ARG, "%s: theta must be above 1", who);
-  if ((sec[0] || sec[1] || sec[2]) &&
-      (sec[0] < 0 || sec[1] < 0 || sec[2] < 0 || (long)sec[0] + sec[1] + sec[2] != c.head_dim / 2))
-    return fail(FC_ERR_INVALID_ARG, "%s: rotary sections %d/%d/%d must sum to head_dim/2 = %d", who,
-                sec[0], sec[1], sec[2], c.head_dim / 2);
-  const uint16_t *in[3] = {x.q, x.k, x.v};
-  const int64_t row[3] = {x.q_row, x.k_row, x.v_row}, item[3] = {x.q_item, x.k_item, x.v_item};
-  const size_t qb = (size_t)B * n * x.n_heads * c.head_dim * 2, ib = (size_t)B * sizeof(int32_t);
-  const int axes = sec[0] || sec[1] || sec[2] ? 3 : 1;
+  if ((st = check_rope(*rope, c.head_dim, who)) != FC_OK) return st;
   QBuffers buf;
   buf.add(c, B);
-  buf.add(q_out, qb);
-  buf.end_written();
-  buf.add(pos, (size_t)axes * n * ib);
-  buf.add(len, ib);
-  buf.add(n_new, ib);
-  if ((uintptr_t)q_out % 16) return fail(FC_ERR_INVALID_ARG, "%s: q_out must be 16-byte aligned", who);
-  for (int i = 0; i < 3; ++i) {
-    if (!in[i]) continue;
-    if ((uintptr_t)in[i] % 16 || row[i] < 0 || item[i] < 0 || row[i] % 8 || item[i] % 8 ||
-        row[i] > (1L << 40) || item[i] > (1L << 40) || (n > 1 && row[i] > (1L << 60) / (n - 1)))
-      return fail(FC_ERR_INVALID_ARG, "%s: q, k and v must be 16-byte aligned, with strides that are "
-                  "multiples of 8 elements, not negative and up to 2^40 (2^60 over a call's tokens)", who);
-    const int width = (i ? c.n_kv_heads : x.n_heads) * c.head_dim;
-    const size_t bytes = ((size_t)(B - 1) * item[i] + (size_t)(n - 1) * row[i] + width) * 2;
-    const bool same = i == 0 && x.q == q_out && (n == 1 || row[0] == width) &&
-                      (B == 1 || item[0] == (int64_t)n * width);
-    if (!same) buf.add(in[i], bytes);
-  }
-  if (buf.clash())
-    return fail(FC_ERR_INVALID_ARG, "%s: q_out or a buffer of the cache overlaps another one (q_out may "
-                "be q itself in the same layout)", who);
+  st = check_appended(buf, x, *rope, c.n_kv_heads, c.head_dim, pos, len, n_new, q_out, B, n, who);
+  if (st != FC_OK) return st;
   DeviceScope dev(ctx);
   if (dev.st != FC_OK) return dev.st;
   return fc::launch_qcache_append(ctx, c, *rope, x, pos, len, n_new, q_out, B, n,
@@ -852,7 +867,7 @@ fc_status fc_qcache_attention(fc_ctx *ctx, const fc_qcache *cache, const uint16_
   if (!q || !len || !out) return fail(FC_ERR_INVALID_ARG, "%s: null queries, lengths or output", who);
   if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)key_mask) % 16)
     return fail(FC_ERR_INVALID_ARG, "%s: q, out and key_mask must be 16-byte aligned", who);
-  if ((st = check_qrows(c, n_heads, B, n, who)) != FC_OK) return st;
+  if ((st = check_qrows(c.n_kv_heads, c.capacity, n_heads, n, who)) != FC_OK) return st;
   if (!std::isfinite(scale)) return fail(FC_ERR_INVALID_ARG, "%s: scale must be finite", who);
   if (accumulate != 0 && accumulate != 1)
     return fail(FC_ERR_INVALID_ARG, "%s: accumulate %d (0 or 1)", who, accumulate);
@@ -911,6 +926,181 @@ fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *ds
   if (dev.st != FC_OK) return dev.st;
   return fc::launch_qcache_evict(ctx, *src, *dst, len, keep, n_sink, n_recent, kept, len_out, B,
                                  reinterpret_cast<hipStream_t>(stream));
+}
+
+// ------------------------------------------------------------------------------- paged cache
+static fc_status check_pcache(fc_ctx *ctx, const fc_pcache *c, int B, const char *who) {
+  if (!ctx) return fail(FC_ERR_INVALID_ARG, "%s: null context", who);
+  if (!c) return fail(FC_ERR_INVALID_ARG, "%s: null cache descriptor", who);
+  if (!c->k || !c->v || !c->state) return fail(FC_ERR_INVALID_ARG, "%s: null cache buffer", who);
+  if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->state) % 16)
+    return fail(FC_ERR_INVALID_ARG, "%s: the cache's k, v and state must be 16-byte aligned", who);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(FC_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128)", who, c->head_dim);
+  if (c->page_rows < 16 || c->page_rows > 1024 || (c->page_rows & (c->page_rows - 1)))
+    return fail(FC_ERR_SHAPE, "%s: pages of %d rows (a power of two from 16 to 1024)", who, c->page_rows);
+  if (c->n_pages < 1 || c->max_pages < 1 || (long)c->max_pages * c->page_rows > (1L << 30))
+    return fail(FC_ERR_SHAPE, "%s: %d pages, up to %d of %d rows an item (at least 1, up to 2^30 rows)", who,
+                c->n_pages, c->max_pages, c->page_rows);
+  if (B < 1 || c->n_kv_heads < 1 || (long)B * c->n_kv_heads > 65535)
+    return fail(FC_ERR_SHAPE, "%s: B=%d items of %d key-value heads (B n_kv from 1 to 65535)", who, B,
+                c->n_kv_heads);
+  if ((long)B * c->max_pages > (1L << 28) || (long)B * c->max_pages * c->page_rows > (1L << 36))
+    return fail(FC_ERR_UNSUPPORTED, "%s: a table of %d x %d pages (at most 2^28, of 2^36 rows)", who, B, c->max_pages);
+  if ((long)c->n_pages * c->n_kv_heads > (1L << 41) / c->page_rows / c->head_dim)
+    return fail(FC_ERR_UNSUPPORTED, "%s: a pool of more than 2^42 bytes", who);
+  return FC_OK;
+}
+
+static size_t pool_bytes(const fc_pcache &c) { return (size_t)c.n_pages * c.n_kv_heads * c.page_rows * c.head_dim * 2; }
+static size_t state_bytes(const fc_pcache &c, int B) { return fc::pcache_state_bytes(B, c.max_pages, c.n_pages); }
+
+// The caches of a plan's layers: alike, apart from each other and from the state.
+static fc_status check_pcaches(fc_ctx *ctx, const fc_pcache *c, int n_layers, int B, const char *who) {
+  if (n_layers < 1 || n_layers > 65536) return fail(FC_ERR_SHAPE, "%s: %d layers (1 to 65536)", who, n_layers);
+  fc_status st = check_pcache(ctx, c, B, who);
+  if (st != FC_OK) return st;
+  const size_t bytes = pool_bytes(*c);
+  std::vector<std::pair<uintptr_t, size_t>> at;
+  try {
+    at.reserve(2 * (size_t)n_layers + 1);
+    at.emplace_back((uintptr_t)c->state, state_bytes(*c, B));
+    for (int l = 0; l < n_layers; ++l) {
+      const fc_pcache &x = c[l];
+      if (!x.k || !x.v || ((uintptr_t)x.k | (uintptr_t)x.v) % 16)
+        return fail(FC_ERR_INVALID_ARG, "%s: null or unaligned pool of layer %d", who, l);
+      if (x.state != c->state || x.n_kv_heads != c->n_kv_heads || x.head_dim != c->head_dim ||
+          x.page_rows != c->page_rows || x.n_pages != c->n_pages || x.max_pages != c->max_pages)
+        return fail(FC_ERR_SHAPE, "%s: layer %d's cache has another state or other sizes than the first one's", who, l);
+      at.emplace_back((uintptr_t)x.k, bytes);
+      at.emplace_back((uintptr_t)x.v, bytes);
+    }
+    std::sort(at.begin(), at.end());
+  } catch (const std::bad_alloc &) {
+    return fail(FC_ERR_INVALID_ARG, "%s: out of host memory", who);
+  }
+  for (size_t i = 1; i < at.size(); ++i)
+    if (at[i].first < at[i - 1].first + at[i - 1].second)
+      return fail(FC_ERR_INVALID_ARG, "%s: two pools, or a pool and the state, overlap", who);
+  if (fc::pcache_plan_numbers(B, c->max_pages, c->n_pages) > (long)ctx->part_elems)
+    return fail(FC_ERR_CAPACITY, "%s: a table of %d x %d pages and %d pages exceed the context's workspace", who, B,
+                c->max_pages, c->n_pages);
+  return FC_OK;
+}
+
+// Whether a small buffer overlaps the state or one of the layers' pools.
+static bool in_pcaches(const fc_pcache *c, int n_layers, int B, const void *p, size_t n) {
+  const size_t bytes = pool_bytes(*c);
+  if (fc::overlap2(p, n, c->state, state_bytes(*c, B))) return true;
+  for (int l = 0; l < n_layers; ++l)
+    if (fc::overlap2(p, n, c[l].k, bytes) || fc::overlap2(p, n, c[l].v, bytes)) return true;
+  return false;
+}
+
+size_t fc_pcache_state_bytes(int32_t B, int32_t max_pages, int32_t n_pages) {
+  if (B < 1 || max_pages < 1 || n_pages < 1 || (long)B * max_pages > (1L << 28)) return 0;
+  return fc::pcache_state_bytes(B, max_pages, n_pages);
+}
+
+fc_status fc_pcache_init(fc_ctx *ctx, const fc_pcache *cache, int32_t B, void *stream) {
+  fc_status st = check_pcache(ctx, cache, B, "fc_pcache_init");
+  if (st != FC_OK) return st;
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_pcache_init(ctx, *cache, B, reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_pcache_append(fc_ctx *ctx, const fc_pcache *cache, const fc_rope_axes *rope,
+                           const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,
+                           const int32_t *n_new, uint16_t *q_out, int32_t B, int32_t n,
+                           void *stream) {
+  const char *who = "fc_pcache_append";
+  fc_status st = check_pcache(ctx, cache, B, who);
+  if (st != FC_OK) return st;
+  const fc_pcache &c = *cache;
+  if (!rope || !rows || !rows->k || !rows->v || !pos || !len || (!rows->q) != (!q_out))
+    return fail(FC_ERR_INVALID_ARG, "%s: null rotary description, rows, positions or lengths, or only "
+                "one of q and q_out", who);
+  const fc_qkv_rows &x = *rows;
+  if ((st = check_qrows(c.n_kv_heads, c.max_pages * c.page_rows, x.n_heads, n, who)) != FC_OK) return st;
+  if ((n + 2L * FC_PCACHE_TILE - 2) / FC_PCACHE_TILE > kQGridBlocks)   // they may start inside a group of rows
+    return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens in one call (at most 2^27 - 22)", who, n);
+  if ((st = check_rope(*rope, c.head_dim, who)) != FC_OK) return st;
+  QBuffers buf;
+  buf.add(c.k, pool_bytes(c));
+  buf.add(c.v, pool_bytes(c));
+  const size_t sb = state_bytes(c, B);
+  if (fc::overlap2(c.state, sb, c.k, pool_bytes(c)) || fc::overlap2(c.state, sb, c.v, pool_bytes(c)) ||
+      fc::overlap2(c.state, sb, q_out, (size_t)B * n * x.n_heads * c.head_dim * 2))
+    return fail(FC_ERR_INVALID_ARG, "%s: the state overlaps a pool or q_out", who);
+  st = check_appended(buf, x, *rope, c.n_kv_heads, c.head_dim, pos, len, n_new, q_out, B, n, who);
+  if (st != FC_OK) return st;
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_pcache_append(ctx, c, *rope, x, pos, len, n_new, q_out, B, n,
+                                  reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_pcache_attention(fc_ctx *ctx, const fc_pcache *cache, const uint16_t *q,
+                              const int32_t *len, const int32_t *n_new, const uint8_t *key_mask,
+                              uint16_t *out, int32_t n_heads, float scale, int32_t B, int32_t n,
+                              void *stream) {
+  const char *who = "fc_pcache_attention";
+  fc_status st = check_pcache(ctx, cache, B, who);
+  if (st != FC_OK) return st;
+  const fc_pcache &c = *cache;
+  if (!q || !len || !out) return fail(FC_ERR_INVALID_ARG, "%s: null queries, lengths or output", who);
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)key_mask) % 16)
+    return fail(FC_ERR_INVALID_ARG, "%s: q, out and key_mask must be 16-byte aligned", who);
+  if ((st = check_qrows(c.n_kv_heads, c.max_pages * c.page_rows, n_heads, n, who)) != FC_OK) return st;
+  if (!std::isfinite(scale)) return fail(FC_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  const size_t qb = (size_t)B * n * n_heads * c.head_dim * 2, ib = (size_t)B * sizeof(int32_t);
+  QBuffers buf;
+  buf.add(out, qb);
+  buf.end_written();
+  buf.add(c.k, pool_bytes(c));
+  buf.add(c.v, pool_bytes(c));
+  buf.add(c.state, state_bytes(c, B));
+  buf.add(q, qb);
+  buf.add(key_mask, (size_t)B * c.max_pages * c.page_rows);
+  buf.add(len, ib);
+  buf.add(n_new, ib);
+  if (buf.clash()) return fail(FC_ERR_INVALID_ARG, "%s: out overlaps another buffer", who);
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_pcache_attention(ctx, c, q, len, n_new, key_mask, out, n_heads, scale, B, n,
+                                     reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_pcache_step(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers,
+                         const int32_t *src, const int32_t *len, const int32_t *n_new, int32_t n,
+                         int32_t *granted, int32_t B, void *stream) {
+  const char *who = "fc_pcache_step";
+  fc_status st = check_pcaches(ctx, caches, n_layers, B, who);
+  if (st != FC_OK) return st;
+  if (!len || !granted) return fail(FC_ERR_INVALID_ARG, "%s: null lengths or granted", who);
+  if (n < 0) return fail(FC_ERR_SHAPE, "%s: n=%d rows", who, n);
+  const size_t ib = (size_t)B * sizeof(int32_t);
+  if (in_pcaches(caches, n_layers, B, granted, ib) || in_pcaches(caches, n_layers, B, len, ib) ||
+      in_pcaches(caches, n_layers, B, src, ib) || in_pcaches(caches, n_layers, B, n_new, ib) ||
+      fc::overlap2(granted, ib, len, ib) || fc::overlap2(granted, ib, src, ib) || fc::overlap2(granted, ib, n_new, ib))
+    return fail(FC_ERR_INVALID_ARG, "%s: a buffer that is written overlaps another one", who);
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_pcache_step(ctx, caches, n_layers, src, len, n_new, n, granted, B,
+                                reinterpret_cast<hipStream_t>(stream));
+}
+
+fc_status fc_pcache_compact(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers, int32_t *live,
+                            int32_t B, void *stream) {
+  const char *who = "fc_pcache_compact";
+  fc_status st = check_pcaches(ctx, caches, n_layers, B, who);
+  if (st != FC_OK) return st;
+  if (in_pcaches(caches, n_layers, B, live, sizeof(int32_t)))
+    return fail(FC_ERR_INVALID_ARG, "%s: live lies in a pool or in the state", who);
+  DeviceScope dev(ctx);
+  if (dev.st != FC_OK) return dev.st;
+  return fc::launch_pcache_compact(ctx, caches, n_layers, live, B, reinterpret_cast<hipStream_t>(stream));
 }
 
 size_t fc_slot_state_bytes(int32_t B, int32_t S) { return fc::slot_state_bytes(B, S); }

@@ -256,6 +256,21 @@ fc_status launch_qcache_evict(fc_ctx *ctx, const fc_qcache &s, const fc_qcache &
                               int keep, int sink, int recent, int32_t *kept, int32_t *len_out, int B,
                               hipStream_t st);
 
+// The paged token cache (pcache.hip, pattn.hip).
+size_t pcache_state_bytes(long B, long width, long pages);
+long pcache_plan_numbers(long B, long width, long pages);   // floats of the workspace that a plan takes
+fc_status launch_pcache_init(fc_ctx *ctx, const fc_pcache &c, int B, hipStream_t st);
+fc_status launch_pcache_append(fc_ctx *ctx, const fc_pcache &c, const fc_rope_axes &rope,
+                               const fc_qkv_rows &x, const int32_t *pos, const int32_t *len,
+                               const int32_t *n_new, uint16_t *q_out, int B, int n, hipStream_t st);
+fc_status launch_pcache_attention(fc_ctx *ctx, const fc_pcache &c, const uint16_t *q, const int32_t *len,
+                                  const int32_t *n_new, const uint8_t *key_mask, uint16_t *out, int n_heads,
+                                  float scale, int B, int n, hipStream_t st);
+fc_status launch_pcache_step(fc_ctx *ctx, const fc_pcache *c, int n_layers, const int32_t *src,
+                             const int32_t *len, const int32_t *n_new, int n, int32_t *granted, int B,
+                             hipStream_t st);
+fc_status launch_pcache_compact(fc_ctx *ctx, const fc_pcache *c, int n_layers, int32_t *live, int B, hipStream_t st);
+
 fc_status upload_select_tables();
 
 }  // namespace fc

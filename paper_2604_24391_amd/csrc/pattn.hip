@@ -1,0 +1,746 @@
+// Attention of new rows over the paged token cache.
+//
+//   S_ij = c q_i . k_j over the rows j <= held + i that have a page and that the key mask shows,
+//   P = softmax_j(S), out_i = sum_j P_ij v_j (a row that sees no key: 0).
+//
+// Laid out as the attention over the 8-bit cache (qattn.hip): the n tokens of an item make R = n G rows
+// of a matrix product per key-value head, S^T = K Q^T and O^T = V^T P^T, so that a lane holds one
+// query row and its softmax is per-lane scalars; the rows of an S^T tile are permuted so that a
+// lane's probabilities are those of neighbouring keys, the B operand of the second product as it
+// stands.  Operands are bfloat16 as the cache stores them.  P is rounded to bfloat16 for the second
+// product (half a step, 2^-8 of each term of a float32 sum whose terms err apart).
+//
+// Probabilities and their sums are held 2^-17 smaller than they are, which their quotient does not
+// show: sums of outputs before the division then stay within float32 for up to 2^9 rows of the
+// largest numbers of bfloat16.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "attn_dev.h"
+#include "fc_internal.h"
+#include "pcache.h"
+
+namespace fc {
+namespace {
+
+struct PAttnArgs {
+  const uint16_t *k, *v;
+  PageTable t;
+  const uint16_t *q;
+  uint16_t *out;
+  const int32_t *len, *n_new;
+  const uint8_t *mask;               // [B][cap], or null
+  float2 *ml;                        // reference (log2) and sum of each split's rows
+  float *part;                       // unnormalised outputs: k_pattn [KV][slots][R][hd], k_pattn_rows as
+                                     // k_pattn_join_rows has it
+  int2 *plan;                        // [B] k_pattn: an item's first slot and its slots
+  float c;                           // scale log2(e)
+  int B, n, H, KV, G, cap, splits, least, tile_rows, slots;
+  int *queue, pieces;                // k_pattn_rows: 8 counts of pieces taken behind the first ones, or null
+  Quot by_g;                         // division by G
+  uint32_t flip;                     // sign bits of a query pair to turn
+};
+
+constexpr float kProbDown = 17.f;    // log2
+
+__device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// Values that are not finite.  0 times one is NaN, so where some row may not see a block whole they become
+// 0 before the product, and what the rows that see them get for them is added afterwards.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+// Their kinds, for one column of 64 keys: NaN, +inf, -inf.
+struct OddKeys {
+  uint64_t kind[3];
+};
+// Eight values of a column: those that are not finite become 0; their bits by kind.
+__device__ __forceinline__ void take_odd(u32x4 &w, uint32_t *bits) {
+  bits[0] = bits[1] = bits[2] = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t x = w[i] >> (16 * s) & 0xFFFFu;
+      if ((x & 0x7F80u) != 0x7F80u) continue;
+      bits[(x & 0x7Fu) ? 0 : (x >> 15) + 1] |= 1u << (2 * i + s);
+      w[i] &= s ? 0x0000FFFFu : 0xFFFF0000u;
+    }
+}
+// What a row that sees `keys` of the column gets for them.
+__device__ __forceinline__ float odd_sum(const OddKeys &o, uint64_t keys) {
+  const bool up = o.kind[1] & keys, down = o.kind[2] & keys;
+  const float inf = __builtin_inff();
+  return (o.kind[0] & keys) || (up && down) ? __builtin_nanf("") : up ? inf : down ? -inf : 0.f;
+}
+
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const uint16_t *p) {
+  const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+  return NT ? __builtin_nontemporal_load(q) : *q;
+}
+
+// All rows of an item (MT tiles of 16: up to 32) against a run of its key blocks, which go round the 4
+// waves; these are joined in LDS.  An item's only slot writes the outputs, several their parts.
+// Loads run ahead: each next block's keys are read when the scores have used theirs, its values after
+// the outputs, its page numbers a block before both.
+template <int HD, int MT, bool NT>
+__global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAttnArgs a) {
+  constexpr int KC = HD / 32;                   // 16-byte pieces of a key row that a lane holds
+  constexpr int DT = HD / 16;                   // output tiles of 16 dims
+  constexpr int OS = HD + 4;
+  __shared__ float sm_o[4][16][OS];
+  __shared__ float2 sm_ml[4][16 * MT];
+  __shared__ float sm_l[16];
+  __shared__ OddKeys sm_odd[4][HD];
+  const Share sh = share_of(a, blockIdx.x);
+  if (sh.item < 0) return;
+  const int b = sh.item, kv = blockIdx.y, R = a.n * a.G;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+  const int held = sh.held, m = sh.m, rows = m * a.G;   // m > 0
+  const int kmax = held + m;                    // keys that any row sees
+  const int kall = held + 1;                    // keys that every row sees, but for the mask
+  const int blocks = (kmax + kKeyBlock - 1) / kKeyBlock, blo = (blockIdx.x - sh.start) * sh.per;
+  const int bhi = min(blocks - blo, sh.per) + blo;
+  const long slot = (long)kv * a.slots + blockIdx.x;
+  if (a.plan && kv == 0 && blo == 0 && tid == 0) a.plan[b] = make_int2(sh.start, sh.used);
+  // S^T row m of tile t is key (m / 4) 16 + 4 t + m % 4
+  const int in_page = (1 << a.t.shift) - 1;
+  const uint16_t *kbase = a.k + (l16 & 3) * HD + g * 8, *vbase = a.v + l16 * kPTile;
+  auto rows_of = [&](int page, int j) { return ((((long)page * a.KV + kv) << a.t.shift) + (j & in_page)) * HD; };
+  // page of the 16 keys that lane group x holds in block blk (blocks behind the last one are read as it)
+  auto page_of = [&](int blk, int x) { return a.t.entry(b, min((blk * kKeyBlock + 16 * x) >> a.t.shift, a.t.width - 1)); };
+  u32x4 kw[4][KC], vw[2][DT];
+  auto load_k = [&](int blk, int page) {
+    const uint16_t *p = kbase + rows_of(a.t.safe(page), blk * kKeyBlock + (l16 >> 2) * 16);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < KC; ++i) kw[t][i] = load16<NT>(p + 4 * t * HD + 32 * i);
+  };
+  auto load_v = [&](int blk, int page) {
+    const uint16_t *p = vbase + rows_of(a.t.safe(page), blk * kKeyBlock + g * 16);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vw[s][d] = load16<NT>(p + s * (HD * kPTile) + 16 * d * kPTile);
+  };
+  const int last = (a.cap + kKeyBlock - 1) / kKeyBlock - 1;
+  int at = min(blo + wave, last), next = min(at + 4, last);
+  int kp = page_of(at, l16 >> 2), vp = page_of(at, g);
+  int kp_next = page_of(next, l16 >> 2), vp_next = page_of(next, g);
+  // mask bytes of the lane's 16 keys, a block ahead as well
+  const uint8_t *mbase = a.mask ? a.mask + (long)b * a.cap : nullptr;
+  u32x4 mw = {~0u, ~0u, ~0u, ~0u};
+  auto load_mask = [&](int blk) {
+    mw = *reinterpret_cast<const u32x4 *>(mbase + min(blk * kKeyBlock + 16 * g, a.cap - 16));
+  };
+  if (mbase) load_mask(at);
+  load_k(at, kp);
+  load_v(at, vp);
+  bf16x8 q[MT][KC];
+  int seen[MT];                                 // keys that the lane's row sees
+  f32x4 o[MT][DT];
+  float mx[MT], sum[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int r = 16 * t + l16, tok = a.by_g(min(r, rows - 1));
+    seen[t] = r < rows ? held + tok + 1 : 0;
+    const uint16_t *src = a.q + (((long)b * a.n + tok) * a.H + kv * a.G + min(r, rows - 1) - tok * a.G) * HD;
+#pragma unroll
+    for (int i = 0; i < KC; ++i) q[t][i] = load_q(src + 32 * i + g * 8, a.flip);
+    mx[t] = kNegInf, sum[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0, 0, 0, 0};
+  }
+
+  for (int blk = blo + wave; blk < bhi; blk += 4) {
+    const int j0 = blk * kKeyBlock, jg = j0 + 16 * g;
+    next = min(blk + 4, last);
+    const int after = min(blk + 8, last);
+    const bool whole = __all(a.t.there(vp));
+    const bool full = !a.mask && j0 + kKeyBlock <= kall && whole;
+    uint32_t vis = 0xFFFFu;                       // the lane's 16 keys that some row may see
+    if (!full) {
+      if (mbase) {
+        vis = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vis |= (mw[i] >> (8 * e) & 0xFFu ? 1u : 0u) << (4 * i + e);
+        load_mask(next);
+      }
+      const int left = kmax - jg;
+      vis &= left >= 16 ? 0xFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+      if (!a.t.there(vp)) vis = 0;
+    }
+    bool odd = false;
+    if (!full) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) any |= odd_halves(vw[s][d][i]);
+      odd = __any(any != 0);
+      if (odd) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint32_t lo[3], hi[3];
+          take_odd(vw[0][d], lo);
+          take_odd(vw[1][d], hi);
+#pragma unroll
+          for (int x = 0; x < 3; ++x)
+            reinterpret_cast<part16 *>(&sm_odd[wave][16 * d + l16].kind[x])[g] = (uint16_t)(lo[x] | hi[x] << 8);
+        }
+        wave_lds_order();
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      f32x4 s[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[x][i]), q[t][i], s[x], 0, 0, 0);
+      }
+      if (t == MT - 1) load_k(next, kp_next);
+      const uint32_t sees = full ? 0xFFFFu : vis & (uint32_t)seen_bits(seen[t] - jg);
+      float top = kNegInf;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float y = s[x][e] * a.c;
+          if (!full) y = sees >> (4 * x + e) & 1u ? y : kNegInf;
+          s[x][e] = y;
+          top = fmaxf(top, y);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(mx[t], top);
+      const float ref = mn == kNegInf ? 0.f : mn;
+      const float corr = exp2_fast(mx[t] - ref);
+      mx[t] = mn;
+      float add = 0.f;
+      bf16x8 p[2];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = exp2_fast(s[x][e] - (ref + kProbDown));
+          add += y;
+          p[x >> 1][(x & 1) * 4 + e] = (__bf16)y;
+        }
+      sum[t] = sum[t] * corr + add;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        o[t][d] *= corr;
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vw[0][d]), p[0], o[t][d], 0, 0, 0);
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vw[1][d]), p[1], o[t][d], 0, 0, 0);
+      }
+      if (odd) {
+        uint64_t keys = (uint64_t)sees << (16 * g);   // that the lane's row sees
+        keys |= __shfl_xor(keys, 16);
+        keys |= __shfl_xor(keys, 32);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][d][e] += odd_sum(sm_odd[wave][16 * d + 4 * g + e], keys);
+      }
+    }
+    load_v(next, vp_next);
+    kp = kp_next, vp = vp_next;
+    kp_next = page_of(after, l16 >> 2), vp_next = page_of(after, g);
+  }
+
+  // the four waves' parts of each row, joined; a lane's group g holds the sum over its own keys
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    float s = sum[t];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (g == 0) sm_ml[wave][16 * t + l16] = make_float2(mx[t], s);
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    __syncthreads();
+    const float2 w0 = sm_ml[0][16 * t + l16], w1 = sm_ml[1][16 * t + l16], w2 = sm_ml[2][16 * t + l16],
+                 w3 = sm_ml[3][16 * t + l16];
+    const float mt = fmaxf(fmaxf(w0.x, w1.x), fmaxf(w2.x, w3.x)), ref = mt == kNegInf ? 0.f : mt;
+    const float f = exp2_fast(mx[t] - ref);
+    const float l = w0.y * exp2_fast(w0.x - ref) + w1.y * exp2_fast(w1.x - ref) +
+                    w2.y * exp2_fast(w2.x - ref) + w3.y * exp2_fast(w3.x - ref);
+    // O^T: lane (g, l16) holds dims 16 d + 4 g + e of row l16
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sm_o[wave][l16][16 * d + 4 * g + e] = o[t][d][e] * f;
+    const int rt = 16 * t;
+    if (wave == 0 && g == 0) {
+      if (a.ml && rt + l16 < rows) a.ml[slot * R + rt + l16] = make_float2(mt, l);
+      sm_l[l16] = l;
+    }
+    __syncthreads();
+    for (int x = tid; x < 16 * HD / 4; x += 256) {
+      const int row = x / (HD / 4), d = x % (HD / 4) * 4, r = rt + row;
+      if (r >= rows) continue;
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        y[e] = sm_o[0][row][d + e] + sm_o[1][row][d + e] + sm_o[2][row][d + e] + sm_o[3][row][d + e];
+      if (a.part) {
+        *reinterpret_cast<float4 *>(a.part + (slot * R + r) * HD + d) = make_float4(y[0], y[1], y[2], y[3]);
+      } else {
+        const float inv = output_factor(sm_l[row]);
+        const bf16x4 w = {(__bf16)(y[0] * inv), (__bf16)(y[1] * inv), (__bf16)(y[2] * inv), (__bf16)(y[3] * inv)};
+        *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
+      }
+    }
+  }
+}
+
+// The parts of one row joined by one workgroup: their outputs weighted by 2^(m_s - m) and divided by the
+// sum.
+template <int HD>
+__global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
+  constexpr int TPR = HD / 4, SG = 256 / TPR;
+  __shared__ float sm_y[SG][HD];
+  __shared__ float2 sm_ml[SG];
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tid = threadIdx.x;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int R = a.n * a.G, rows = m * a.G, r = blockIdx.x;
+  if (r >= rows) return;
+  // part s of row r: at + s R
+  const int2 sh = a.plan[b];          // (written, as the item has rows)
+  const long at = ((long)kv * a.slots + sh.x) * R + r;
+  const int used = sh.y, sg = tid / TPR, d = tid % TPR * 4;
+  float mt = kNegInf, l = 0.f;
+  f32x4 y = {0, 0, 0, 0};
+  for (int s = sg; s < used; s += SG) {
+    const float2 z = a.ml[(long)s * R + at];
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + ((long)s * R + at) * HD + d);
+    const float mn = fmaxf(mt, z.x), ref = mn == kNegInf ? 0.f : mn;
+    const float f = exp2_fast(mt - ref), h = exp2_fast(z.x - ref);
+    mt = mn;
+    l = l * f + z.y * h;
+    y = y * f + x * h;
+  }
+  if (tid % TPR == 0) sm_ml[sg] = make_float2(mt, l);
+  __syncthreads();
+  float top = kNegInf;
+#pragma unroll
+  for (int i = 0; i < SG; ++i) top = fmaxf(top, sm_ml[i].x);
+  const float ref = top == kNegInf ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < SG; ++i) sum += sm_ml[i].y * exp2_fast(sm_ml[i].x - ref);
+  *reinterpret_cast<f32x4 *>(&sm_y[sg][d]) = y * exp2_fast(mt - ref);
+  __syncthreads();
+  if (tid < TPR) {
+    f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < SG; ++i) t += *reinterpret_cast<const f32x4 *>(&sm_y[i][d]);
+    t *= output_factor(sum);
+    const bf16x4 w = {(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
+    *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + a.by_g(r)) * a.H + kv * a.G + r - a.by_g(r) * a.G) * HD + d) = w;
+  }
+}
+
+// More than 32 rows: 4 waves of 32 each (2 up to 64 rows) share the key blocks, which the DMA brings into
+// LDS a block ahead (32 KB at hd 128).  32 x 32 matrix instructions; a lane holds one row and, of a
+// block's keys, the 32 of its half wave.  Pieces of work go round the XCDs and, in ragged batches of
+// many rounds, into queues, as in k_qattn_rows.
+//
+// A row of keys is 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
+// together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks; columns of
+// values lie side by side as they are.
+template <int HD>
+__device__ __forceinline__ int pkey_swz(int row) {
+  return HD == 128 ? row & 15 : (row >> 1) & 7;
+}
+
+template <int HD, int NW, bool QUEUE>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnArgs args) {
+  constexpr int PC = HD / 8;                    // 16-byte pieces of a key row
+  constexpr int DT = HD / 32;                   // output tiles of 32 dims
+  constexpr int TILE = kKeyBlock * HD * 2;      // bytes of a block's keys, and of its values
+  constexpr int DMAS = TILE / 1024 / NW;        // DMA instructions of a wave for either
+  constexpr int SUBS = 4 / NW;                  // runs of 16 rows that a wave brings, DMAS / SUBS instructions each
+  constexpr int ROWS = 32 * NW;
+  constexpr int STAGES = 2;
+  __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
+  __shared__ OddKeys sm_odd[NW][HD];
+  __shared__ __align__(16) uint8_t sm_mask[STAGES][NW][256];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  auto work = [&](const PAttnArgs &a, int id) {
+    const int P = a.B * a.KV, R = a.n * a.G;
+    const int rest = id / P, hb = QUEUE ? id % P : (id % P + rest) % P, split = rest % a.splits;
+    const int r0 = ((R + ROWS - 1) / ROWS - 1 - rest / a.splits) * ROWS;
+    const int b = hb / a.KV, kv = hb % a.KV;
+    const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+    const int rows = m * a.G;
+    if (r0 >= rows) return;
+    const int kmax = held + a.by_g(min(r0 + ROWS, rows) - 1) + 1;
+    const int blocks = (kmax + kKeyBlock - 1) / kKeyBlock, used = splits_used(kmax, a);
+    if (split >= used) return;
+    const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
+
+    // pages of a block's four runs of 16 rows: those that this wave brings, and the keys that have one
+    typedef const __attribute__((address_space(4))) int32_t *uniform_ints;
+    const uniform_ints table = (uniform_ints)(uintptr_t)(a.t.table + (long)b * a.t.width);
+    struct Pages {
+      int mine[SUBS];
+      uint64_t there;
+    };
+    auto pages_of = [&](int blk) {
+      Pages p;
+      p.there = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int e = table[min((blk * kKeyBlock + 16 * x) >> a.t.shift, a.t.width - 1)];
+        if (a.t.there(e)) p.there |= 0xFFFFull << (16 * x);
+#pragma unroll
+        for (int i = 0; i < SUBS; ++i)
+          if (x == wave * SUBS + i) p.mine[i] = a.t.safe(e);
+      }
+      return p;
+    };
+    const int in_page = (1 << a.t.shift) - 1;
+    int ksrc[DMAS];
+#pragma unroll
+    for (int i = 0; i < DMAS; ++i) {
+      const int p = (wave * DMAS + i) * 64 + lane, kr = p / PC;
+      ksrc[i] = (kr & 15) * HD + ((p % PC) ^ pkey_swz<HD>(kr)) * 8;
+    }
+    auto fetch = [&](int blk, int stage, const Pages &pg) {
+#pragma unroll
+      for (int i = 0; i < DMAS; ++i) {
+        constexpr int per = DMAS / SUBS;
+        const int u = wave * SUBS + i / per;
+        const long at = ((((long)pg.mine[i / per] * a.KV + kv) << a.t.shift) + ((blk * kKeyBlock + 16 * u) & in_page)) * HD;
+        dma16(a.k + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
+        dma16(a.v + at + (i % per * 64 + lane) * 8, lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
+      }
+      // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
+      if (a.mask) dma4(a.mask + (long)b * a.cap + min(blk * kKeyBlock + (lane & 15) * 4, a.cap - 4), lds_addr(&sm_mask[stage][wave][0]));
+    };
+
+    const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
+    const int seen = r < rows ? held + tok + 1 : 0;                              // keys that the lane's row sees
+    const int wmax = w0 < rows ? held + a.by_g(min(w0 + 32, rows) - 1) + 1 : 0;  // that any row of the wave sees
+    const int wall = held + a.by_g(w0) + 1;                                      // that every one does
+    const long at_q = (((long)b * a.n + tok) * a.H + head) * HD;
+    bf16x8 q[HD / 16];
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) q[i] = load_q(a.q + at_q + 16 * i + 8 * h, a.flip);
+    Pages pg = pages_of(blo), pg_next = pages_of(min(blo + 1, bhi - 1));
+    loads_done();
+    fetch(blo, 0, pg);
+
+    // S^T row x of tile t is key 32 t + x with bits 2 and 3 of x exchanged
+    const int kr = (l32 & 19) | ((l32 >> 2) & 1) << 3 | ((l32 >> 3) & 1) << 2;
+    const int koff = kr * HD * 2, kx = pkey_swz<HD>(kr);
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
+
+    int stage = 0;
+    for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
+      wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
+      lds_barrier();                   // every wave has left the other stage
+      const uint64_t there = pg.there;
+      if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1, pg_next);
+      pg = pg_next;
+      pg_next = pages_of(min(blk + 2, bhi - 1));
+      if (w0 >= rows) continue;        // it only brings its part of the blocks
+      const int j0 = blk * kKeyBlock;
+      f32x16 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bf16x8 w = *reinterpret_cast<const bf16x8 *>(&sm[stage][0][koff + t * 64 * HD + (((2 * i + h) ^ kx) * 16)]);
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i], s[t], 0, 0, 0);
+        }
+      // the keys that have a page and that the mask shows, and whether some row of the wave may not see
+      // the block whole
+      uint64_t shown = there;
+      if (a.mask) shown &= __ballot(sm_mask[stage][wave][lane] != 0);
+      const bool later = j0 + kKeyBlock > wall, part = later || shown != ~0ull;
+      uint64_t some = ~0ull;           // keys that some row may see
+      bool odd = false;
+      if (part) {
+        some = shown & seen_bits(wmax - j0);
+        // the lane's 32 keys: 16 i + 8 h + e
+        const uint64_t sees64 = (some & seen_bits(seen - j0)) >> (8 * h);
+        const uint32_t sees = __builtin_amdgcn_perm((uint32_t)(sees64 >> 32), (uint32_t)sees64, 0x06040200u);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
+      }
+      float top = kNegInf;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
+      // the reference follows the maximum only where it is 2^8 behind: most blocks need not touch O
+      // (each row's by its own scores alone: another row's may come from keys that are hidden from it)
+      if (__any(top > ref + 8.f)) {
+        const bool up = top > ref + 8.f;
+        const float corr = up ? exp2_fast(ref - top) : 1.f;
+        ref = up ? top : ref;
+        sum *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= corr;
+      }
+      const float sub = (ref == kNegInf ? 0.f : ref) + kProbDown;
+      // 16 keys of the block at a time: their values, their exponentials, their products
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        u32x4 vw[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][((2 * t + h) * HD + 32 * d + l32) * 16]);
+        if (part) {                    // as in k_pattn
+          uint32_t any = 0;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) any |= odd_halves(vw[d][x]);
+          if (__any(any != 0)) {
+            if (!odd) {
+#pragma unroll
+              for (int d = 0; d < DT; ++d) sm_odd[wave][32 * d + l32] = OddKeys{{0, 0, 0}};
+              wave_lds_order();
+            }
+            odd = true;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              uint32_t bits[3];
+              take_odd(vw[d], bits);
+#pragma unroll
+              for (int x = 0; x < 3; ++x)
+                reinterpret_cast<part8 *>(&sm_odd[wave][32 * d + l32].kind[x])[2 * t + h] = (uint8_t)bits[x];
+            }
+          }
+        }
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = exp2_fast(fmaf(s[t / 2][8 * (t % 2) + e], a.c, -sub));
+          sum += y;
+          p[e] = (__bf16)y;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw[d]), p, o[d], 0, 0, 0);
+      }
+      if (odd) {
+        const uint64_t keys = some & seen_bits(seen - j0);
+        wave_lds_order();
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] += odd_sum(sm_odd[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4], keys);
+        wave_lds_order();
+      }
+    }
+
+    sum += __shfl_xor(sum, 32);
+    if (r >= rows) return;
+    if (a.splits > 1) {
+      const long to = (long)split * P * R + (long)hb * R + r;
+      if (h == 0) a.ml[to] = make_float2(ref, sum);
+      f32x4 *dst = reinterpret_cast<f32x4 *>(a.part) + (((long)split * P + hb) * ((R + 31) / 32) + w0 / 32) * (HD / 8) * 64 + lane;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dst[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    } else {
+      const float inv = output_factor(sum);
+      uint16_t *dst = a.out + at_q;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x4 w = {(__bf16)(o[d][4 * j] * inv), (__bf16)(o[d][4 * j + 1] * inv), (__bf16)(o[d][4 * j + 2] * inv), (__bf16)(o[d][4 * j + 3] * inv)};
+          *reinterpret_cast<bf16x4 *>(dst + 32 * d + 8 * j + 4 * h) = w;
+        }
+    }
+  };
+  if constexpr (!QUEUE) {
+    work(args, blockIdx.x);
+  } else {
+    __shared__ int sm_next;
+    int id = blockIdx.x, from = blockIdx.x % 8;
+    for (int done = 0;;) {             // queues found empty
+      const PAttnArgs a = args_again<PAttnArgs>();
+      work(a, id);
+      for (;;) {
+        __syncthreads();
+        if (tid == 0) sm_next = (int)gridDim.x + 8 * atomicAdd(&a.queue[kQueueStep * from], 1) + from;
+        __syncthreads();
+        id = __builtin_amdgcn_readfirstlane(sm_next);
+        if (id < a.pieces) break;
+        if (++done == 8) return;
+        from = (from + 1) % 8;
+      }
+    }
+  }
+}
+
+__global__ void k_pattn_queue(int *queue) { queue[kQueueStep * threadIdx.x] = 0; }
+
+// The same for k_pattn_rows, whose rows are many and splits few: a workgroup joins 32 dims of 32 rows,
+// eight splits' parts in flight at a time.  Parts lie as that kernel's lanes hold them, [split][pair]
+// [32 rows][HD / 8][half wave][row] by four dims, so that both kernels move runs of 1 KB.
+template <int HD>
+__global__ __launch_bounds__(256) void k_pattn_join_rows(PAttnArgs a) {
+  constexpr int DT = HD / 32;
+  const int hb = blockIdx.y, b = hb / a.KV, kv = hb % a.KV, tile = blockIdx.x / DT, dt = blockIdx.x % DT;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = 32 * dt + 8 * wave + lane / 32 * 4;
+  const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
+  const int R = a.n * a.G, rows = m * a.G, r = tile * 32 + lane % 32;
+  if (r >= rows) return;
+  const int last = min(r / a.tile_rows * a.tile_rows + a.tile_rows, rows) - 1;
+  const int used = splits_used(held + a.by_g(last) + 1, a);
+  const long step = (long)a.B * a.KV * R, at = (long)hb * R + r, R32 = (R + 31) / 32;
+  const long pstep = (long)a.B * a.KV * R32 * (HD / 8) * 64;
+  const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part) + ((hb * R32 + tile) * (HD / 8) + 4 * dt + wave) * 64 + lane;
+  float mt = kNegInf, l = 0.f;
+  f32x4 y = {0, 0, 0, 0};
+  for (int s0 = 0; s0 < used; s0 += 8) {
+    float2 z[8];
+    f32x4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = min(s0 + i, used - 1);
+      z[i] = a.ml[p * step + at];
+      x[i] = part[p * pstep];
+    }
+    float mn = mt;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mn = fmaxf(mn, z[i].x);
+    const float ref = mn == kNegInf ? 0.f : mn, f = exp2_fast(mt - ref);
+    mt = mn;
+    l *= f;
+    y *= f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float h = exp2_fast(z[i].x - ref);
+      if (s0 + i >= used) break;
+      l += z[i].y * h;
+      y += x[i] * h;
+    }
+  }
+  y *= output_factor(l);
+  const int tok = a.by_g(r);
+  const bf16x4 w = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+  *reinterpret_cast<bf16x4 *>(a.out + (((long)b * a.n + tok) * a.H + kv * a.G + r - tok * a.G) * HD + d) = w;
+}
+
+template <int HD>
+fc_status run_pattn(fc_ctx *ctx, PAttnArgs &a, hipStream_t st) {
+  const long R = (long)a.n * a.G, pairs = (long)a.B * a.KV;
+  const bool many = R > 32;
+  const int MT = R <= 16 ? 1 : 2, NW = R <= 64 ? 2 : 4, tile = many ? 32 * NW : 16 * MT;
+  const long tiles = (R + tile - 1) / tile;
+  const long per = pairs * R, padded = many ? pairs * ((R + 31) / 32 * 32) : per, ws = (long)ctx->part_elems;
+  auto up4 = [](long x) { return (x + 3) / 4 * 4; };
+  const long plan = up4(2L * a.B), all_blocks = (a.cap + kKeyBlock - 1) / kKeyBlock;
+  long splits = 1, slots = a.B;
+  if (many) {
+    // as in run_qattn
+    const long units = pairs * tiles, spread = std::min<long>(ctx->num_cus / units, all_blocks / 4);
+    const long places = 8L / NW * ctx->num_cus;
+    splits = std::min<long>(places / units, all_blocks / 8);
+    a.least = spread >= splits ? 4 : 8;
+    splits = std::max<long>(1, std::max(spread, splits));
+    auto filled = [&](long s) { return (double)(units * s) / ((units * s + places - 1) / places * places); };
+    if (units < places)
+      for (long s = splits + 1; s <= 8 && all_blocks / s >= 16; ++s)
+        if (filled(s) > filled(splits) + 0.1) splits = s;
+    splits = std::max<long>(1, std::min<long>(splits, (ws - plan) / (up4(2 * per) + padded * HD)));
+  } else {
+    slots = ctx->num_cus / a.KV;
+    if (a.mask || HD == 64 || slots < 4L * a.B) slots = 2L * ctx->num_cus / a.KV;
+    slots = std::min<long>(slots, all_blocks / 4 * a.B);
+    slots = std::max<long>(a.B, std::min<long>(slots, (ws - plan - 4) / (a.KV * R * (HD + 2))));
+  }
+  const bool parts = many ? splits > 1 : slots > a.B;
+  a.splits = (int)splits;
+  a.tile_rows = tile;
+  a.slots = many ? 0 : (int)slots;
+  float *at = ctx->part;
+  if (parts) {
+    a.plan = reinterpret_cast<int2 *>(at);
+    at += plan;
+    a.part = at;
+    a.ml = reinterpret_cast<float2 *>(at + (many ? splits * padded : slots * a.KV * R) * HD);
+  }
+  if (many) {
+    if (pairs * tiles * splits > (1L << 24) - 1)   // nothing has been launched yet
+      return fail(FC_ERR_UNSUPPORTED, "fc_pcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
+    a.pieces = (int)(pairs * tiles * splits);
+    const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;     // workgroups that run at once
+    if (NW == 4 && !parts && a.B > 1 && a.n_new && a.pieces >= 4 * once && 8 * kQueueStep <= ws) {
+      a.queue = reinterpret_cast<int *>(at);
+      hipLaunchKernelGGL(k_pattn_queue, dim3(1), dim3(8), 0, st, a.queue);
+      FC_LAUNCH_OK(st, "k_pattn_queue");
+    }
+    ProfScope ps(ctx, st, "fc_pattn_rows");
+    if (a.queue) hipLaunchKernelGGL((k_pattn_rows<HD, 4, true>), dim3((unsigned)once), dim3(256), 0, st, a);
+    else if (NW == 4) hipLaunchKernelGGL((k_pattn_rows<HD, 4, false>), dim3((unsigned)a.pieces), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_pattn_rows<HD, 2, false>), dim3((unsigned)a.pieces), dim3(128), 0, st, a);
+    FC_LAUNCH_OK(st, "k_pattn_rows");
+  } else {
+    const dim3 grid((unsigned)a.slots, (unsigned)a.KV);
+    ProfScope ps(ctx, st, "fc_pattn");
+    const bool big = std::min(pairs * a.cap, ((long)a.t.pages * a.KV) << a.t.shift) * HD * 4 > (384L << 20);
+    if (MT == 1 && big) hipLaunchKernelGGL((k_pattn<HD, 1, true>), grid, dim3(256), 0, st, a);
+    else if (MT == 1) hipLaunchKernelGGL((k_pattn<HD, 1, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_pattn<HD, 2, false>), grid, dim3(256), 0, st, a);
+    FC_LAUNCH_OK(st, "k_pattn");
+  }
+  if (parts) {
+    ProfScope ps(ctx, st, "fc_pattn_join");
+    if (many)
+      hipLaunchKernelGGL(k_pattn_join_rows<HD>, dim3((unsigned)((R + 31) / 32 * (HD / 32)), (unsigned)pairs), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_pattn_join<HD>, dim3((unsigned)R, (unsigned)pairs), dim3(256), 0, st, a);
+    FC_LAUNCH_OK(st, "k_pattn_join");
+  }
+  return FC_OK;
+}
+
+}  // namespace
+
+fc_status launch_pcache_attention(fc_ctx *ctx, const fc_pcache &c, const uint16_t *q, const int32_t *len,
+                                  const int32_t *n_new, const uint8_t *key_mask, uint16_t *out, int n_heads,
+                                  float scale, int B, int n, hipStream_t st) {
+  PAttnArgs a{};
+  a.k = c.k, a.v = c.v, a.t = page_table(c);
+  a.q = q, a.out = out, a.len = len, a.n_new = n_new, a.mask = key_mask;
+  // as in launch_qcache_attention
+  a.c = std::min(std::max(std::fabs(scale) * kLog2e, 1.2e-38f), 3.4e38f);
+  a.flip = scale < 0.f ? 0x80008000u : 0u;
+  a.B = B, a.n = n, a.H = n_heads, a.KV = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.cap = c.max_pages * c.page_rows;
+  a.by_g = quot_by(a.G);
+  return c.head_dim == 128 ? run_pattn<128>(ctx, a, st) : run_pattn<64>(ctx, a, st);
+}
+
+}  // namespace fc

@@ -37,7 +37,8 @@ EXPORTS = ("fc_version", "fc_last_error", "fc_create", "fc_destroy", "fc_select"
            "fc_phase_correlate", "fc_phase_correlate_rotation", "fc_vit_block_forward",
            "fc_vit_cache_update", "fc_vit_merger_forward", "fc_slot_state_bytes",
            "fc_slot_map_init", "fc_qcache_append", "fc_qcache_attention", "fc_qcache_evict",
-           "fc_profile_enable", "fc_profile_only", "fc_profile_read")
+           "fc_pcache_state_bytes", "fc_pcache_init", "fc_pcache_append", "fc_pcache_attention",
+           "fc_pcache_step", "fc_pcache_compact", "fc_profile_enable", "fc_profile_only", "fc_profile_read")
 
 
 class FcError(RuntimeError):
@@ -104,6 +105,11 @@ class fc_vit_cache(ctypes.Structure):
 class fc_qcache(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale", "weight")] + \
         [("n_kv_heads", c_int32), ("head_dim", c_int32), ("capacity", c_int32)]
+
+
+class fc_pcache(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "state")] + \
+        [(n, c_int32) for n in ("n_kv_heads", "head_dim", "page_rows", "n_pages", "max_pages")]
 
 
 class fc_rope_axes(ctypes.Structure):
@@ -182,6 +188,18 @@ def lib() -> ctypes.CDLL:
         L.fc_qcache_evict.argtypes = [c_void_p, ctypes.POINTER(fc_qcache), ctypes.POINTER(fc_qcache),
                                       c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
                                       c_int32, c_void_p]
+        L.fc_pcache_state_bytes.argtypes = [c_int32, c_int32, c_int32]
+        L.fc_pcache_state_bytes.restype = ctypes.c_size_t
+        L.fc_pcache_init.argtypes = [c_void_p, ctypes.POINTER(fc_pcache), c_int32, c_void_p]
+        L.fc_pcache_append.argtypes = [c_void_p, ctypes.POINTER(fc_pcache), ctypes.POINTER(fc_rope_axes),
+                                       ctypes.POINTER(fc_qkv_rows), c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_int32, c_int32, c_void_p]
+        L.fc_pcache_attention.argtypes = [c_void_p, ctypes.POINTER(fc_pcache), c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_void_p, c_int32, c_float, c_int32,
+                                          c_int32, c_void_p]
+        L.fc_pcache_step.argtypes = [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
+                                     c_void_p, c_int32, c_void_p]
+        L.fc_pcache_compact.argtypes = [c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_void_p]
         L.fc_debug.argtypes = [c_int32]
         L.fc_debug.restype = c_int32
         L.fc_profile_enable.argtypes = [c_void_p, c_int32]
@@ -193,7 +211,8 @@ def lib() -> ctypes.CDLL:
                   "fc_layer_forward_trail", "fc_phase_correlate", "fc_phase_correlate_rotation",
                   "fc_vit_block_forward", "fc_vit_cache_update",
                   "fc_slot_map_init", "fc_qcache_append", "fc_qcache_attention",
-                  "fc_qcache_evict", "fc_profile_enable",
+                  "fc_qcache_evict", "fc_pcache_init", "fc_pcache_append", "fc_pcache_attention",
+                  "fc_pcache_step", "fc_pcache_compact", "fc_profile_enable",
                   "fc_profile_only", "fc_profile_read"):
             getattr(L, n).restype = c_int32
         _lib = L
@@ -958,6 +977,26 @@ def _qrows(dev: int, t: torch.Tensor, B: int, n: int, heads: int, hd: int, name:
     return t.data_ptr(), (row if n > 1 else 0), (item if B > 1 else 0)
 
 
+def _append_args(dev: int, rope: RopeAxes, q, k, v, pos, lens, n_new, q_out, kv: int, hd: int):
+    """What the appends' C calls take between the cache and the stream."""
+    if (q is None) != (q_out is None):
+        raise ValueError("give both q and q_out or neither")
+    B, n = k.shape[:2]
+    heads = kv if q is None else q.shape[2]
+    pk, k_row, k_item = _qrows(dev, k, B, n, kv, hd, "k")
+    pv, v_row, v_item = _qrows(dev, v, B, n, kv, hd, "v")
+    if q is None:
+        pq, q_row, q_item, po = None, 0, 0, None
+    else:
+        pq, q_row, q_item = _qrows(dev, q, B, n, heads, hd, "q")
+        po = _arg(dev, q_out, torch.bfloat16, B * n * heads * hd, "q_out")
+    if pos.numel() != rope.axes * B * n:
+        raise ValueError(f"pos has {pos.numel()} positions, {rope.axes} axes of {B} x {n} tokens need {rope.axes * B * n}")
+    return (ctypes.byref(rope._c),
+            ctypes.byref(fc_qkv_rows(pq, pk, pv, q_row, k_row, v_row, q_item, k_item, v_item, heads)),
+            _ints(dev, pos, 1, "pos"), _ints(dev, lens, B, "lens"), _ints(dev, n_new, B, "n_new"), po, B, n)
+
+
 def fc_qcache_append(ctx: Context, cache: QCache, rope: RopeAxes, q: torch.Tensor | None,
                      k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, lens: torch.Tensor,
                      n_new: torch.Tensor | None, q_out: torch.Tensor | None, stream=None):
@@ -971,23 +1010,8 @@ def fc_qcache_append(ctx: Context, cache: QCache, rope: RopeAxes, q: torch.Tenso
     Bc, kv, _, hd = cache.k.shape
     if B != Bc or cache.k.get_device() != dev:
         raise ValueError(f"k has {B} items, the cache {Bc} on {cache.k.device}, the context is on GPU {dev}")
-    if (q is None) != (q_out is None):
-        raise ValueError("give both q and q_out or neither")
-    heads = kv if q is None else q.shape[2]
-    pk, k_row, k_item = _qrows(dev, k, B, n, kv, hd, "k")
-    pv, v_row, v_item = _qrows(dev, v, B, n, kv, hd, "v")
-    if q is None:
-        pq, q_row, q_item, po = None, 0, 0, None
-    else:
-        pq, q_row, q_item = _qrows(dev, q, B, n, heads, hd, "q")
-        po = _arg(dev, q_out, torch.bfloat16, B * n * heads * hd, "q_out")
-    if pos.numel() != rope.axes * B * n:
-        raise ValueError(f"pos has {pos.numel()} positions, {rope.axes} axes of {B} x {n} tokens need {rope.axes * B * n}")
-    _check(lib().fc_qcache_append(
-        ctx.handle, ctypes.byref(cache.c()), ctypes.byref(rope._c),
-        ctypes.byref(fc_qkv_rows(pq, pk, pv, q_row, k_row, v_row, q_item, k_item, v_item, heads)),
-        _ints(dev, pos, 1, "pos"), _ints(dev, lens, B, "lens"), _ints(dev, n_new, B, "n_new"), po, B, n,
-        _dev_stream(dev, stream)))
+    args = _append_args(dev, rope, q, k, v, pos, lens, n_new, q_out, kv, hd)
+    _check(lib().fc_qcache_append(ctx.handle, ctypes.byref(cache.c()), *args, _dev_stream(dev, stream)))
 
 
 def fc_qcache_attention(ctx: Context, cache: QCache, q: torch.Tensor, lens: torch.Tensor,
@@ -1034,6 +1058,188 @@ def fc_qcache_evict(ctx: Context, src: QCache, dst: QCache, lens: torch.Tensor, 
         ctx.handle, ctypes.byref(src.c()), ctypes.byref(dst.c()), _ints(dev, lens, B, "lens"), keep, sink,
         recent, _ints(dev, kept, B * kv * max(keep, 0), "kept"), _ints(dev, lens_out, B, "lens_out"), B,
         _dev_stream(dev, stream)))
+
+
+# ------------------------------------------------------------------------------ paged token cache
+PCACHE_TILE = 8   # rows of a page whose values lie together, by columns
+
+
+def pcache_state_bytes(B: int, max_pages: int, n_pages: int) -> int:
+    return lib().fc_pcache_state_bytes(B, max_pages, n_pages)
+
+
+@dataclass(frozen=True)
+class PageState:
+    """Which pages hold the rows of B items, for the caches of all layers: `state` int32, the table
+    [B, max_pages] (page or -1), zeros up to a multiple of four numbers, and the holders [n_pages]
+    of each page."""
+    state: torch.Tensor
+    B: int
+    max_pages: int
+    n_pages: int
+
+    def __post_init__(self):
+        if self.B < 1 or self.max_pages < 1 or self.n_pages < 1:
+            raise ValueError(f"PageState: {self.B} items of up to {self.max_pages} of {self.n_pages} pages")
+        need = pcache_state_bytes(self.B, self.max_pages, self.n_pages) // 4
+        if need == 0:
+            raise ValueError(f"PageState: a table of {self.B} x {self.max_pages} pages")
+        _ptr(self.state, _INT32, need, "state")
+
+    @staticmethod
+    def alloc(B: int, max_pages: int, n_pages: int, device="cuda") -> "PageState":
+        """An empty state: no item holds a page."""
+        state = torch.zeros(pcache_state_bytes(B, max_pages, n_pages) // 4, dtype=_INT32, device=device)
+        state[:B * max_pages] = -1
+        return PageState(state, B, max_pages, n_pages)
+
+    @property
+    def table(self) -> torch.Tensor:
+        return self.state[:self.B * self.max_pages].view(self.B, self.max_pages)
+
+    @property
+    def holders(self) -> torch.Tensor:
+        at = (self.B * self.max_pages + 3) // 4 * 4
+        return self.state[at:at + self.n_pages]
+
+
+@dataclass(frozen=True)
+class PCache:
+    """One layer's pool of pages of bfloat16 rows: k [n_pages, n_kv, page_rows, head_dim] (rotated),
+    v [n_pages, n_kv, page_rows / 8, head_dim, 8], each eight rows by columns.  `pages` says whose
+    rows they hold; it serves every layer."""
+    k: torch.Tensor
+    v: torch.Tensor
+    pages: PageState
+
+    def __post_init__(self):
+        if self.k.dim() != 4:
+            raise ValueError("PCache: k must be [n_pages, n_kv, page_rows, head_dim]")
+        P, kv, rows, hd = self.k.shape
+        if P != self.pages.n_pages:
+            raise ValueError(f"PCache: {P} pages, the state has {self.pages.n_pages}")
+        if rows % PCACHE_TILE:
+            raise ValueError(f"PCache: pages of {rows} rows (a power of two from 16 to 1024)")
+        if tuple(self.v.shape) != (P, kv, rows // PCACHE_TILE, hd, PCACHE_TILE):
+            raise ValueError(f"PCache: v is {tuple(self.v.shape)}, not {(P, kv, rows // PCACHE_TILE, hd, PCACHE_TILE)}")
+        for name, t in (("v", self.v), ("the state", self.pages.state)):
+            if t.device != self.k.device:
+                raise ValueError(f"PCache: {name} is on {t.device}, k on {self.k.device}")
+        object.__setattr__(self, "_c", None)
+        self.c()
+
+    @staticmethod
+    def alloc(pages: PageState, n_kv_heads: int, head_dim: int, page_rows: int = 64) -> "PCache":
+        """A layer's pool for `pages`."""
+        shape, kw = (pages.n_pages, n_kv_heads), dict(dtype=_BF16, device=pages.state.device)
+        return PCache(torch.zeros(*shape, page_rows, head_dim, **kw),
+                      torch.zeros(*shape, page_rows // PCACHE_TILE, head_dim, PCACHE_TILE, **kw), pages)
+
+    @property
+    def capacity(self) -> int:
+        """Rows that an item can hold."""
+        return self.pages.max_pages * self.k.shape[2]
+
+    def c(self) -> fc_pcache:
+        """The C descriptor, made once and again if a tensor has got other memory."""
+        p = (self.k.data_ptr(), self.v.data_ptr(), self.pages.state.data_ptr())
+        if self._c is None or self._c[0] != p:
+            P, kv, rows, hd = self.k.shape
+            for t, name in ((self.k, "k"), (self.v, "v")):
+                _ptr(t, _BF16, P * kv * rows * hd, name)
+            _ptr(self.pages.state, _INT32, pcache_state_bytes(self.pages.B, self.pages.max_pages, P) // 4, "state")
+            c = fc_pcache(*p, kv, hd, rows, P, self.pages.max_pages)
+            object.__setattr__(self, "_c", (p, c, bytes(c)))
+        return self._c[1]
+
+    def rows(self, item: int, values: bool = False) -> torch.Tensor:
+        """The keys (or values) of an item's table entries, in order: [n_kv, capacity, head_dim], 0
+        where there is no page."""
+        t = self.pages.table[item]
+        x = (self.v.transpose(-1, -2).reshape(self.k.shape) if values else self.k)[t.clamp(min=0).long()]
+        return torch.where((t >= 0)[:, None, None, None], x, 0).transpose(0, 1).flatten(1, 2)
+
+
+def _page_args(dev: int, cache: PCache, x: torch.Tensor, name: str):
+    """Checks that rows x [B, n, heads, hd] and the context go with the cache."""
+    if x.dim() != 4 or x.shape[0] != cache.pages.B or x.shape[3] != cache.k.shape[3]:
+        raise ValueError(f"{name} is {tuple(x.shape)}, the cache has {cache.pages.B} items of head_dim {cache.k.shape[3]}")
+    if cache.k.get_device() != dev:
+        raise ValueError(f"the cache is on {cache.k.device}, the context on GPU {dev}")
+
+
+def fc_pcache_init(ctx: Context, cache: PCache, stream=None):
+    """No item holds a page any more."""
+    if cache.k.get_device() != ctx.device:
+        raise ValueError(f"the cache is on {cache.k.device}, the context on GPU {ctx.device}")
+    _check(lib().fc_pcache_init(ctx.handle, ctypes.byref(cache.c()), cache.pages.B, _dev_stream(ctx.device, stream)))
+
+
+def fc_pcache_append(ctx: Context, cache: PCache, rope: RopeAxes, q: torch.Tensor | None,
+                     k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, lens: torch.Tensor,
+                     n_new: torch.Tensor | None, q_out: torch.Tensor | None, stream=None):
+    """New rows into the pages behind the lens[b] rows held, as fc_qcache_append; fc_pcache_step has
+    given the items the pages before."""
+    dev = ctx.device
+    _page_args(dev, cache, k, "k")
+    args = _append_args(dev, rope, q, k, v, pos, lens, n_new, q_out, cache.k.shape[1], cache.k.shape[3])
+    _check(lib().fc_pcache_append(ctx.handle, ctypes.byref(cache.c()), *args, _dev_stream(dev, stream)))
+
+
+def fc_pcache_attention(ctx: Context, cache: PCache, q: torch.Tensor, lens: torch.Tensor,
+                        n_new: torch.Tensor | None, out: torch.Tensor,
+                        key_mask: torch.Tensor | None = None, scale: float | None = None, stream=None):
+    """Causal attention of the tokens just appended (q, out [B, n, n_heads, hd] bfloat16; lens and
+    n_new as given to fc_pcache_append) over the paged cache.  key_mask [B, capacity] uint8 or bool:
+    0 hides a row.  scale: 1 / sqrt(hd) by default."""
+    dev = ctx.device
+    _page_args(dev, cache, q, "q")
+    B, n, heads, hd = q.shape
+    size = B * n * heads * hd
+    if key_mask is not None:
+        if key_mask.dtype is torch.bool:
+            key_mask = key_mask.view(torch.uint8)
+        key_mask = _arg(dev, key_mask, torch.uint8, B * cache.capacity, "key_mask")
+    _check(lib().fc_pcache_attention(
+        ctx.handle, ctypes.byref(cache.c()), _arg(dev, q, _BF16, size, "q"), _ints(dev, lens, B, "lens"),
+        _ints(dev, n_new, B, "n_new"), key_mask, _arg(dev, out, _BF16, size, "out"), heads,
+        hd ** -0.5 if scale is None else scale, B, n, _dev_stream(dev, stream)))
+
+
+def _pcaches(dev: int, caches):
+    """fc_pcache[len(caches)] of the layers of a model, and the state they share."""
+    caches = list(caches)
+    if not caches:
+        raise ValueError("no caches")
+    pages = caches[0].pages
+    for c in caches:
+        if c.pages.state is not pages.state or c.pages.B != pages.B or c.k.get_device() != dev:
+            raise ValueError(f"the caches must share one PageState, on GPU {dev}")
+        c.c()
+    return b"".join([c._c[2] for c in caches]), len(caches), pages
+
+
+def fc_pcache_step(ctx: Context, caches, lens: torch.Tensor, n_new: torch.Tensor | None, n: int,
+                   granted: torch.Tensor, src: torch.Tensor | None = None, stream=None):
+    """Pages for a step, in all layers' caches at once: item b goes on from the first lens[b] rows of
+    item src[b] (None: its own; several may go on from one) and gets pages for n_new[b] (None: n)
+    more, as far as there are any; granted[b] says for how many.  lens[b] = 0 ends an item.  A partly
+    filled page that several hold is copied for those about to write it."""
+    dev = ctx.device
+    raw, layers, pages = _pcaches(dev, caches)
+    B = pages.B
+    _check(lib().fc_pcache_step(
+        ctx.handle, raw, layers, _ints(dev, src, B, "src"), _ints(dev, lens, B, "lens"),
+        _ints(dev, n_new, B, "n_new"), n, _ints(dev, granted, B, "granted"), B, _dev_stream(dev, stream)))
+
+
+def fc_pcache_compact(ctx: Context, caches, live: torch.Tensor | None = None, stream=None):
+    """The pages that items hold, moved to the lowest numbers in all layers' caches; live [1] int32
+    receives how many there are."""
+    dev = ctx.device
+    raw, layers, pages = _pcaches(dev, caches)
+    _check(lib().fc_pcache_compact(ctx.handle, raw, layers, _ints(dev, live, 1, "live"), pages.B,
+                                   _dev_stream(dev, stream)))
 
 
 # ------------------------------------------------------------------------------ timing
