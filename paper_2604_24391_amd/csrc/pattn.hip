@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attn_dev.h"
 #include "fc_internal.h"
@@ -44,6 +45,8 @@ struct PAttnArgs {
 };
 
 constexpr float kProbDown = 17.f;    // log2
+
+constexpr float kProbMost = 0x1p-8f; // 2^9 of what is held 2^-17 smaller
 
 __device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
@@ -351,9 +354,18 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 }
 
 // More than 32 rows: 4 waves of 32 each (2 up to 64 rows) share the key blocks, which the DMA brings into
-// LDS a block ahead (32 KB at hd 128).  32 x 32 matrix instructions; a lane holds one row and, of a
-// block's keys, the 32 of its half wave.  Pieces of work go round the XCDs and, in ragged batches of
+// LDS a block ahead (32 KB at hd 128).  32 x 32 matrix instructions; a lane holds one row and, of half a
+// block's keys, the 16 of its half wave.  Pieces of work go round the XCDs and, in ragged batches of
 // many rounds, into queues, as in k_qattn_rows.
+//
+// A wave goes half a block (32 keys) at a time: the scores of the next half are computed beside the
+// exponentials of this one, so that matrix and vector instructions alternate within the wave (with each
+// kind in a run of its own, two waves on a SIMD took the sum of both: 544 us for a prompt of 8192 rows
+// of 28 heads).  Keys are therefore brought half a block ahead of values, and every operand is read from
+// LDS a step before its use.  No maximum is looked for (see `step`): a third fewer vector instructions.
+// That prompt (0.48 TFLOP) takes 478 to 498 us, 0.97 to 1.01 PFLOP/s, the matrix unit busy for 49 % of its
+// cycles, at a clock of 1.9 to 2.0 GHz of 2.4: power holds it there, and cycles saved since came back as a
+// lower clock.
 //
 // A row of keys is 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks; columns of
@@ -363,18 +375,25 @@ __device__ __forceinline__ int pkey_swz(int row) {
   return HD == 128 ? row & 15 : (row >> 1) & 7;
 }
 
+// Both numbers of a pair of bfloat16 and c added up.
+__device__ __forceinline__ float pair_sum(uint32_t pair, float c) {
+  const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, c, false);
+}
+
 template <int HD, int NW, bool QUEUE>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnArgs args) {
   constexpr int PC = HD / 8;                    // 16-byte pieces of a key row
   constexpr int DT = HD / 32;                   // output tiles of 32 dims
+  constexpr int KS = HD / 16;                   // products of a tile of scores
   constexpr int TILE = kKeyBlock * HD * 2;      // bytes of a block's keys, and of its values
   constexpr int DMAS = TILE / 1024 / NW;        // DMA instructions of a wave for either
   constexpr int SUBS = 4 / NW;                  // runs of 16 rows that a wave brings, DMAS / SUBS instructions each
   constexpr int ROWS = 32 * NW;
-  constexpr int STAGES = 2;
-  __shared__ __align__(1024) uint8_t sm[STAGES][2][TILE];
-  __shared__ OddKeys sm_odd[NW][HD];
-  __shared__ __align__(16) uint8_t sm_mask[STAGES][NW][256];
+  __shared__ __align__(1024) uint8_t sm_k[2][TILE], sm_v[2][TILE];
+  __shared__ OddKeys sm_odd[2][HD];
+  __shared__ int sm_flag[2][NW];
+  __shared__ __align__(16) uint8_t sm_mask[2][NW][256];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   auto work = [&](const PAttnArgs &a, int id) {
     const int P = a.B * a.KV, R = a.n * a.G;
@@ -389,175 +408,266 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     if (split >= used) return;
     const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
-    // pages of a block's four runs of 16 rows: those that this wave brings, and the keys that have one
+    // pages of a block's four runs of 16 rows (blocks behind the last one are read as it)
     typedef const __attribute__((address_space(4))) int32_t *uniform_ints;
     const uniform_ints table = (uniform_ints)(uintptr_t)(a.t.table + (long)b * a.t.width);
+    // (neither an array nor a choice between members: the compiler would put them into memory for a wave's
+    // number to index)
     struct Pages {
-      int mine[SUBS];
-      uint64_t there;
+      uint64_t ab, cd;
+      __device__ int of(int run) const {
+        const uint64_t m = 0 - (uint64_t)(run >> 1 & 1);
+        return (int)(((ab & ~m) | (cd & m)) >> (32 * (run & 1)));
+      }
     };
     auto pages_of = [&](int blk) {
-      Pages p;
-      p.there = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int e = table[min((blk * kKeyBlock + 16 * x) >> a.t.shift, a.t.width - 1)];
-        if (a.t.there(e)) p.there |= 0xFFFFull << (16 * x);
-#pragma unroll
-        for (int i = 0; i < SUBS; ++i)
-          if (x == wave * SUBS + i) p.mine[i] = a.t.safe(e);
+      const int at = min(blk, bhi - 1);
+      if (a.t.shift >= 6) {
+        const uint64_t e = (uint64_t)(uint32_t)table[at >> (a.t.shift - 6)];
+        return Pages{e | e << 32, e | e << 32};
       }
-      return p;
+      auto entry = [&](int run) { return (uint64_t)(uint32_t)table[min((4 * at + run) >> (a.t.shift - 4), a.t.width - 1)]; };
+      return Pages{entry(0) | entry(1) << 32, entry(2) | entry(3) << 32};
+    };
+    auto there = [&](const Pages &p) -> uint64_t {   // keys that have one
+      if (a.t.shift >= 6) return a.t.there(p.of(0)) ? ~0ull : 0ull;
+      uint64_t m = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (a.t.there(p.of(x))) m |= 0xFFFFull << (16 * x);
+      return m;
     };
     const int in_page = (1 << a.t.shift) - 1;
-    int ksrc[DMAS];
+    // element of a pool where run u of block blk begins, in the page of p's run x
+    auto run_at = [&](int blk, const Pages &p, int x, int u) {
+      const int e = p.of(x);
+      return ((((long)a.t.safe(e) * a.KV + kv) << a.t.shift) + ((min(blk, bhi - 1) * kKeyBlock + 16 * u) & in_page)) * HD;
+    };
+    constexpr int PER = DMAS / SUBS;
+    // a lane's bytes of a run's first KB of keys (piece ^ f(row)): those of the i-th KB are 64 i away in an exclusive or
+    const int ksrc = lane / PC * (HD * 2) + ((lane % PC) ^ pkey_swz<HD>(lane / PC)) * 16;
+    // keys of the second half of block blk and of the first half of the next one
+    auto fetch_k = [&](int blk, int stage, const Pages &p, const Pages &p_next) {
 #pragma unroll
-    for (int i = 0; i < DMAS; ++i) {
-      const int p = (wave * DMAS + i) * 64 + lane, kr = p / PC;
-      ksrc[i] = (kr & 15) * HD + ((p % PC) ^ pkey_swz<HD>(kr)) * 8;
-    }
-    auto fetch = [&](int blk, int stage, const Pages &pg) {
-#pragma unroll
-      for (int i = 0; i < DMAS; ++i) {
-        constexpr int per = DMAS / SUBS;
-        const int u = wave * SUBS + i / per;
-        const long at = ((((long)pg.mine[i / per] * a.KV + kv) << a.t.shift) + ((blk * kKeyBlock + 16 * u) & in_page)) * HD;
-        dma16(a.k + at + ksrc[i], lds_addr(&sm[stage][0][(wave * DMAS + i) * 1024]));
-        dma16(a.v + at + (i % per * 64 + lane) * 8, lds_addr(&sm[stage][1][(wave * DMAS + i) * 1024]));
+      for (int u = 0; u < SUBS; ++u) {
+        const int run = wave * SUBS + u;
+        const bool behind = run > 1;
+        const uint64_t m = 0 - (uint64_t)behind;
+        const uint16_t *src = a.k + run_at(blk + behind, Pages{(p.cd & ~m) | (p_next.ab & m), 0}, run & 1, (run + 2) & 3);
+        dma_run<PER, 64>(src, ksrc, lds_addr(&sm_k[stage][(wave * DMAS + u * PER) * 1024]));
       }
-      // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
-      if (a.mask) dma4(a.mask + (long)b * a.cap + min(blk * kKeyBlock + (lane & 15) * 4, a.cap - 4), lds_addr(&sm_mask[stage][wave][0]));
+      // their 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
+      if (a.mask) dma4(a.mask + (long)b * a.cap + min(blk * kKeyBlock + 32 + (lane & 15) * 4, a.cap - 4), lds_addr(&sm_mask[stage][wave][0]));
+    };
+    auto fetch_v = [&](int blk, int stage, const Pages &p) {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+        dma_run<PER, 0>(a.v + run_at(blk, p, wave * SUBS + u, wave * SUBS + u), lane * 16, lds_addr(&sm_v[stage][(wave * DMAS + u * PER) * 1024]));
     };
 
     const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
     const int seen = r < rows ? held + tok + 1 : 0;                              // keys that the lane's row sees
-    const int wmax = w0 < rows ? held + a.by_g(min(w0 + 32, rows) - 1) + 1 : 0;  // that any row of the wave sees
-    const int wall = held + a.by_g(w0) + 1;                                      // that every one does
+    const int wall = held + a.by_g(w0) + 1;                                      // that every row of the wave sees
+    const int gall = held + a.by_g(r0) + 1;                                      // that every row of the workgroup does
     const long at_q = (((long)b * a.n + tok) * a.H + head) * HD;
-    bf16x8 q[HD / 16];
+    bf16x8 q[KS];
 #pragma unroll
-    for (int i = 0; i < HD / 16; ++i) q[i] = load_q(a.q + at_q + 16 * i + 8 * h, a.flip);
-    Pages pg = pages_of(blo), pg_next = pages_of(min(blo + 1, bhi - 1));
+    for (int i = 0; i < KS; ++i) q[i] = load_q(a.q + at_q + 16 * i + 8 * h, a.flip);
+    Pages pg = pages_of(blo), pg1 = pages_of(blo + 1), pg2 = pages_of(blo + 2);   // of the blocks blk, blk + 1, blk + 2
     loads_done();
-    fetch(blo, 0, pg);
+    // (of the block before the first one the second half is nobody's: the first block's again)
+    fetch_k(blo - 1, 1, pg, pg);
+    fetch_v(blo, 0, pg);
 
-    // S^T row x of tile t is key 32 t + x with bits 2 and 3 of x exchanged
+    // S^T row x of a half block is key x with bits 2 and 3 of x exchanged
     const int kr = (l32 & 19) | ((l32 >> 2) & 1) << 3 | ((l32 >> 3) & 1) << 2;
-    const int koff = kr * HD * 2, kx = pkey_swz<HD>(kr);
+    const int koff = kr * HD * 2 + (h ^ pkey_swz<HD>(kr)) * 16;   // piece h; piece 2 i + h is 32 i away in an exclusive or
+    const int voff = (h * HD + l32) * 16;
+    auto key_frag = [&](int stage, int half, int at, int i) {
+      return *reinterpret_cast<const bf16x8 *>(&sm_k[stage][(at ^ (32 * i)) + half * 64 * HD]);
+    };
+    auto value_frag = [&](int stage, int half, int t, int d) {
+      return *reinterpret_cast<const bf16x8 *>(&sm_v[stage][voff + ((4 * half + 2 * t) * HD + 32 * d) * 16]);
+    };
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-    float ref = kNegInf, sum = 0.f;   // exponents are taken relative to ref
+    float ref = kNegInf, sum = 0.f, sub = kProbDown;   // exponents are taken relative to ref, ref + kProbDown
+    // a lane's sum of probabilities of 16 keys beyond which ref is looked at (any, as long as its row has seen no key)
+    float limit = r < rows ? -1.f : __builtin_inff();
+    f32x16 sa, sb;                    // scores of a block's halves
 
-    int stage = 0;
-    for (int blk = blo; blk < bhi; ++blk, stage ^= 1) {
-      wait_vm<0>();                    // this wave's part of the block; the barrier adds the others', and
-      lds_barrier();                   // every wave has left the other stage
-      const uint64_t there = pg.there;
-      if (blk + 1 < bhi) fetch(blk + 1, stage ^ 1, pg_next);
-      pg = pg_next;
-      pg_next = pages_of(min(blk + 2, bhi - 1));
-      if (w0 >= rows) continue;        // it only brings its part of the blocks
-      const int j0 = blk * kKeyBlock;
-      f32x16 s[2];
+    // What a row does not see of a half block, given its scores and the keys shown.
+    auto hide = [&](f32x16 &s, int j0, uint32_t shown) {
+      if (j0 + 32 <= wall && shown == ~0u) return;
+      // the lane's 16 keys: 16 i + 8 h + e
+      const uint32_t sees = (shown & (uint32_t)seen_bits(seen - j0)) >> (8 * h);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int e = 0; e < 16; ++e)
+        if (!(sees >> (16 * (e / 8) + e % 8) & 1u)) s[e] = kNegInf;
+    };
+    // Values that are not finite, of the runs that this wave has brought, where not every row may see them:
+    // they become 0, and their places are listed.
+    auto clean = [&](int stage) {
+      uint32_t any = 0;
+      u32x4 *at = reinterpret_cast<u32x4 *>(&sm_v[stage][wave * DMAS * 1024]) + lane;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+      for (int i = 0; i < DMAS; ++i) {
+        const u32x4 w = at[64 * i];
 #pragma unroll
-      for (int i = 0; i < HD / 16; ++i)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const bf16x8 w = *reinterpret_cast<const bf16x8 *>(&sm[stage][0][koff + t * 64 * HD + (((2 * i + h) ^ kx) * 16)]);
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i], s[t], 0, 0, 0);
-        }
-      // the keys that have a page and that the mask shows, and whether some row of the wave may not see
-      // the block whole
-      uint64_t shown = there;
-      if (a.mask) shown &= __ballot(sm_mask[stage][wave][lane] != 0);
-      const bool later = j0 + kKeyBlock > wall, part = later || shown != ~0ull;
-      uint64_t some = ~0ull;           // keys that some row may see
-      bool odd = false;
-      if (part) {
-        some = shown & seen_bits(wmax - j0);
-        // the lane's 32 keys: 16 i + 8 h + e
-        const uint64_t sees64 = (some & seen_bits(seen - j0)) >> (8 * h);
-        const uint32_t sees = __builtin_amdgcn_perm((uint32_t)(sees64 >> 32), (uint32_t)sees64, 0x06040200u);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!(sees >> (16 * t + e) & 1u)) s[t][e] = kNegInf;
+        for (int x = 0; x < 4; ++x) any |= odd_halves(w[x]);
       }
-      float top = kNegInf;
+      const bool odd = __any(any != 0);
+      if (odd)
+#pragma unroll 1
+        for (int i = 0; i < DMAS; ++i) {
+          u32x4 w = at[64 * i];
+          uint32_t bits[3];
+          take_odd(w, bits);
+          at[64 * i] = w;
+          const int p = (wave * DMAS + i) * 64 + lane;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+          for (int x = 0; x < 3; ++x) reinterpret_cast<part8 *>(&sm_odd[stage][p % HD].kind[x])[p / HD] = (uint8_t)bits[x];
+        }
+      if (lane == 0) sm_flag[stage][wave] = odd;
+    };
+    // and what the rows that see them get for them
+    auto add_odd = [&](int blk, int stage, uint64_t shown) {
+      uint64_t listed = 0;
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[t][e]), s[t][e + 1]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
-      // the reference follows the maximum only where it is 2^8 behind: most blocks need not touch O
-      // (each row's by its own scores alone: another row's may come from keys that are hidden from it)
-      if (__any(top > ref + 8.f)) {
-        const bool up = top > ref + 8.f;
+      for (int w = 0; w < NW; ++w)
+        if (sm_flag[stage][w]) listed |= (NW == 4 ? 0xFFFFull : 0xFFFFFFFFull) << (64 / NW * w);
+      if (__builtin_amdgcn_readfirstlane((int)(listed != 0)) == 0) return;
+      const uint64_t keys = listed & shown & seen_bits(seen - blk * kKeyBlock);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] += odd_sum(sm_odd[stage][32 * d + 8 * (e / 4) + 4 * h + e % 4], keys);
+    };
+    auto both_halves = [&](float x) {
+      const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    };
+
+    // Half a block of 32 keys, whose scores are in s: their exponentials beside the products of the next half's
+    // scores, then the products with their values.
+    //
+    // Exponents are taken relative to ref, which follows a row's largest score only where the sum of a lane's
+    // probabilities shows that it has been left far behind (or where the row has seen no key yet): most
+    // steps need not look for their maximum, nor touch O.  Each row's ref follows its own scores alone:
+    // another row's may come from keys that are hidden from it.
+    bf16x8 kf[KS], vf[2][DT];         // operands of the step's products, read ahead
+    auto step = [&](auto st, auto second, f32x16 &s, f32x16 &next, int j_next, uint32_t show_next) {
+      constexpr int stage = decltype(st)::value, half = decltype(second)::value;
+      u32x4 p[2];
+      float add = 0.f;
+      float y[16];
+      auto exps = [&](int from, int to) {
+#pragma unroll
+        for (int e = from; e < to; ++e) y[e] = exp2_fast(fmaf(s[e], a.c, -sub));
+      };
+      auto pack = [&](int from, int to) {
+#pragma unroll
+        for (int e = from; e < to; e += 2) {
+          const bf16x2 w = {(__bf16)y[e], (__bf16)y[e + 1]};
+          uint32_t u = __builtin_bit_cast(uint32_t, w);
+          asm volatile("" : "+v"(u));   // rounded here: the pairs' registers are needed
+          p[e / 8][e % 8 / 2] = u;
+          add = pair_sum(u, add);
+        }
+      };
+      constexpr int PM = 16 / KS;       // scores beside each product
+#pragma unroll
+      for (int e = 0; e < 16; ++e) next[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], q[i], next, 0, 0, 0);
+        if (half == 0) kf[i] = key_frag(stage, 1, koff, i);
+        if (half == 0 ? i == KS - 1 : i == 0)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) vf[1][d] = value_frag(stage, half, 1, d);
+        exps(PM * i, PM * (i + 1));
+        if (i > 0) pack(PM * (i - 1), PM * i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      pack(16 - PM, 16);
+      if (__any(add > limit)) {
+        float top = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[e]), s[e + 1]);
+        top = both_halves(top) * a.c;
+        const bool up = top > ref + 4.f;
         const float corr = up ? exp2_fast(ref - top) : 1.f;
         ref = up ? top : ref;
+        sub = (ref == kNegInf ? 0.f : ref) + kProbDown;
+        limit = ref == kNegInf ? limit : kProbMost;
         sum *= corr;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= corr;
+        add = 0.f;
+        exps(0, 16);
+        pack(0, 16);
       }
-      const float sub = (ref == kNegInf ? 0.f : ref) + kProbDown;
-      // 16 keys of the block at a time: their values, their exponentials, their products
+      sum += add;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        u32x4 vw[DT];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          vw[d] = *reinterpret_cast<const u32x4 *>(&sm[stage][1][((2 * t + h) * HD + 32 * d + l32) * 16]);
-        if (part) {                    // as in k_pattn
-          uint32_t any = 0;
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) any |= odd_halves(vw[d][x]);
-          if (__any(any != 0)) {
-            if (!odd) {
-#pragma unroll
-              for (int d = 0; d < DT; ++d) sm_odd[wave][32 * d + l32] = OddKeys{{0, 0, 0}};
-              wave_lds_order();
-            }
-            odd = true;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              uint32_t bits[3];
-              take_odd(vw[d], bits);
-#pragma unroll
-              for (int x = 0; x < 3; ++x)
-                reinterpret_cast<part8 *>(&sm_odd[wave][32 * d + l32].kind[x])[2 * t + h] = (uint8_t)bits[x];
-            }
-          }
+        for (int d = 0; d < DT; ++d) {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][d], __builtin_bit_cast(bf16x8, p[t]), o[d], 0, 0, 0);
+          if (half == 0 && t == 0) vf[0][d] = value_frag(stage, 1, 0, d);
         }
-        bf16x8 p;
+      hide(next, j_next, show_next);
+    };
+    // keys that a block's half steps look at ahead: its second half and the next one's first, by page and mask
+    auto shown_ahead = [&](int stage, const Pages &p, const Pages &p_next) {
+      uint64_t m = there(p) >> 32 | there(p_next) << 32;
+      if (a.mask) m &= __ballot(sm_mask[stage][wave][lane] != 0);
+      return m;
+    };
+
+    // the first half block's scores
+    wait_vm<0>();
+    lds_barrier();
+    uint32_t show = (uint32_t)(shown_ahead(1, pg, pg) >> 32);   // of the block's first half
+    if (w0 < rows) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float y = exp2_fast(fmaf(s[t / 2][8 * (t % 2) + e], a.c, -sub));
-          sum += y;
-          p[e] = (__bf16)y;
-        }
+      for (int e = 0; e < 16; ++e) sa[e] = 0.f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw[d]), p, o[d], 0, 0, 0);
+      for (int i = 0; i < KS; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag(1, 1, koff, i), q[i], sa, 0, 0, 0);
+      hide(sa, blo * kKeyBlock, show);
+    }
+    fetch_k(blo, 0, pg, pg1);
+    auto block = [&](auto st, int blk) {
+      constexpr int stage = decltype(st)::value;
+      const Pages pg3 = pages_of(blk + 3);
+      const bool partly = a.mask || blk * kKeyBlock + kKeyBlock > gall || there(pg) != ~0ull;
+      wait_vm<0>();                    // this wave's parts of the blocks; the barrier adds the others', and
+      if (partly) clean(stage);
+      lds_barrier();                   // every wave has left what the loads below write over
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kf[i] = key_frag(stage, 0, koff, i);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[0][d] = value_frag(stage, 0, 0, d);
+      __builtin_amdgcn_sched_barrier(0);
+      if (blk + 1 < bhi) {
+        fetch_k(blk + 1, stage ^ 1, pg1, pg2);
+        fetch_v(blk + 1, stage ^ 1, pg1);
       }
-      if (odd) {
-        const uint64_t keys = some & seen_bits(seen - j0);
-        wave_lds_order();
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] += odd_sum(sm_odd[wave][32 * d + 8 * (e / 4) + 4 * h + e % 4], keys);
-        wave_lds_order();
+      if (w0 < rows) {                 // (otherwise it only brings its part of the blocks)
+        const uint64_t ahead = shown_ahead(stage, pg, pg1);
+        const int j0 = blk * kKeyBlock;
+        step(st, std::integral_constant<int, 0>(), sa, sb, j0 + 32, (uint32_t)ahead);
+        step(st, std::integral_constant<int, 1>(), sb, sa, j0 + 64, (uint32_t)(ahead >> 32));
+        if (partly) add_odd(blk, stage, (uint64_t)(uint32_t)ahead << 32 | show);
+        show = (uint32_t)(ahead >> 32);
       }
+      pg = pg1, pg1 = pg2, pg2 = pg3;
+    };
+    for (int blk = blo; blk < bhi; blk += 2) {
+      block(std::integral_constant<int, 0>(), blk);
+      if (blk + 1 < bhi) block(std::integral_constant<int, 1>(), blk + 1);
     }
 
     sum += __shfl_xor(sum, 32);
