@@ -39,6 +39,7 @@ struct PAttnArgs {
   int2 *plan;                        // [B] k_pattn: an item's first slot and its slots
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, least, tile_rows, slots;
+  int row_tiles, stride;             // k_pattn_rows: of a pair; pairs whose pieces take turns
   int *queue, pieces;                // k_pattn_rows: 8 counts of pieces taken behind the first ones, or null
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
@@ -355,8 +356,16 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 
 // More than 32 rows: 4 waves of 32 each (2 up to 64 rows) share the key blocks, which the DMA brings into
 // LDS a block ahead (32 KB at hd 128).  32 x 32 matrix instructions; a lane holds one row and, of half a
-// block's keys, the 16 of its half wave.  Pieces of work go round the XCDs and, in ragged batches of
-// many rounds, into queues, as in k_qattn_rows.
+// block's keys, the 16 of its half wave.
+//
+// Pieces of work are numbered pair by pair (item and key-value head), eight pairs taking turns as
+// workgroups go round the 8 XCDs (fewer where their number is no multiple of eight), the last rows, which
+// see most keys, first: an XCD works on one or two pairs at a time, whose keys its L2 holds (sixteen frames
+// 634 us with all pairs at once, 597 so).  Items of one batch differ in length, so from two rounds of
+// workgroups on pieces come from queues: as many workgroups as run at once, each going on with the next
+// piece of its XCD's pairs, then with the others' (eight items of 10 to 4000 rows and 300 new ones
+// 165 us before and 114 now, of 1024 397 and 323, ragged 310 and 254; of equal length 312 without queues
+// and 319 with).
 //
 // A wave goes half a block (32 keys) at a time: the scores of the next half are computed beside the
 // exponentials of this one, so that matrix and vector instructions alternate within the wave (with each
@@ -396,9 +405,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
   __shared__ __align__(16) uint8_t sm_mask[2][NW][256];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   auto work = [&](const PAttnArgs &a, int id) {
-    const int P = a.B * a.KV, R = a.n * a.G;
-    const int rest = id / P, hb = QUEUE ? id % P : (id % P + rest) % P, split = rest % a.splits;
-    const int r0 = ((R + ROWS - 1) / ROWS - 1 - rest / a.splits) * ROWS;
+    const int P = a.B * a.KV, R = a.n * a.G;   // pairs of item and key-value head, rows of each
+    const int seq = id / a.stride, per = a.row_tiles * a.splits, rest = seq % per;
+    const int hb = id % a.stride + a.stride * (seq / per), split = rest % a.splits;
+    const int r0 = (a.row_tiles - 1 - rest / a.splits) * ROWS;
     const int b = hb / a.KV, kv = hb % a.KV;
     const int held = q_held(a.len, b, a.cap), m = q_new(a.n_new, b, a.n, held, a.cap);
     const int rows = m * a.G;
@@ -806,8 +816,10 @@ fc_status run_pattn(fc_ctx *ctx, PAttnArgs &a, hipStream_t st) {
     if (pairs * tiles * splits > (1L << 24) - 1)   // nothing has been launched yet
       return fail(FC_ERR_UNSUPPORTED, "fc_pcache_attention: %ld row tiles of %ld heads in one call", tiles, pairs);
     a.pieces = (int)(pairs * tiles * splits);
+    a.row_tiles = (int)tiles;
+    a.stride = pairs % 8 == 0 ? 8 : pairs % 4 == 0 ? 4 : pairs % 2 == 0 ? 2 : 1;
     const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;     // workgroups that run at once
-    if (NW == 4 && !parts && a.B > 1 && a.n_new && a.pieces >= 4 * once && 8 * kQueueStep <= ws) {
+    if (NW == 4 && !parts && a.B > 1 && a.pieces >= 2 * once && 8 * kQueueStep <= ws) {
       a.queue = reinterpret_cast<int *>(at);
       hipLaunchKernelGGL(k_pattn_queue, dim3(1), dim3(8), 0, st, a.queue);
       FC_LAUNCH_OK(st, "k_pattn_queue");
