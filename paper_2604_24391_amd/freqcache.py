@@ -1068,7 +1068,7 @@ def pcache_state_bytes(B: int, max_pages: int, n_pages: int) -> int:
     return lib().fc_pcache_state_bytes(B, max_pages, n_pages)
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class PageState:
     """Which pages hold the rows of B items, for the caches of all layers: `state` int32, the table
     [B, max_pages] (page or -1), zeros up to a multiple of four numbers, and the holders [n_pages]
@@ -1103,7 +1103,7 @@ class PageState:
         return self.state[at:at + self.n_pages]
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class PCache:
     """One layer's pool of pages of bfloat16 rows: k [n_pages, n_kv, page_rows, head_dim] (rotated),
     v [n_pages, n_kv, page_rows / 8, head_dim, 8], each eight rows by columns.  `pages` says whose
@@ -1149,7 +1149,8 @@ class PCache:
                 _ptr(t, _BF16, P * kv * rows * hd, name)
             _ptr(self.pages.state, _INT32, pcache_state_bytes(self.pages.B, self.pages.max_pages, P) // 4, "state")
             c = fc_pcache(*p, kv, hd, rows, P, self.pages.max_pages)
-            object.__setattr__(self, "_c", (p, c, bytes(c)))
+            for name, x in (("_c", (p, c)), ("_raw", bytes(c)), ("_kp", p[0]), ("_vp", p[1])):
+                object.__setattr__(self, name, x)
         return self._c[1]
 
     def rows(self, item: int, values: bool = False) -> torch.Tensor:
@@ -1206,17 +1207,26 @@ def fc_pcache_attention(ctx: Context, cache: PCache, q: torch.Tensor, lens: torc
         hd ** -0.5 if scale is None else scale, B, n, _dev_stream(dev, stream)))
 
 
+_data_ptr = torch.Tensor.data_ptr
+_pc_k, _pc_v, _pc_kp, _pc_vp, _pc_raw, _pc_pages = map(operator.attrgetter, ("k", "v", "_kp", "_vp", "_raw", "pages"))
+
+
 def _pcaches(dev: int, caches):
-    """fc_pcache[len(caches)] of the layers of a model, and the state they share."""
-    caches = list(caches)
+    """fc_pcache[len(caches)] of the layers of a model, and the state they share.  The checks go over the
+    whole list in C loops (28 layers one by one took longer than the call's kernels); a list that
+    fails one is looked at again cache by cache."""
     if not caches:
         raise ValueError("no caches")
-    pages = caches[0].pages
-    for c in caches:
-        if c.pages.state is not pages.state or c.pages.B != pages.B or c.k.get_device() != dev:
-            raise ValueError(f"the caches must share one PageState, on GPU {dev}")
-        c.c()
-    return b"".join([c._c[2] for c in caches]), len(caches), pages
+    n, pages = len(caches), caches[0].pages
+    if not (list(map(_data_ptr, map(_pc_k, caches))) == list(map(_pc_kp, caches))
+            and list(map(_data_ptr, map(_pc_v, caches))) == list(map(_pc_vp, caches))
+            and list(map(_pc_pages, caches)).count(pages) == n and caches[0]._c[0][2] == pages.state.data_ptr()
+            and pages.state.get_device() == dev):
+        for c in caches:
+            if c.pages.state is not pages.state or c.pages.B != pages.B or c.k.get_device() != dev:
+                raise ValueError(f"the caches must share one PageState, on GPU {dev}")
+            c.c()
+    return b"".join(map(_pc_raw, caches)), n, pages
 
 
 def fc_pcache_step(ctx: Context, caches, lens: torch.Tensor, n_new: torch.Tensor | None, n: int,
