@@ -129,8 +129,9 @@ __global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAt
 #pragma unroll
       for (int d = 0; d < DT; ++d) vw[s][d] = load16<NT>(p + s * (HD * kPTile) + 16 * d * kPTile);
   };
-  const int last = (a.cap + kKeyBlock - 1) / kKeyBlock - 1;
-  int at = min(blo + wave, last), next = min(at + 4, last);
+  // the block that a wave goes on with; its last one again, which the L2 holds, where it has no other
+  auto behind = [&](int blk) { return blk + 4 < bhi ? blk + 4 : blk; };
+  int at = min(blo + wave, bhi - 1), next = behind(at);
   int kp = page_of(at, l16 >> 2), vp = page_of(at, g);
   int kp_next = page_of(next, l16 >> 2), vp_next = page_of(next, g);
   // mask bytes of the lane's 16 keys, a block ahead as well
@@ -160,8 +161,8 @@ __global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAt
 
   for (int blk = blo + wave; blk < bhi; blk += 4) {
     const int j0 = blk * kKeyBlock, jg = j0 + 16 * g;
-    next = min(blk + 4, last);
-    const int after = min(blk + 8, last);
+    next = behind(blk);
+    const int after = behind(next);
     const bool whole = __all(a.t.there(vp));
     const bool full = !a.mask && j0 + kKeyBlock <= kall && whole;
     uint32_t vis = 0xFFFFu;                       // the lane's 16 keys that some row may see
