@@ -51,11 +51,18 @@ struct Share {
   int item, start, used, per;       // the item, its first slot, its slots, blocks of each
   int held, m;                      // its rows held and new
 };
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return __builtin_amdgcn_readfirstlane(x);
+// Sums over a wave's lanes up to each one, by moves within the vector unit: rows of 16 lanes first, then a
+// row's sum to the next one, then the first half's to the second.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast:15 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast:31 to rows 2 and 3
+  return x;
 }
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 // The share of the item that slot `slot` falls to (item -1: none).
 template <class A>
 __device__ __forceinline__ Share share_of(const A &a, int slot) {
@@ -97,12 +104,7 @@ __device__ __forceinline__ Share share_of(const A &a, int slot) {
   int run = 0;
   for (int i = 0;;) {
     const int u = (int)((unsigned)(x + per - 1) / (unsigned)per);
-    int inc = u;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o);
-      if (lane >= o) inc += y;
-    }
+    const int inc = wave_scan(u);
     const int at = run + inc - u;
     const unsigned long long hit = __ballot(slot >= at && slot < at + u);
     if (hit) {

@@ -39,6 +39,7 @@ struct PAttnArgs {
   int2 *plan;                        // [B] k_pattn: an item's first slot and its slots
   float c;                           // scale log2(e)
   int B, n, H, KV, G, cap, splits, least, tile_rows, slots;
+  int head_xcds;                     // k_pattn: XCDs of a head, or 0: heads along the grid's other axis
   int row_tiles, stride;             // k_pattn_rows: of a pair; pairs whose pieces take turns
   int *queue, pieces;                // k_pattn_rows: 8 counts of pieces taken behind the first ones, or null
   Quot by_g;                         // division by G
@@ -93,20 +94,31 @@ __global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAt
   constexpr int KC = HD / 32;                   // 16-byte pieces of a key row that a lane holds
   constexpr int DT = HD / 16;                   // output tiles of 16 dims
   constexpr int OS = HD + 4;
+  // Whether a wave's last look ahead is made too: short shares are better off without (sixteen items of 2200
+  // rows 20.0 and 16.9 us, of up to 4200 25.2 and 23.6; one of 2176 10.9 and 9.8), but the branch costs
+  // where loads are what bounds it (eight long ones 149.6 and 152.6) and with two row tiles (27.0 and 27.8).
+  constexpr bool ALWAYS = NT || MT == 2;
   __shared__ float sm_o[4][16][OS];
   __shared__ float2 sm_ml[4][16 * MT];
   __shared__ float sm_l[16];
   __shared__ OddKeys sm_odd[4][HD];
-  const Share sh = share_of(a, blockIdx.x);
+  // Workgroups go round the 8 XCDs; each of these keeps to one head (several share it where there are fewer),
+  // so that pages that several items hold come out of its L2 (sixteen answers on one history 17.1 to 16.5 us,
+  // 64 items of their own 67.9 to 68.8).
+  const int xcd = blockIdx.x % 8, turn = blockIdx.x / 8;
+  const int kv = a.head_xcds ? xcd / a.head_xcds : blockIdx.y;
+  const int my_slot = a.head_xcds ? turn * a.head_xcds + xcd % a.head_xcds : blockIdx.x;
+  if (my_slot >= a.slots) return;
+  const Share sh = share_of(a, my_slot);
   if (sh.item < 0) return;
-  const int b = sh.item, kv = blockIdx.y, R = a.n * a.G;
+  const int b = sh.item, R = a.n * a.G;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, l16 = lane & 15;
   const int held = sh.held, m = sh.m, rows = m * a.G;   // m > 0
   const int kmax = held + m;                    // keys that any row sees
   const int kall = held + 1;                    // keys that every row sees, but for the mask
-  const int blocks = (kmax + kKeyBlock - 1) / kKeyBlock, blo = (blockIdx.x - sh.start) * sh.per;
+  const int blocks = (kmax + kKeyBlock - 1) / kKeyBlock, blo = (my_slot - sh.start) * sh.per;
   const int bhi = min(blocks - blo, sh.per) + blo;
-  const long slot = (long)kv * a.slots + blockIdx.x;
+  const long slot = (long)kv * a.slots + my_slot;
   if (a.plan && kv == 0 && blo == 0 && tid == 0) a.plan[b] = make_int2(sh.start, sh.used);
   // S^T row m of tile t is key (m / 4) 16 + 4 t + m % 4
   const int in_page = (1 << a.t.shift) - 1;
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAt
         for (int i = 0; i < KC; ++i)
           s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[x][i]), q[t][i], s[x], 0, 0, 0);
       }
-      if (t == MT - 1) load_k(next, kp_next);
+      if (t == MT - 1 && (ALWAYS || blk + 4 < bhi)) load_k(next, kp_next);
       const uint32_t sees = full ? 0xFFFFu : vis & (uint32_t)seen_bits(seen[t] - jg);
       float top = kNegInf;
 #pragma unroll
@@ -257,7 +269,7 @@ __global__ __launch_bounds__(256, HD == 128 && MT == 2 ? 1 : 2) void k_pattn(PAt
           for (int e = 0; e < 4; ++e) o[t][d][e] += odd_sum(sm_odd[wave][16 * d + 4 * g + e], keys);
       }
     }
-    load_v(next, vp_next);
+    if (ALWAYS || blk + 4 < bhi) load_v(next, vp_next);
     kp = kp_next, vp = vp_next;
     kp_next = page_of(after, l16 >> 2), vp_next = page_of(after, g);
   }
@@ -831,7 +843,8 @@ fc_status run_pattn(fc_ctx *ctx, PAttnArgs &a, hipStream_t st) {
     else hipLaunchKernelGGL((k_pattn_rows<HD, 2, false>), dim3((unsigned)a.pieces), dim3(128), 0, st, a);
     FC_LAUNCH_OK(st, "k_pattn_rows");
   } else {
-    const dim3 grid((unsigned)a.slots, (unsigned)a.KV);
+    a.head_xcds = 8 % a.KV == 0 ? 8 / a.KV : 0;
+    const dim3 grid = a.head_xcds ? dim3((unsigned)((a.slots + a.head_xcds - 1) / a.head_xcds * 8)) : dim3((unsigned)a.slots, (unsigned)a.KV);
     ProfScope ps(ctx, st, "fc_pattn");
     const bool big = std::min(pairs * a.cap, ((long)a.t.pages * a.KV) << a.t.shift) * HD * 4 > (384L << 20);
     if (MT == 1 && big) hipLaunchKernelGGL((k_pattn<HD, 1, true>), grid, dim3(256), 0, st, a);
