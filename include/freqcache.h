@@ -605,7 +605,8 @@ fc_status fc_pcache_init(fc_ctx *ctx, const fc_pcache *cache, int32_t B, void *s
  * nearest even), keys and values into their rows' pages, for item b the rows len[b] .. len[b] +
  * n_new[b] - 1.  Arguments and their limits as in fc_qcache_append, with max_pages page_rows as
  * the capacity.  Rows without a page are dropped (their q_out is written), rows past the capacity
- * too (their q_out left as it is).  The pages must be the item's own where rows are written
+ * too (their q_out left as it is).  FC_ERR_UNSUPPORTED for more than 65535 heads, 2^27 - 15 tokens
+ * or 2^30 rows (tokens times heads) an item.  The pages must be the item's own where rows are written
  * (fc_pcache_step has granted them): of two items that write one row either may win. */
 fc_status fc_pcache_append(fc_ctx *ctx, const fc_pcache *cache, const fc_rope_axes *rope,
                            const fc_qkv_rows *rows, const int32_t *pos, const int32_t *len,

@@ -1024,7 +1024,7 @@ fc_status fc_pcache_append(fc_ctx *ctx, const fc_pcache *cache, const fc_rope_ax
   const fc_qkv_rows &x = *rows;
   if ((st = check_qrows(c.n_kv_heads, c.max_pages * c.page_rows, x.n_heads, n, who)) != FC_OK) return st;
   if ((n + 2L * FC_PCACHE_TILE - 2) / FC_PCACHE_TILE > kQGridBlocks)   // they may start inside a group of rows
-    return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens in one call (at most 2^27 - 22)", who, n);
+    return fail(FC_ERR_UNSUPPORTED, "%s: %d tokens in one call (at most 2^27 - 15)", who, n);
   if ((st = check_rope(*rope, c.head_dim, who)) != FC_OK) return st;
   QBuffers buf;
   buf.add(c.k, pool_bytes(c));

@@ -459,3 +459,315 @@ def test_step_many_items_and_pages(fc, ctx):
         keep = [int(lens[s] * rng.random()) for s in src]
         run_step(fc, ctx, caches, src, keep, [int(x) for x in rng.integers(0, 40, B)], 40)
         run_compact(fc, ctx, caches)
+
+
+def test_init(fc, ctx):
+    state = fc.PageState(torch.full((103,), 5, dtype=torch.int32, device="cuda"), 3, 7, 75)      # 21 entries, 3 zeros, 75 holders, the rest not its own
+    cache = fc.PCache.alloc(state, 1, 64, 16)
+    fc.fc_pcache_init(ctx, cache)
+    assert state.state.tolist() == [-1] * 21 + [0] * 78 + [5] * 4
+
+
+# ------------------------------------------------------------------------------ as a program runs them
+@pytest.mark.parametrize("heads,R", [("qwen", 64), ("toy", 16), ("three", 32)])
+def test_answers_from_one_history(fc, ctx, heads, R):
+    """A prompt, answers that go on from it and from each other, items that end and begin, a compaction: at
+    every step the attention is that over the rows which each item's own text has brought."""
+    g = torch.Generator().manual_seed(9)
+    H, kv, hd, sec = HEADS[heads]
+    B, M, layers = 4, op.pages_of(150, R) + 1, 2
+    state = fc.PageState.alloc(B, M, B * M)
+    caches = [fc.PCache.alloc(state, kv, hd, R) for _ in range(layers)]
+    rope = fc.RopeAxes(1e6, sec)
+    none = torch.zeros(0, kv, hd, dtype=torch.float64)
+    rows = [[(none, none)] * B for _ in range(layers)]      # what each item has brought, per layer: keys rotated in 64 bits, values
+    lens = [0] * B
+    plan = [(None, [77, 0, 0, 0]), ([0, 0, 0, -1], [1, 1, 1, 0]), (None, [1, 1, 1, 1]), ([1, 1, 2, 1], [5, 5, 5, 0]), (None, [1, 0, 2, 1]),
+            ([3, 2, 2, 0], [40, 1, 1, 1])]
+    for turn, (src, new) in enumerate(plan):
+        base = [(lens[s] if 0 <= s < B else 0) for s in (src or range(B))]
+        if turn == 4:
+            base[2] = 60                                     # rows given up
+        n = max(new)
+        granted = torch.zeros(B, dtype=torch.int32, device="cuda")
+        fc.fc_pcache_step(ctx, caches, ints(base), ints(new), n, granted, src=None if src is None else ints(src))
+        if turn == 3:
+            fc.fc_pcache_compact(ctx, caches)
+        assert granted.tolist() == new
+        for layer, c in enumerate(caches):
+            q, k, v = randn(g, B, n, H + 2 * kv, hd).split([H, kv, kv], 2)
+            pos = torch.randint(0, 3000, (rope.axes, B, n), generator=g, dtype=torch.int32).cuda()
+            qo, out = torch.zeros(B, n, H, hd, dtype=torch.bfloat16, device="cuda"), torch.full((B, n, H, hd), 9.0, dtype=torch.bfloat16, device="cuda")
+            fc.fc_pcache_append(ctx, c, rope, q, k, v, pos, ints(base), granted, qo)
+            fc.fc_pcache_attention(ctx, c, qo, ints(base), granted, out)
+            torch.cuda.synchronize()
+            old = [rows[layer][s] if 0 <= s < B else (none, none) for s in (src or range(B))]
+            for b in range(B):
+                kr = torch.from_numpy(op.rotate(f64(k[b]), pos[:, b].cpu().numpy(), sec, 1e6))
+                kk = torch.cat([old[b][0][:base[b]], kr[:new[b]]])
+                vv = torch.cat([old[b][1][:base[b]], torch.from_numpy(f64(v[b]))[:new[b]]])
+                rows[layer][b] = (kk, vv)
+                m, L = new[b], base[b] + new[b]
+                want, absv, mass = op.attention(kk.numpy().transpose(1, 0, 2), vv.numpy().transpose(1, 0, 2), f64(qo[b, :m]), base[b], hd ** -0.5, np.ones(L))
+                # keys are rounded to bfloat16 when they are appended: 2^-8 of sum |q k|, twice in a quotient of exponentials
+                rel = (4 * (hd + 4) * 2.0 ** -24 + 2 * 1.01 * 2.0 ** -8) * mass + 2.0 ** -22 + L * 2.0 ** -24
+                rel = np.expm1(rel)
+                off = np.abs(f64(out[b, :m]) - want) - 2.0 ** -8 * np.abs(want) - (2.0 ** -8 + rel)[..., None] * absv
+                assert (off <= 0).all() and (out[b, m:] == 9).all(), f"turn {turn}, layer {layer}, item {b}: {off.max()}"
+                # and exactly what the cache holds
+                check(c, b, qo[b], out[b], base[b], m, hd ** -0.5)
+        lens = [h + m for h, m in zip(base, new)]
+
+
+def test_captured_step_replays_match_eager(fc, ctx):
+    """Pages granted, rows appended, attention, the lengths' advance and a compaction captured into one graph,
+    replayed with other inputs and with eager calls between; each replay equals the eager calls."""
+    g = torch.Generator().manual_seed(14)
+    H, kv, hd, sec = HEADS["qwen"]
+    B, n, R, M, P = 3, 3, 32, 8, 20
+    rope = fc.RopeAxes(1e6, sec)
+
+    def make():
+        state = fc.PageState.alloc(B, M, P)
+        return dict(pages=state, c=[fc.PCache.alloc(state, kv, hd, R) for _ in range(2)], src=ints([0] * B), lens=ints([0] * B), new=ints([0] * B),
+                    granted=ints([0] * B), live=ints([0]), x=torch.zeros(B, n, H + 2 * kv, hd, dtype=torch.bfloat16, device="cuda"), pos=ints([[[0] * n] * B] * 3),
+                    q=torch.zeros(B, n, H, hd, dtype=torch.bfloat16, device="cuda"), out=torch.zeros(B, n, H, hd, dtype=torch.bfloat16, device="cuda"))
+
+    def step(s):
+        fc.fc_pcache_step(ctx, s["c"], s["lens"], s["new"], n, s["granted"], src=s["src"])
+        fc.fc_pcache_compact(ctx, s["c"], s["live"])
+        q, k, v = s["x"].split([H, kv, kv], 2)
+        for c in s["c"]:
+            fc.fc_pcache_append(ctx, c, rope, q, k, v, s["pos"], s["lens"], s["granted"], s["q"])
+            fc.fc_pcache_attention(ctx, c, s["q"], s["lens"], s["granted"], s["out"])
+        s["lens"].add_(s["granted"])
+
+    def tensors(s):
+        return [c.k for c in s["c"]] + [c.v for c in s["c"]] + [s["pages"].state] + [s[x] for x in ("lens", "granted", "live", "q", "out")]
+
+    init = make()
+    fill_table(init["pages"], [200, 40, 0], R, g)
+    for c in init["c"]:
+        c.k.copy_(randn(g, *c.k.shape))
+        c.v.copy_(randn(g, *c.v.shape))
+    a, e = make(), make()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a)
+    for rep, (src, held, new) in enumerate([([0, 1, 2], [200, 40, 0], [3, 1, 2]), ([0, 0, 0], [199, 130, 65], [3, 3, 3]), ([1, 1, 0], [39, 40, 5], [0, 2, 3]),
+                                            ([0, 1, 1], [200, 33, 33], [3, 1, 1])]):
+        x = randn(g, B, n, H + 2 * kv, hd)
+        pos = torch.randint(0, 999, (3, B, n), generator=g, dtype=torch.int32).cuda()
+        for s in (a, e):
+            for c, d in zip(s["c"], init["c"]):
+                c.k.copy_(d.k)
+                c.v.copy_(d.v)
+            s["pages"].state.copy_(init["pages"].state)
+            for name, t in (("x", x), ("pos", pos), ("src", ints(src)), ("lens", ints(held)), ("new", ints(new))):
+                s[name].copy_(t)
+            s["q"].zero_()
+            s["out"].zero_()
+        step(e)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (u, w) in enumerate(zip(tensors(a), tensors(e))):
+            assert torch.equal(u.view(torch.uint8), w.view(torch.uint8)), f"replay {rep}, tensor {i}"
+
+
+def test_two_streams_two_contexts(fc, ctx):
+    """Calls at once on two streams, each with its own context, give what they give alone."""
+    g = torch.Generator().manual_seed(15)
+    H, kv, hd, _ = HEADS["qwen"]
+    B, R, M, lens = 2, 64, 33, [2000, 1500]
+    caches, q = [], [randn(g, B, n, H, hd) for n in (1, 40)]
+    for _ in range(2):
+        state = fc.PageState.alloc(B, M, B * M)
+        fill_table(state, [h + 40 for h in lens], R, g)
+        caches.append(pool(g, state, kv, hd, R, fc))
+    out, want = [torch.zeros_like(x) for x in q], [torch.zeros_like(x) for x in q]
+    for i in range(2):
+        fc.fc_pcache_attention(ctx, caches[i], q[i], ints(lens), None, want[i])
+    torch.cuda.synchronize()
+    t = ints(lens)
+    with fc.Context(fc.Caps(**SMALL)) as other:
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for i, (s, c) in enumerate(zip(streams, (ctx, other))):
+                with torch.cuda.stream(s):
+                    fc.fc_pcache_attention(c, caches[i], q[i], t, None, out[i])
+        torch.cuda.synchronize()
+        for i in range(2):                                   # a stream by name
+            out[i].zero_()
+        torch.cuda.synchronize()
+        fc.fc_pcache_attention(other, caches[1], q[1], t, None, out[1], stream=streams[0])
+        streams[0].synchronize()
+        assert torch.equal(out[1], want[1])
+        fc.fc_pcache_attention(other, caches[0], q[0], t, None, out[0], stream=streams[1])
+        torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(out[i], want[i])
+
+
+@pytest.mark.parametrize("heads,n", [("qwen", 1), ("wide", 37), ("qwen", 300)])
+def test_same_inputs_same_bytes(fc, ctx, heads, n):
+    """And an item's rows do not depend on what else is in its batch's pages, nor on which pages hold them."""
+    g = torch.Generator().manual_seed(16)
+    H, kv, hd, _ = HEADS[heads]
+    B, R, M, lens = 3, 32, 60, [900, 500, 0]
+    k, v, q = randn(g, B, kv, M * R, hd), randn(g, B, kv, M * R, hd), randn(g, B, n, H, hd)
+    got = []
+    for turn in range(3):
+        state = fc.PageState.alloc(B, M, B * M + 5)
+        table = fill_table(state, [h + n for h in lens], R, g)
+        cache = pool(g, state, kv, hd, R, fc)
+        for b in range(B):
+            for i, p in enumerate(table[b]):
+                if p >= 0:
+                    cache.k[p] = k[b, :, i * R:(i + 1) * R]
+                    cache.v[p] = v[b, :, i * R:(i + 1) * R].reshape(kv, R // 8, 8, hd).transpose(-1, -2)
+        for _ in range(2):
+            out = torch.zeros_like(q)
+            fc.fc_pcache_attention(ctx, cache, q, ints(lens), None, out)
+            got.append(out)
+    for o in got[1:]:
+        assert torch.equal(o, got[0])
+
+
+def test_guards(fc, ctx):
+    """Every buffer inside a larger allocation whose bytes around it stay as they are."""
+    from tests.test_gpu_guards import Guarded
+    g = torch.Generator().manual_seed(17)
+    H, kv, hd, sec = HEADS["qwen"]
+    B, n, R, M, P = 3, 70, 32, 7, 17
+    gd = Guarded()
+
+    def buf(shape, dtype, fill):
+        return gd.new(shape, dtype, fill if isinstance(fill, torch.Tensor) else torch.full((1,), fill, dtype=dtype, device="cuda"))
+    bf, i32 = torch.bfloat16, torch.int32
+    state = fc.PageState(buf((24 + P,), i32, -1), B, M, P)
+    caches = [fc.PCache(buf((P, kv, R, hd), bf, float("nan")), buf((P, kv, R // 8, hd, 8), bf, float("nan")), state) for _ in range(2)]
+    fc.fc_pcache_init(ctx, caches[0])
+    x = buf((B, n, H + 2 * kv, hd), bf, randn(g, B, n, H + 2 * kv, hd))
+    q, out = buf((B, n, H, hd), bf, 0), buf((B, n, H, hd), bf, 0)
+    pos, lens, new = buf((3, B, n), i32, 5), buf((B,), i32, ints([0, 0, 0])), buf((B,), i32, ints([70, 64, 3]))
+    granted, live, src = buf((B,), i32, 0), buf((1,), i32, 0), buf((B,), i32, ints([2, 0, 0]))
+    mask = buf((B, M * R), torch.uint8, 1)
+    for turn in range(4):
+        fc.fc_pcache_step(ctx, caches, lens, new, n, granted, src=src if turn == 1 else None)
+        fc.fc_pcache_compact(ctx, caches, live)
+        a, b, c = x.split([H, kv, kv], 2)
+        for cache in caches:
+            fc.fc_pcache_append(ctx, cache, fc.RopeAxes(1e6, sec), a, b, c, pos, lens, granted, q)
+            fc.fc_pcache_attention(ctx, cache, q, lens, granted, out, key_mask=mask)
+        lens.copy_(ints([3, 40, 70]) if turn == 0 else lens + granted)
+    gd.check()
+    assert not out.isnan().any()
+
+
+def test_debug_mode_and_kernel_times(fc, ctx):
+    """The calls run under the debug mode, and their kernels appear in the context's timing."""
+    g = torch.Generator().manual_seed(18)
+    prev = fc.fc_debug(True)
+    fc.fc_profile_enable(ctx, True)
+    try:
+        fc.fc_profile_read(ctx, None, reset=True)
+        test_append(fc, ctx, "toy", 5, 16, [14, 12, 11], [5, 5, 0])
+        run_attention(fc, ctx, g, "toy", 1, 16, [700], None)
+        run_attention(fc, ctx, g, "toy", 60, 16, [700], None)
+        test_step_edges(fc, ctx)
+        test_init(fc, ctx)
+        for name in ("fc_pappend", "fc_pattn", "fc_pattn_rows", "fc_pattn_join", "fc_pstep", "fc_pstep_copy", "fc_pcompact", "fc_pcompact_move", "fc_pinit"):
+            assert fc.fc_profile_read(ctx, name)[1] >= 1, name
+    finally:
+        fc.fc_profile_enable(ctx, False)
+        fc.fc_profile_read(ctx, None, reset=True)
+        fc.fc_debug(prev)
+
+
+def test_binding_refusals(fc, ctx):
+    """What the binding and the library refuse, with nothing written."""
+    H, kv, hd, sec = HEADS["toy"]
+    state, other = fc.PageState.alloc(2, 4, 9), fc.PageState.alloc(2, 4, 9)
+    c, d = fc.PCache.alloc(state, kv, hd, 32), fc.PCache.alloc(other, kv, hd, 32)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    x = torch.ones(2, 3, H + 2 * kv, hd, **bf)
+    q, k, v = x.split([H, kv, kv], 2)
+    pos, lens, rope = ints([[[0] * 3] * 2] * 3), ints([0, 0]), fc.RopeAxes(1e6, sec)
+    qo, granted, live = torch.ones(2, 3, H, hd, **bf), ints([7, 7]), ints([7])
+    state.table.fill_(3)
+    kept = [c.k, c.v, state.state, qo, granted, live]
+    before = [t.clone() for t in kept]
+    bad = [
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos[0], lens, None, qo),                      # one axis for three
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos, lens, None, None),
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k[:1], v, pos, lens, None, qo),
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k.float(), v, pos, lens, None, qo),
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos, lens.long(), None, qo),
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos, lens, ints([1]), qo),
+        lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos.cpu(), lens, None, qo),
+        lambda: fc.fc_pcache_attention(ctx, c, qo[..., :32].contiguous(), lens, None, qo),
+        lambda: fc.fc_pcache_attention(ctx, c, qo[:1], lens, None, qo),
+        lambda: fc.fc_pcache_attention(ctx, c, qo[0], lens, None, qo),
+        lambda: fc.fc_pcache_attention(ctx, c, qo, lens, None, torch.ones(2, 3, H, hd, device="cuda")),
+        lambda: fc.fc_pcache_attention(ctx, c, qo, lens, None, torch.ones_like(qo), key_mask=torch.ones(2, 127, dtype=torch.uint8, device="cuda")),
+        lambda: fc.fc_pcache_step(ctx, [], lens, None, 3, granted),
+        lambda: fc.fc_pcache_step(ctx, [c, d], lens, None, 3, granted),
+        lambda: fc.fc_pcache_step(ctx, [c], lens[:1], None, 3, granted),
+        lambda: fc.fc_pcache_step(ctx, [c], lens, None, 3, granted.long()),
+        lambda: fc.fc_pcache_step(ctx, [c], lens, None, 3, granted, src=lens.cpu()),
+        lambda: fc.fc_pcache_compact(ctx, [d, c], live),
+        lambda: fc.PCache(c.k[:8], c.v[:8], state),
+        lambda: fc.PCache(c.k, c.v.view(9, kv, 4, 8, hd), state),
+        lambda: fc.PCache(c.k.float(), c.v, state),
+        lambda: fc.PageState(state.state[:16], 2, 4, 9),
+        lambda: fc.PageState(state.state.long(), 2, 4, 9),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} went through")
+    status = [
+        (1, lambda: fc.fc_pcache_append(ctx, c, fc.RopeAxes(1e6, (8, 8, 8)), q, k, v, pos, lens, None, qo)),
+        (2, lambda: fc.fc_pcache_append(ctx, c, rope, q[:, :, :3], k, v, pos, lens, None, qo)),
+        (1, lambda: fc.fc_pcache_append(ctx, c, rope, q, k, v, pos, lens, None, x.view(-1)[:2 * 3 * H * hd].view(2, 3, H, hd))),
+        (1, lambda: fc.fc_pcache_attention(ctx, c, qo, lens, None, qo)),
+        (1, lambda: fc.fc_pcache_attention(ctx, c, qo, lens, None, torch.ones_like(qo), scale=float("nan"))),
+        (2, lambda: fc.fc_pcache_attention(ctx, c, torch.ones(2, 129, H, hd, **bf), lens, None, torch.ones(2, 129, H, hd, **bf))),
+        (1, lambda: fc.fc_pcache_step(ctx, [c, c], lens, None, 3, granted)),
+        (2, lambda: fc.fc_pcache_step(ctx, [c], lens, None, -1, granted)),
+        (1, lambda: fc.fc_pcache_step(ctx, [c], granted, None, 3, granted)),
+        (1, lambda: fc.fc_pcache_compact(ctx, [c], state.holders)),
+        (2, lambda: fc.fc_pcache_step(ctx, [c, fc.PCache.alloc(state, kv, 128, 32)], lens, None, 3, granted)),
+        (6, lambda: fc.fc_pcache_attention(ctx, fc.PCache.alloc(state, kv, 32, 32), torch.ones(2, 1, H, 32, **bf), lens, None, torch.ones(2, 1, H, 32, **bf))),
+        (2, lambda: fc.fc_pcache_init(ctx, fc.PCache.alloc(state, kv, hd, 8))),
+    ]
+    for i, (want, f) in enumerate(status):
+        with pytest.raises(fc.FcError) as e:
+            f()
+            pytest.fail(f"call {i} went through")
+        assert e.value.status == want, (i, str(e.value))
+    torch.cuda.synchronize()
+    for t, u in zip(before, kept):
+        assert torch.equal(t.view(torch.uint8), u.view(torch.uint8))
+
+
+def test_a_cache_whose_memory_has_moved(fc, ctx):
+    """The layers' descriptors follow their tensors."""
+    g = torch.Generator().manual_seed(19)
+    _, kv, hd, _ = HEADS["toy"]
+    state = fc.PageState.alloc(2, 4, 9)
+    caches = [pool(g, state, kv, hd, 16, fc) for _ in range(2)]
+    run_step(fc, ctx, caches, None, [0, 0], [30, 20], 64)
+    old = caches[1].k.clone()
+    caches[1].k.set_(old)
+    run_step(fc, ctx, caches, [0, 0], [30, 30], [5, 5], 5)
+    caches[0].v.set_(caches[0].v[:8].clone())
+    with pytest.raises(ValueError, match="elements"):
+        fc.fc_pcache_step(ctx, caches, ints([0, 0]), None, 64, ints([0, 0]))

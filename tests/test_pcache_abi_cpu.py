@@ -1,0 +1,75 @@
+"""The argument checks of the paged token cache's calls without a GPU: the C ABI's statuses through a host
+driver (tests/pcache_validation_host.hip), once linked to the built library and once with the checks
+compiled under the host sanitizers, the binding's struct against the header, and the binding's own
+checks."""
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+
+
+@pytest.fixture(scope="module")
+def fc():
+    import paper_2604_24391_amd as fc
+    fc.lib()
+    return fc
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
+@pytest.mark.parametrize("sanitized", [False, True])
+def test_statuses(fc, tmp_path, sanitized):
+    exe, lib = str(tmp_path / "pcache_validation"), fc.freqcache.LIB
+    checks = []
+    if sanitized:
+        for what in ("address", "undefined"):
+            checks += ["-Xarch_host", "-fsanitize=" + what]
+        checks += ["-Xarch_host", "-fno-sanitize-recover=all", os.path.join(ROOT, "paper_2604_24391_amd", "csrc", "abi.hip")]
+    cmd = [HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-result",
+           "-Wno-unused-value", *checks, os.path.join(ROOT, "tests", "pcache_validation_host.hip"), "-L" + os.path.dirname(lib),
+           "-l:" + os.path.basename(lib), "-Wl,-rpath," + os.path.dirname(lib), "-o", exe]
+    res = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert res.returncode == 0, res.stderr[-4000:]
+    env = dict(os.environ, HIP_VISIBLE_DEVICES="")      # never a device, even where one exists
+    env.pop("FC_DEBUG", None)
+    env["ASAN_OPTIONS"] = "detect_leaks=0:abort_on_error=0:halt_on_error=1"
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120, env=env)
+    assert run.returncode == 0 and "OK (0 failed expectations)" in run.stdout, run.stdout + run.stderr
+
+
+def test_struct_layout(fc, tmp_path):
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no C compiler")
+    st = fc.freqcache.fc_pcache
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "freqcache.h"', 'int main(void) {', '  printf("%zu\\n", sizeof(fc_pcache));']
+    lines += [f'  printf("%zu\\n", offsetof(fc_pcache, {n}));' for n, _ in st._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ['  return 0;', '}']) + "\n")
+    subprocess.run([cc, "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(st)] + [getattr(st, n).offset for n, _ in st._fields_]
+
+
+def test_handle_checks(fc):
+    """Shapes are checked before devices: a CPU tensor is refused for being one only when all else fits."""
+    for args, word in (((0, 3, 5), "items"), ((2, 0, 5), "items"), ((2, 3, 0), "items"), ((1 << 15, 1 << 15, 5), "table"), ((2, 3, 5), "GPU")):
+        with pytest.raises(ValueError, match=word):
+            fc.PageState(torch.zeros(100, dtype=torch.int32), *args)
+
+    class Pages:           # stands for a state on a GPU
+        state, n_pages, max_pages, B = torch.zeros(100, dtype=torch.int32), 5, 3, 2
+    bf = torch.bfloat16
+    k, v = torch.zeros(5, 2, 32, 64, dtype=bf), torch.zeros(5, 2, 4, 64, 8, dtype=bf)
+    for a, b, word in ((k[0], v, "n_kv"), (k[:4], v, "pages"), (k, k, "v is"), (k, v[:, :, :3], "v is"), (k[:, :, :20], v, "pages of 20"), (k, v, "GPU")):
+        with pytest.raises(ValueError, match=word):
+            fc.PCache(a, b, Pages)
+
+
+def test_state_bytes(fc):
+    assert fc.pcache_state_bytes(3, 3, 5) == 68 and fc.pcache_state_bytes(0, 3, 5) == 0
