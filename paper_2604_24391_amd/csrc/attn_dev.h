@@ -132,40 +132,25 @@ __device__ __forceinline__ void dma4(const void *gp, uint32_t lds) {
       : "memory");
 }
 
-// N KB as dma16, from base (wave-uniform) on to lds on: a lane brings the bytes (off ^ i STEP) of the i-th KB.
-// (An instruction's offset counts on both sides.)
-template <int N, int STEP>
-__device__ __forceinline__ void dma_run(const void *base, int off, uint32_t lds) {
-  static_assert(N == 2 || N == 4, "runs of 2 or 4 KB");
-  const uint32_t l = __builtin_amdgcn_readfirstlane(lds);
-  const uint64_t p = (uint64_t)(uintptr_t)base;
-  const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
-                      (uint32_t)__builtin_amdgcn_readfirstlane((int)p);
+// 1 KB as dma16, from base + off + AT (base wave-uniform, off in bytes) to lds + AT: an instruction's offset counts
+// on both sides.
+template <int AT>
+__device__ __forceinline__ void dma16_at(uint64_t base, int off, uint32_t lds) {
   uint32_t saved;
-  if constexpr (N == 4)
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %6\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off), "v"(off ^ STEP), "v"(off ^ 2 * STEP), "v"(off ^ 3 * STEP), "s"(at), "s"(l)
-        : "memory");
-  else
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %4\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off), "v"(off ^ STEP), "s"(at), "s"(l)
-        : "memory");
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2 offset:%c4\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(off), "s"(base), "s"(lds), "i"(AT)
+      : "memory");
+}
+__device__ __forceinline__ uint64_t uniform_address(const void *p) {
+  const uint64_t x = (uint64_t)(uintptr_t)p;
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
 // The kernel's arguments read anew, which keeps no register between two reads.

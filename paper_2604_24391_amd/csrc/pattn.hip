@@ -380,14 +380,20 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 // 165 us before and 114 now, of 1024 397 and 323, ragged 310 and 254; of equal length 312 without queues
 // and 319 with).
 //
-// A wave goes half a block (32 keys) at a time: the scores of the next half are computed beside the
-// exponentials of this one, so that matrix and vector instructions alternate within the wave (with each
-// kind in a run of its own, two waves on a SIMD took the sum of both: 544 us for a prompt of 8192 rows
-// of 28 heads).  Keys are therefore brought half a block ahead of values, and every operand is read from
-// LDS a step before its use.  No maximum is looked for (see `step`): a third fewer vector instructions.
-// That prompt (0.48 TFLOP) takes 478 to 498 us, 0.97 to 1.01 PFLOP/s, the matrix unit busy for 49 % of its
-// cycles, at a clock of 1.9 to 2.0 GHz of 2.4: power holds it there, and cycles saved since came back as a
-// lower clock.
+// A wave goes half a block (32 keys) at a time: beside the exponentials of its scores run the products of the
+// next half's scores and of the last half's values, one exponential to a product, so that matrix and
+// vector unit work at the same time (with each kind in a run of its own two waves on a SIMD took the sum of
+// both: 544 us for a prompt of 8192 rows of 28 heads; with the values' products alone in a run 499).  Keys are
+// therefore brought a block ahead of values, and operands are read from LDS four products before their use (eight: the
+// same).  No maximum is looked for (see `step`): a third fewer vector instructions.  Page numbers come by vector
+// loads a block ahead, as a scalar load would have every wait for LDS wait for it.
+//
+// That prompt (0.48 TFLOP) takes 470 to 497 us, 0.97 to 1.02 PFLOP/s, the matrix unit busy for half of its
+// cycles, at a clock of 1.86 GHz of 2.4: power holds it there, and cycles saved (a seventh of them since
+// 531 us) came back as a lower clock.  Two row tiles in a wave would halve what LDS delivers for each
+// product, but the compiler keeps no 128 output registers out of the vector unit's way there (650 us).
+// 256 tokens over 2176 rows: 23 us, eight or nine blocks one after the other on 224 workgroups, and their
+// start and end.
 //
 // A row of keys is 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks; columns of
@@ -431,9 +437,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     if (split >= used) return;
     const int blo = (int)((long)blocks * split / used), bhi = (int)((long)blocks * (split + 1) / used);
 
-    // pages of a block's four runs of 16 rows (blocks behind the last one are read as it)
-    typedef const __attribute__((address_space(4))) int32_t *uniform_ints;
-    const uniform_ints table = (uniform_ints)(uintptr_t)(a.t.table + (long)b * a.t.width);
+    // Pages of a block's four runs of 16 rows (blocks behind the last one are read as it).  They are loaded
+    // by lanes (0 to 3: a run each) a block before they are looked at: scalar loads would have every
+    // wait for LDS wait for them too.
     // (neither an array nor a choice between members: the compiler would put them into memory for a wave's
     // number to index)
     struct Pages {
@@ -443,14 +449,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
         return (int)(((ab & ~m) | (cd & m)) >> (32 * (run & 1)));
       }
     };
-    auto pages_of = [&](int blk) {
-      const int at = min(blk, bhi - 1);
-      if (a.t.shift >= 6) {
-        const uint64_t e = (uint64_t)(uint32_t)table[at >> (a.t.shift - 6)];
-        return Pages{e | e << 32, e | e << 32};
-      }
-      auto entry = [&](int run) { return (uint64_t)(uint32_t)table[min((4 * at + run) >> (a.t.shift - 4), a.t.width - 1)]; };
-      return Pages{entry(0) | entry(1) << 32, entry(2) | entry(3) << 32};
+    auto entries_of = [&](int blk) {
+      return a.t.entry(b, min((4 * min(blk, bhi - 1) + (lane & 3)) >> (a.t.shift - 4), a.t.width - 1));
+    };
+    auto unpack = [&](int e) {
+      auto lane_of = [&](int x) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(e, x); };
+      return Pages{lane_of(0) | lane_of(1) << 32, lane_of(2) | lane_of(3) << 32};
     };
     auto there = [&](const Pages &p) -> uint64_t {   // keys that have one
       if (a.t.shift >= 6) return a.t.there(p.of(0)) ? ~0ull : 0ull;
@@ -461,31 +465,46 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
       return m;
     };
     const int in_page = (1 << a.t.shift) - 1;
-    // element of a pool where run u of block blk begins, in the page of p's run x
-    auto run_at = [&](int blk, const Pages &p, int x, int u) {
-      const int e = p.of(x);
+    // element of a pool where run u of block blk begins
+    auto run_at = [&](int blk, const Pages &p, int u) {
+      const int e = p.of(u);
       return ((((long)a.t.safe(e) * a.KV + kv) << a.t.shift) + ((min(blk, bhi - 1) * kKeyBlock + 16 * u) & in_page)) * HD;
     };
     constexpr int PER = DMAS / SUBS;
     // a lane's bytes of a run's first KB of keys (piece ^ f(row)): those of the i-th KB are 64 i away in an exclusive or
     const int ksrc = lane / PC * (HD * 2) + ((lane % PC) ^ pkey_swz<HD>(lane / PC)) * 16;
-    // keys of the second half of block blk and of the first half of the next one
-    auto fetch_k = [&](int blk, int stage, const Pages &p, const Pages &p_next) {
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u) {
-        const int run = wave * SUBS + u;
-        const bool behind = run > 1;
-        const uint64_t m = 0 - (uint64_t)behind;
-        const uint16_t *src = a.k + run_at(blk + behind, Pages{(p.cd & ~m) | (p_next.ab & m), 0}, run & 1, (run + 2) & 3);
-        dma_run<PER, 64>(src, ksrc, lds_addr(&sm_k[stage][(wave * DMAS + u * PER) * 1024]));
-      }
-      // their 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
-      if (a.mask) dma4(a.mask + (long)b * a.cap + min(blk * kKeyBlock + 32 + (lane & 15) * 4, a.cap - 4), lds_addr(&sm_mask[stage][wave][0]));
+    // What a wave brings of a block, keys and values.
+    struct Source {
+      uint64_t k[SUBS], v[SUBS];
     };
-    auto fetch_v = [&](int blk, int stage, const Pages &p) {
+    auto source_k = [&](Source &src, int blk, const Pages &p) {
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u)
-        dma_run<PER, 0>(a.v + run_at(blk, p, wave * SUBS + u, wave * SUBS + u), lane * 16, lds_addr(&sm_v[stage][(wave * DMAS + u * PER) * 1024]));
+      for (int u = 0; u < SUBS; ++u) src.k[u] = uniform_address(a.k + run_at(blk, p, wave * SUBS + u));
+    };
+    auto source_v = [&](Source &src, int blk, const Pages &p) {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) src.v[u] = uniform_address(a.v + run_at(blk, p, wave * SUBS + u));
+    };
+    // the i-th KB of either
+    auto fetch_k = [&](const Source &src, int stage, auto kb) {
+      constexpr int u = decltype(kb)::value / PER, i = decltype(kb)::value % PER;
+      dma16_at<i * 1024>(src.k[u], ksrc ^ (64 * i), lds_addr(&sm_k[stage][(wave * DMAS + u * PER) * 1024]));
+    };
+    auto fetch_v = [&](const Source &src, int stage, auto kb) {
+      constexpr int u = decltype(kb)::value / PER, i = decltype(kb)::value % PER;
+      dma16_at<i * 1024>(src.v[u], lane * 16, lds_addr(&sm_v[stage][(wave * DMAS + u * PER) * 1024]));
+    };
+    auto each_kb = [&](auto f) {
+      if constexpr (DMAS == 2) f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>());
+      else if constexpr (DMAS == 4)
+        f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>()), f(std::integral_constant<int, 2>()), f(std::integral_constant<int, 3>());
+      else
+        f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>()), f(std::integral_constant<int, 2>()), f(std::integral_constant<int, 3>()),
+        f(std::integral_constant<int, 4>()), f(std::integral_constant<int, 5>()), f(std::integral_constant<int, 6>()), f(std::integral_constant<int, 7>());
+    };
+    // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
+    auto fetch_mask = [&](int blk, int stage) {
+      dma4(a.mask + (long)b * a.cap + min(min(blk, bhi - 1) * kKeyBlock + (lane & 15) * 4, a.cap - 4), lds_addr(&sm_mask[stage][wave][0]));
     };
 
     const int w0 = r0 + 32 * wave, r = w0 + l32, tok = a.by_g(min(r, rows - 1)), head = kv * a.G + min(r, rows - 1) - tok * a.G;
@@ -496,11 +515,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     bf16x8 q[KS];
 #pragma unroll
     for (int i = 0; i < KS; ++i) q[i] = load_q(a.q + at_q + 16 * i + 8 * h, a.flip);
-    Pages pg = pages_of(blo), pg1 = pages_of(blo + 1), pg2 = pages_of(blo + 2);   // of the blocks blk, blk + 1, blk + 2
+    const int e0 = entries_of(blo), e1 = entries_of(blo + 1);
+    int e2 = entries_of(blo + 2);
+    Pages pg = unpack(e0), pg1 = unpack(e1), pg2;   // of the blocks blk, blk + 1, blk + 2
     loads_done();
-    // (of the block before the first one the second half is nobody's: the first block's again)
-    fetch_k(blo - 1, 1, pg, pg);
-    fetch_v(blo, 0, pg);
+    Source src;
+    source_k(src, blo, pg);
+    source_v(src, blo, pg);
+    each_kb([&](auto kb) { fetch_k(src, 0, kb); });
+    if (a.mask) fetch_mask(blo, 0);
+    each_kb([&](auto kb) { fetch_v(src, 0, kb); });
 
     // S^T row x of a half block is key x with bits 2 and 3 of x exchanged
     const int kr = (l32 & 19) | ((l32 >> 2) & 1) << 3 | ((l32 >> 3) & 1) << 2;
@@ -574,17 +598,33 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
       return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
     };
 
-    // Half a block of 32 keys, whose scores are in s: their exponentials beside the products of the next half's
-    // scores, then the products with their values.
+    // A step of 32 keys, whose scores are in s: their exponentials beside the products of the next step's scores
+    // and of the values of the step before, one to each (two at hd 64), so that neither unit waits for the
+    // other.  Operands are read from LDS AHEAD products before their use.
     //
     // Exponents are taken relative to ref, which follows a row's largest score only where the sum of a lane's
     // probabilities shows that it has been left far behind (or where the row has seen no key yet): most
     // steps need not look for their maximum, nor touch O.  Each row's ref follows its own scores alone:
     // another row's may come from keys that are hidden from it.
-    bf16x8 kf[KS], vf[2][DT];         // operands of the step's products, read ahead
-    auto step = [&](auto st, auto second, f32x16 &s, f32x16 &next, int j_next, uint32_t show_next) {
-      constexpr int stage = decltype(st)::value, half = decltype(second)::value;
-      u32x4 p[2];
+    constexpr int SLOTS = KS + 2 * DT, PM = 16 / SLOTS, AHEAD = 4;
+    bf16x8 frag[AHEAD];
+    u32x4 p[2][2];                    // probabilities of the last two steps
+    // the operand of product i: keys of the next step's half (next_half of the block at key stage ks), then values
+    // of the step before (the other half of the block at stage vs)
+    auto operand = [&](int ks, int vs, int half, int i) {
+      return i < KS ? key_frag(ks, half, koff, i) : value_frag(vs, half, (i - KS) / DT, (i - KS) % DT);
+    };
+    auto read_ahead = [&](int ks, int vs, int half) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) frag[i] = operand(ks, vs, half, i);
+    };
+    // half: of the block that the next scores and the last values are of; first: the one behind the barrier, which
+    // loads go with; last: no scores are left; start: no values yet
+    enum { kFirst = 1, kLast = 2, kStart = 4 };
+    auto step = [&](auto key_stage, auto value_stage, auto which, auto kind, f32x16 &s, f32x16 &next, int j_next, uint32_t show_next) {
+      constexpr int ks = decltype(key_stage)::value, vs = decltype(value_stage)::value, half = decltype(which)::value;
+      constexpr int what = decltype(kind)::value;
+      constexpr int parity = half ^ 1;          // of the step itself: the second half's scores follow the first's
       float add = 0.f;
       float y[16];
       auto exps = [&](int from, int to) {
@@ -597,25 +637,51 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
           const bf16x2 w = {(__bf16)y[e], (__bf16)y[e + 1]};
           uint32_t u = __builtin_bit_cast(uint32_t, w);
           asm volatile("" : "+v"(u));   // rounded here: the pairs' registers are needed
-          p[e / 8][e % 8 / 2] = u;
+          p[parity][e / 8][e % 8 / 2] = u;
           add = pair_sum(u, add);
         }
       };
-      constexpr int PM = 16 / KS;       // scores beside each product
 #pragma unroll
       for (int e = 0; e < 16; ++e) next[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], q[i], next, 0, 0, 0);
-        if (half == 0) kf[i] = key_frag(stage, 1, koff, i);
-        if (half == 0 ? i == KS - 1 : i == 0)
-#pragma unroll
-          for (int d = 0; d < DT; ++d) vf[1][d] = value_frag(stage, half, 1, d);
+      auto slot = [&](auto at) {
+        constexpr int i = decltype(at)::value, f = i + AHEAD;
+        if constexpr (i < KS) {
+          if constexpr (!(what & kLast)) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % AHEAD], q[i], next, 0, 0, 0);
+        } else if constexpr (!(what & kStart)) {
+          constexpr int x = i - KS;
+          o[x % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % AHEAD], __builtin_bit_cast(bf16x8, p[parity ^ 1][x / DT]), o[x % DT], 0, 0, 0);
+        }
+        if constexpr (f < SLOTS && !(f < KS ? what & kLast : what & kStart)) frag[f % AHEAD] = operand(ks, vs, half, f);
+        if constexpr (f >= SLOTS && (what & kFirst) && !(what & kLast)) frag[f % AHEAD] = operand(ks, vs, half ^ 1, f - SLOTS);
+        if constexpr ((what & kFirst) && !(what & kLast)) {   // the loads of the blocks to come, which wait for one another, spread out
+          constexpr int per = 2 * DMAS;
+          if constexpr (per <= SLOTS) {
+            if constexpr (i % (SLOTS / per) == 0) {
+              constexpr int x = i / (SLOTS / per);
+              if constexpr (x < DMAS) fetch_k(src, vs, std::integral_constant<int, x>());
+              else fetch_v(src, ks, std::integral_constant<int, x - DMAS>());
+            }
+          } else {
+            static_assert(per == 2 * SLOTS);
+            fetch_k(src, vs, at);
+            fetch_v(src, ks, at);
+          }
+        }
         exps(PM * i, PM * (i + 1));
-        if (i > 0) pack(PM * (i - 1), PM * i);
+        if constexpr (PM == 2) {
+          if constexpr (i > 0) pack(2 * i - 2, 2 * i);
+        } else {
+          if constexpr (i > 0 && i % 2 == 0) pack(i - 2, i);
+        }
         __builtin_amdgcn_sched_barrier(0);
+      };
+      slot(std::integral_constant<int, 0>()), slot(std::integral_constant<int, 1>()), slot(std::integral_constant<int, 2>()), slot(std::integral_constant<int, 3>());
+      slot(std::integral_constant<int, 4>()), slot(std::integral_constant<int, 5>()), slot(std::integral_constant<int, 6>()), slot(std::integral_constant<int, 7>());
+      if constexpr (SLOTS == 16) {
+        slot(std::integral_constant<int, 8>()), slot(std::integral_constant<int, 9>()), slot(std::integral_constant<int, 10>()), slot(std::integral_constant<int, 11>());
+        slot(std::integral_constant<int, 12>()), slot(std::integral_constant<int, 13>()), slot(std::integral_constant<int, 14>()), slot(std::integral_constant<int, 15>());
       }
-      pack(16 - PM, 16);
+      pack(14, 16);
       if (__any(add > limit)) {
         float top = kNegInf;
 #pragma unroll
@@ -634,63 +700,83 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
         pack(0, 16);
       }
       sum += add;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][d], __builtin_bit_cast(bf16x8, p[t]), o[d], 0, 0, 0);
-          if (half == 0 && t == 0) vf[0][d] = value_frag(stage, 1, 0, d);
-        }
-      hide(next, j_next, show_next);
+      if constexpr (!(what & kLast)) hide(next, j_next, show_next);
     };
-    // keys that a block's half steps look at ahead: its second half and the next one's first, by page and mask
-    auto shown_ahead = [&](int stage, const Pages &p, const Pages &p_next) {
-      uint64_t m = there(p) >> 32 | there(p_next) << 32;
+    // a block's keys that have a page and that the mask shows
+    auto shown_of = [&](int stage, const Pages &pages) {
+      uint64_t m = there(pages);
       if (a.mask) m &= __ballot(sm_mask[stage][wave][lane] != 0);
       return m;
     };
+    std::integral_constant<int, 0> zero;
+    std::integral_constant<int, 1> one;
 
-    // the first half block's scores
+    // The first block's scores, and its first step, which has no values to multiply.
     wait_vm<0>();
     lds_barrier();
-    uint32_t show = (uint32_t)(shown_ahead(1, pg, pg) >> 32);   // of the block's first half
+    uint64_t show = shown_of(0, pg);
     if (w0 < rows) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) sa[e] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag(1, 1, koff, i), q[i], sa, 0, 0, 0);
-      hide(sa, blo * kKeyBlock, show);
+      for (int i = 0; i < KS; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag(0, 0, koff, i), q[i], sa, 0, 0, 0);
+      hide(sa, blo * kKeyBlock, (uint32_t)show);
+      read_ahead(0, 0, 1);
+      step(zero, zero, one, std::integral_constant<int, kStart>(), sa, sb, blo * kKeyBlock + 32, (uint32_t)(show >> 32));
     }
-    fetch_k(blo, 0, pg, pg1);
-    auto block = [&](auto st, int blk) {
-      constexpr int stage = decltype(st)::value;
-      const Pages pg3 = pages_of(blk + 3);
+    source_k(src, blo + 1, pg1);
+    each_kb([&](auto kb) { fetch_k(src, 1, kb); });
+    if (a.mask) fetch_mask(blo + 1, 1);
+    // When block blk begins, its values and the keys of the next one have come: the second step of its scores, with
+    // the values of its first half, and the first step of the next block's, with those of its second.
+    auto block = [&](auto st, auto other, auto goes_on, int blk) {
+      constexpr int stage = decltype(st)::value;   // of its values, and of the keys of the block after the next
+      constexpr bool more = decltype(goes_on)::value;
       const bool partly = a.mask || blk * kKeyBlock + kKeyBlock > gall || there(pg) != ~0ull;
       wait_vm<0>();                    // this wave's parts of the blocks; the barrier adds the others', and
       if (partly) clean(stage);
       lds_barrier();                   // every wave has left what the loads below write over
-#pragma unroll
-      for (int i = 0; i < KS; ++i) kf[i] = key_frag(stage, 0, koff, i);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) vf[0][d] = value_frag(stage, 0, 0, d);
-      __builtin_amdgcn_sched_barrier(0);
-      if (blk + 1 < bhi) {
-        fetch_k(blk + 1, stage ^ 1, pg1, pg2);
-        fetch_v(blk + 1, stage ^ 1, pg1);
+      pg2 = unpack(e2);                // (come with the loads waited for above)
+      uint64_t ahead = 0;
+      if (more) {
+        source_k(src, blk + 2, pg2);
+        source_v(src, blk + 1, pg1);
+        e2 = entries_of(blk + 3);
+        ahead = shown_of(stage ^ 1, pg1);
+        if (a.mask) fetch_mask(blk + 2, stage);
       }
-      if (w0 < rows) {                 // (otherwise it only brings its part of the blocks)
-        const uint64_t ahead = shown_ahead(stage, pg, pg1);
-        const int j0 = blk * kKeyBlock;
-        step(st, std::integral_constant<int, 0>(), sa, sb, j0 + 32, (uint32_t)ahead);
-        step(st, std::integral_constant<int, 1>(), sb, sa, j0 + 64, (uint32_t)(ahead >> 32));
-        if (partly) add_odd(blk, stage, (uint64_t)(uint32_t)ahead << 32 | show);
-        show = (uint32_t)(ahead >> 32);
+      if (w0 < rows) {
+        const int j1 = blk * kKeyBlock + kKeyBlock;
+        if constexpr (more) {
+          read_ahead(stage ^ 1, stage, 0);
+          step(other, st, zero, std::integral_constant<int, kFirst>(), sb, sa, j1, (uint32_t)ahead);
+          step(other, st, one, zero, sa, sb, j1 + 32, (uint32_t)(ahead >> 32));
+        } else {
+#pragma unroll
+          for (int i = KS; i < KS + AHEAD; ++i) frag[i % AHEAD] = operand(stage ^ 1, stage, 0, i);
+          step(other, st, zero, std::integral_constant<int, kLast>(), sb, sa, j1, 0u);
+#pragma unroll
+          for (int x = 0; x < 2 * DT; ++x)
+            o[x % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_frag(stage, 1, x / DT, x % DT), __builtin_bit_cast(bf16x8, p[1][x / DT]), o[x % DT], 0, 0, 0);
+        }
+        if (partly) add_odd(blk, stage, show);
+      } else if (more) {               // it only brings its part of the blocks
+        each_kb([&](auto kb) { fetch_k(src, stage, kb); });
+        each_kb([&](auto kb) { fetch_v(src, stage ^ 1, kb); });
       }
-      pg = pg1, pg1 = pg2, pg2 = pg3;
+      show = ahead;
+      pg = pg1, pg1 = pg2;
     };
-    for (int blk = blo; blk < bhi; blk += 2) {
-      block(std::integral_constant<int, 0>(), blk);
-      if (blk + 1 < bhi) block(std::integral_constant<int, 1>(), blk + 1);
+    int blk = blo;
+    for (; blk + 2 < bhi; blk += 2) {
+      block(zero, one, std::true_type(), blk);
+      block(one, zero, std::true_type(), blk + 1);
+    }
+    if (blk + 1 < bhi) {
+      block(zero, one, std::true_type(), blk);
+      block(one, zero, std::false_type(), blk + 1);
+    } else {
+      block(zero, one, std::false_type(), blk);
     }
 
     sum += __shfl_xor(sum, 32);
