@@ -10,9 +10,9 @@
 // stands.  Operands are bfloat16 as the cache stores them.  P is rounded to bfloat16 for the second
 // product (half a step, 2^-8 of each term of a float32 sum whose terms err apart).
 //
-// Probabilities and their sums are held 2^-17 smaller than they are, which their quotient does not
-// show: sums of outputs before the division then stay within float32 for up to 2^9 rows of the
-// largest numbers of bfloat16.
+// Probabilities and their sums are held 2^-25 smaller than they are, which their quotient does not
+// show: there is room for a running reference 2^16 behind a row's largest probability, and sums of
+// outputs before the division still stay within float32 for 2^9 rows of bfloat16's largest numbers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -46,9 +46,8 @@ struct PAttnArgs {
   uint32_t flip;                     // sign bits of a query pair to turn
 };
 
-constexpr float kProbDown = 17.f;    // log2
-
-constexpr float kProbMost = 0x1p-8f; // 2^9 of what is held 2^-17 smaller
+constexpr float kProbDown = 25.f;    // log2
+constexpr float kProbMost = 0x1p-9f; // as they are held: 2^16
 
 __device__ __forceinline__ float output_factor(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
@@ -383,12 +382,12 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 // A wave goes half a block (32 keys) at a time: beside the exponentials of its scores run the products of the
 // next half's scores and of the last half's values, one exponential to a product, so that matrix and
 // vector unit work at the same time (with each kind in a run of its own two waves on a SIMD took the sum of
-// both: 544 us for a prompt of 8192 rows of 28 heads; with the values' products alone in a run 499).  Keys are
+// both: 544 us for a prompt of 8192 rows of 28 heads; with the values' products alone in a run 499; 471 now).  Keys are
 // therefore brought a block ahead of values, and operands are read from LDS four products before their use (eight: the
 // same).  No maximum is looked for (see `step`): a third fewer vector instructions.  Page numbers come by vector
 // loads a block ahead, as a scalar load would have every wait for LDS wait for it.
 //
-// That prompt (0.48 TFLOP) takes 470 to 497 us, 0.97 to 1.02 PFLOP/s, the matrix unit busy for half of its
+// That prompt (0.48 TFLOP) takes 471 us, 1.02 PFLOP/s (of several cards the slowest took 560), the matrix unit busy for half of its
 // cycles, at a clock of 1.86 GHz of 2.4: power holds it there, and cycles saved (a seventh of them since
 // 531 us) came back as a lower clock.  Two row tiles in a wave would halve what LDS delivers for each
 // product, but the compiler keeps no 128 output registers out of the vector unit's way there (650 us).
@@ -603,9 +602,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     // other.  Operands are read from LDS AHEAD products before their use.
     //
     // Exponents are taken relative to ref, which follows a row's largest score only where the sum of a lane's
-    // probabilities shows that it has been left far behind (or where the row has seen no key yet): most
-    // steps need not look for their maximum, nor touch O.  Each row's ref follows its own scores alone:
-    // another row's may come from keys that are hidden from it.
+    // probabilities shows that it has been left 2^16 behind (or where the row has seen no key yet): most
+    // steps need not look for their maximum, nor touch O (2^9: 495 us for the prompt above, 471 now).
+    // Each row's ref follows its own scores alone: another row's may come from keys that are hidden from
+    // it, and would show in how this one's are rounded.
     constexpr int SLOTS = KS + 2 * DT, PM = 16 / SLOTS, AHEAD = 4;
     bf16x8 frag[AHEAD];
     u32x4 p[2][2];                    // probabilities of the last two steps
@@ -682,12 +682,13 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
         slot(std::integral_constant<int, 12>()), slot(std::integral_constant<int, 13>()), slot(std::integral_constant<int, 14>()), slot(std::integral_constant<int, 15>());
       }
       pack(14, 16);
-      if (__any(add > limit)) {
+      if (const uint64_t over = __ballot(add > limit)) {
+        const uint64_t rows_over = over | over << 32 | over >> 32;   // of either half wave
         float top = kNegInf;
 #pragma unroll
         for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[e]), s[e + 1]);
         top = both_halves(top) * a.c;
-        const bool up = top > ref + 4.f;
+        const bool up = __builtin_amdgcn_inverse_ballot_w64(rows_over) && top > ref;
         const float corr = up ? exp2_fast(ref - top) : 1.f;
         ref = up ? top : ref;
         sub = (ref == kNegInf ? 0.f : ref) + kProbDown;

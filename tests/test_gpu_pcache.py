@@ -257,6 +257,30 @@ def test_hidden_bytes_have_no_effect(fc, ctx, heads, n):
         assert torch.isnan(got[0, 1:new[0], :, 0]).all() and not torch.isfinite(got[0, 1:new[0]][..., cols]).any()
 
 
+@pytest.mark.parametrize("heads,n", [("qwen", 4), ("qwen", 9), ("qwen", 16), ("toy", 50), ("wide", 20)])
+def test_later_tokens_do_not_change_how_earlier_ones_are_rounded(fc, ctx, heads, n):
+    """Scores that rise from step to step, and keys of the second half of the tokens that are far larger, or
+    not: the first half's outputs are the same bytes, though they share tiles with rows that see those."""
+    H, kv, hd, _ = HEADS[heads]
+    g = torch.Generator().manual_seed(n)
+    R, held = 32, 100
+    state = fc.PageState.alloc(1, 8, 8)
+    table = fill_table(state, [held + n], R, g)
+    cache = pool(g, state, kv, hd, R, fc)
+    for j in range(held + n):
+        cache.k[table[0][j // R], :, j % R] *= 0.02 * 1.02 ** min(j, 64) if j < 80 else 2.0
+    q = randn(g, 1, n, H, hd)
+    outs = []
+    for large in (1, 40):
+        for j in range(held + n // 2, held + n):
+            cache.k[table[0][j // R], :, j % R] *= large
+        outs.append(torch.zeros_like(q))
+        fc.fc_pcache_attention(ctx, cache, q, ints([held]), None, outs[-1])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][:, :n // 2], outs[1][:, :n // 2])
+    assert not torch.equal(outs[0][:, n // 2:], outs[1][:, n // 2:])
+
+
 @pytest.mark.parametrize("n", [1, 3, 9])
 def test_attention_extreme_numbers(fc, ctx, n):
     """Scores of many orders, and values whose sum leaves float32 where their mean does not."""
