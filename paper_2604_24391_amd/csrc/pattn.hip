@@ -42,6 +42,7 @@ struct PAttnArgs {
   int head_xcds;                     // k_pattn: XCDs of a head, or 0: heads along the grid's other axis
   int row_tiles, stride;             // k_pattn_rows: of a pair; pairs whose pieces take turns
   int *queue, pieces;                // k_pattn_rows: 8 counts of pieces taken behind the first ones, or null
+  int back;                          // and from which one on an XCD takes its pieces from the last one back, or 0
   Quot by_g;                         // division by G
   uint32_t flip;                     // sign bits of a query pair to turn
 };
@@ -803,7 +804,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     }
   };
   if constexpr (!QUEUE) {
-    work(args, blockIdx.x);
+    const int turn = blockIdx.x / 8, last = gridDim.x / 8 - 1;
+    work(args, args.back && turn >= args.back ? 8 * (last - (turn - args.back)) + blockIdx.x % 8 : blockIdx.x);
   } else {
     __shared__ int sm_next;
     int id = blockIdx.x, from = blockIdx.x % 8;
@@ -884,16 +886,22 @@ fc_status run_pattn(fc_ctx *ctx, PAttnArgs &a, hipStream_t st) {
   const long plan = up4(2L * a.B), all_blocks = (a.cap + kKeyBlock - 1) / kKeyBlock;
   long splits = 1, slots = a.B;
   if (many) {
-    // as in run_qattn
-    const long units = pairs * tiles, spread = std::min<long>(ctx->num_cus / units, all_blocks / 4);
-    const long places = 8L / NW * ctx->num_cus;
-    splits = std::min<long>(places / units, all_blocks / 8);
-    a.least = spread >= splits ? 4 : 8;
-    splits = std::max<long>(1, std::max(spread, splits));
-    auto filled = [&](long s) { return (double)(units * s) / ((units * s + places - 1) / places * places); };
-    if (units < places)
-      for (long s = splits + 1; s <= 8 && all_blocks / s >= 16; ++s)
-        if (filled(s) > filled(splits) + 0.1) splits = s;
+    // What a number of splits costs in microseconds, from the capacity, as lengths are on the device: blocks one
+    // after the other, for one wave on a SIMD or two that share it, and the parts, written and read, with
+    // the join's launch.  (A frame of 256 rows over 2176: 43, 31, 27, 30 us with 1, 2, 4, 8 splits, over
+    // 8320: 144, 81, 51, 46; a prompt of 1000: 26 and 35 with 1 and 2.)
+    const long units = pairs * tiles;
+    const double blocks = all_blocks * (HD == 128 ? 1.05 : 0.65), part = padded * HD * 8 / 4.5e6;
+    auto cost = [&](long s) {
+      const double waves = (double)units * s * NW / (4. * ctx->num_cus);
+      return blocks / s * (waves <= 1 ? 1 : 1.25 * std::ceil(waves / 2)) + (s > 1 ? 4 + s * part : 0.);
+    };
+    a.least = 4;
+    for (long places : {4L, 8L}) {       // up to a wave on each SIMD, up to two
+      const long most = std::min<long>(places * ctx->num_cus / NW / units, all_blocks / 4);
+      const long s = std::min<long>(most, std::lround(std::sqrt(blocks * (places == 4 ? 1 : 1.25) / part)));
+      if (s > 1 && cost(s) < cost(splits)) splits = s;
+    }
     splits = std::max<long>(1, std::min<long>(splits, (ws - plan) / (up4(2 * per) + padded * HD)));
   } else {
     slots = ctx->num_cus / a.KV;
@@ -918,8 +926,17 @@ fc_status run_pattn(fc_ctx *ctx, PAttnArgs &a, hipStream_t st) {
     a.pieces = (int)(pairs * tiles * splits);
     a.row_tiles = (int)tiles;
     a.stride = pairs % 8 == 0 ? 8 : pairs % 4 == 0 ? 4 : pairs % 2 == 0 ? 2 : 1;
-    const int once = (HD == 64 ? 3 : 2) * ctx->num_cus / 8 * 8;     // workgroups that run at once
-    if (NW == 4 && !parts && a.B > 1 && a.pieces >= 2 * once && 8 * kQueueStep <= ws) {
+    // A CU gets a second workgroup when each has one: the shortest go to the CUs of the longest (a prompt of
+    // 2048: 50 to 47 us; four of 4096 in 4 heads of 64, whose pairs also begin at once: 79 to 64).
+    const int round = 4 / NW * (ctx->num_cus / 8 * 8);
+    if (splits == 1 && a.pieces % 8 == 0 && a.pieces > round && a.pieces <= 2 * round) {
+      if (pairs % 8 == 0) a.stride = (int)pairs;
+      if (a.stride == pairs) a.back = round / 8;
+    }
+    // workgroups that run at once (without a queue a CU has three at hd 64: 1024 pieces 96 us with and 84, 2048
+    // 152 and 175)
+    const int once = 2 * ctx->num_cus / 8 * 8;
+    if (NW == 4 && !parts && a.B > 1 && a.pieces >= (HD == 64 ? 3 : 2) * once && 8 * kQueueStep <= ws) {
       a.queue = reinterpret_cast<int *>(at);
       hipLaunchKernelGGL(k_pattn_queue, dim3(1), dim3(8), 0, st, a.queue);
       FC_LAUNCH_OK(st, "k_pattn_queue");
