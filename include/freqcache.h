@@ -595,7 +595,7 @@ fc_status fc_qcache_evict(fc_ctx *ctx, const fc_qcache *src, const fc_qcache *ds
                           int32_t *kept, int32_t *len_out, int32_t B, void *stream);
 
 /* Bytes of the state of B items of up to max_pages pages each and a pool of n_pages (0 for counts
- * below 1 and for B max_pages above 2^30).  (host function, no device work) */
+ * below 1 and for B max_pages above 2^28).  (host function, no device work) */
 size_t fc_pcache_state_bytes(int32_t B, int32_t max_pages, int32_t n_pages);
 
 /* An empty state: every table entry -1, no page held.  Stream-ordered. */
@@ -652,8 +652,8 @@ fc_status fc_pcache_attention(fc_ctx *ctx, const fc_pcache *cache, const uint16_
  * are those held, rounded up to a multiple of eight.  Where a
  *            copy finds no page, its item is granted 0, and so is every later one that would
  *            write that page.
- * Uses the context's partial-sum workspace (FC_ERR_CAPACITY when B max_pages + 4 B + 4 n_pages
- * numbers exceed it); allocates nothing. */
+ * Uses the context's partial-sum workspace (FC_ERR_CAPACITY when B (max_pages + 1) + 3 n_pages +
+ * 3 max(B, n_pages) + 8 numbers exceed it); allocates nothing. */
 fc_status fc_pcache_step(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers,
                          const int32_t *src, const int32_t *len, const int32_t *n_new, int32_t n,
                          int32_t *granted, int32_t B, void *stream);

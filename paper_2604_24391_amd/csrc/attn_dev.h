@@ -1,4 +1,4 @@
-// Device code that the attention kernels over token caches share (qattn.hip): the deal of
+// Device code that the attention kernels over token caches share (qattn.hip, pattn.hip): the deal of
 // key blocks over workgroups, what a row sees of a block, loads.
 #pragma once
 

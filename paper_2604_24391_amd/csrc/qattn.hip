@@ -93,7 +93,7 @@ __device__ __forceinline__ float prob(float y, float L) { return y == kNegInf ? 
 // a CU several times what HBM delivers), so loads run ahead: each next block's keys are read when the
 // scores have used theirs, its values after the outputs.  Eight items of 40000 to 65535 rows (433 MB)
 // take 70 us, 6.1 TB/s.  Short shares are bound by latency: sixteen items of 2200 to 4200 rows (54 MB, in
-// the memory-side cache) 16 us, 3.4 TB/s, where a wave has three or four blocks and reads one more that
+// the memory-side cache) 15 us, 3.6 TB/s, where a wave has three or four blocks and reads one more that
 // it does not use; one of 2176 6.5 us, most of it the launch and one pass.  Two tiles (17 to 32 rows)
 // take 366 registers at hd 128, one wave on a SIMD: 4 tokens of those sixteen items 30 us with the join.
 //
