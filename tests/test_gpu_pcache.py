@@ -193,6 +193,21 @@ def test_attention_long_histories(fc, ctx, heads, n, B):
     run_attention(fc, ctx, g, heads, n, 64, [5000 // (b * b + 1) for b in range(B)], None)
 
 
+@pytest.mark.parametrize("heads,n,B", [("toy", 64, 1), ("one", 40, 2), ("wide", 10, 1), ("three", 100, 1)])
+def test_attention_in_many_parts(fc, heads, n, B):
+    """Histories that many rows are split over: tens of parts to a row."""
+    with fc.Context(fc.Caps(max_batch=4, max_height=448, max_width=448, max_tokens=1024, max_seq=4096, max_d_model=2048, max_ffn=8192, max_qkv=4096)) as ctx:
+        run_attention(fc, ctx, torch.Generator().manual_seed(n), heads, n, 64, [9000 // (b + 1) for b in range(B)], None)
+
+
+@pytest.mark.parametrize("heads,n,B,new", [("qwen", 1316, 1, False), ("toy", 40, 160, True), ("group2", 1700, 8, False)])
+def test_attention_up_to_two_workgroups_a_cu(fc, ctx, heads, n, B, new):
+    """Numbers of pieces whose shortest go beside the longest, in one group of pairs and in several."""
+    g = torch.Generator().manual_seed(n)
+    held = [(5 * b) % 90 for b in range(B)]
+    run_attention(fc, ctx, g, heads, n, 64, held, [n - b % 30 for b in range(B)] if new else None)
+
+
 @pytest.mark.parametrize("heads,n", [("qwen", 1), ("toy", 1), ("qwen", 4), ("qwen", 9), ("wide", 30), ("three", 150)])
 def test_hidden_bytes_have_no_effect(fc, ctx, heads, n):
     """NaN and infinities in masked rows, in pages that nobody holds, behind the last row, in the buffers'
