@@ -132,23 +132,38 @@ __device__ __forceinline__ void dma4(const void *gp, uint32_t lds) {
       : "memory");
 }
 
-// 1 KB as dma16, from base + off + AT (base wave-uniform, off in bytes) to lds + AT: an instruction's offset counts
-// on both sides.
-template <int AT>
-__device__ __forceinline__ void dma16_at(uint64_t base, int off, uint32_t lds) {
+// N KB as dma16, the i-th from base + off[i] + 1024 i (base wave-uniform, off in bytes) to lds + 1024 i: an
+// instruction's offset counts on both sides.  One M0 serves them.
+template <int N>
+__device__ __forceinline__ void dma16_run(uint64_t base, const int (&off)[N], uint32_t lds) {
+  static_assert(N == 2 || N == 4);
   uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %3\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, %2 offset:%c4\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(off), "s"(base), "s"(lds), "i"(AT)
-      : "memory");
+  if constexpr (N == 2)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %4\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off[0]), "v"(off[1]), "s"(base), "s"(lds)
+        : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %6\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %5\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds)
+        : "memory");
 }
-__device__ __forceinline__ uint64_t uniform_address(const void *p) {
-  const uint64_t x = (uint64_t)(uintptr_t)p;
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
          (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }

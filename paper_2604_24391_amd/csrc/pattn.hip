@@ -440,67 +440,64 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     // Pages of a block's four runs of 16 rows (blocks behind the last one are read as it).  They are loaded
     // by lanes (0 to 3: a run each) a block before they are looked at: scalar loads would have every
     // wait for LDS wait for them too.
-    // (neither an array nor a choice between members: the compiler would put them into memory for a wave's
-    // number to index)
     struct Pages {
-      uint64_t ab, cd;
-      __device__ int of(int run) const {
-        const uint64_t m = 0 - (uint64_t)(run >> 1 & 1);
-        return (int)(((ab & ~m) | (cd & m)) >> (32 * (run & 1)));
-      }
+      int run[SUBS];                   // those of the runs that this wave brings
+      uint32_t there;                  // the runs that have one
     };
     auto entries_of = [&](int blk) {
       return a.t.entry(b, min((4 * min(blk, bhi - 1) + (lane & 3)) >> (a.t.shift - 4), a.t.width - 1));
     };
     auto unpack = [&](int e) {
-      auto lane_of = [&](int x) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane(e, x); };
-      return Pages{lane_of(0) | lane_of(1) << 32, lane_of(2) | lane_of(3) << 32};
+      Pages p;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) p.run[u] = __builtin_amdgcn_readlane(e, wave * SUBS + u);
+      p.there = (uint32_t)__ballot(a.t.there(e)) & 15;
+      return p;
     };
     auto there = [&](const Pages &p) -> uint64_t {   // keys that have one
-      if (a.t.shift >= 6) return a.t.there(p.of(0)) ? ~0ull : 0ull;
+      if (p.there == 15) return ~0ull;
       uint64_t m = 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        if (a.t.there(p.of(x))) m |= 0xFFFFull << (16 * x);
+        if (p.there >> x & 1) m |= 0xFFFFull << (16 * x);
       return m;
     };
     const int in_page = (1 << a.t.shift) - 1;
-    // element of a pool where run u of block blk begins
+    // bytes from a pool's start to where run u of this wave's of block blk begins
     auto run_at = [&](int blk, const Pages &p, int u) {
-      const int e = p.of(u);
-      return ((((long)a.t.safe(e) * a.KV + kv) << a.t.shift) + ((min(blk, bhi - 1) * kKeyBlock + 16 * u) & in_page)) * HD;
+      const int j = min(blk, bhi - 1) * kKeyBlock + 16 * (wave * SUBS + u);
+      return uniform(((((long)a.t.safe(p.run[u]) * a.KV + kv) << a.t.shift) + (j & in_page)) * (2 * HD));
     };
     constexpr int PER = DMAS / SUBS;
     // a lane's bytes of a run's first KB of keys (piece ^ f(row)): those of the i-th KB are 64 i away in an exclusive or
     const int ksrc = lane / PC * (HD * 2) + ((lane % PC) ^ pkey_swz<HD>(lane / PC)) * 16;
-    // What a wave brings of a block, keys and values.
+    // Where in the pools a wave's runs of a block lie.
     struct Source {
-      uint64_t k[SUBS], v[SUBS];
+      uint64_t at[SUBS];
     };
-    auto source_k = [&](Source &src, int blk, const Pages &p) {
+    auto source = [&](int blk, const Pages &p) {
+      Source s;
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) src.k[u] = uniform_address(a.k + run_at(blk, p, wave * SUBS + u));
+      for (int u = 0; u < SUBS; ++u) s.at[u] = run_at(blk, p, u);
+      return s;
     };
-    auto source_v = [&](Source &src, int blk, const Pages &p) {
+    const uint64_t k_pool = (uint64_t)(uintptr_t)a.k, v_pool = (uint64_t)(uintptr_t)a.v;
+    // the u-th run of either
+    auto fetch_k = [&](const Source &src, int stage, int u) {
+      int off[PER];
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) src.v[u] = uniform_address(a.v + run_at(blk, p, wave * SUBS + u));
+      for (int i = 0; i < PER; ++i) off[i] = ksrc ^ (64 * i);
+      dma16_run<PER>(k_pool + src.at[u], off, lds_addr(&sm_k[stage][(wave * DMAS + u * PER) * 1024]));
     };
-    // the i-th KB of either
-    auto fetch_k = [&](const Source &src, int stage, auto kb) {
-      constexpr int u = decltype(kb)::value / PER, i = decltype(kb)::value % PER;
-      dma16_at<i * 1024>(src.k[u], ksrc ^ (64 * i), lds_addr(&sm_k[stage][(wave * DMAS + u * PER) * 1024]));
+    auto fetch_v = [&](const Source &src, int stage, int u) {
+      int off[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) off[i] = lane * 16;
+      dma16_run<PER>(v_pool + src.at[u], off, lds_addr(&sm_v[stage][(wave * DMAS + u * PER) * 1024]));
     };
-    auto fetch_v = [&](const Source &src, int stage, auto kb) {
-      constexpr int u = decltype(kb)::value / PER, i = decltype(kb)::value % PER;
-      dma16_at<i * 1024>(src.v[u], lane * 16, lds_addr(&sm_v[stage][(wave * DMAS + u * PER) * 1024]));
-    };
-    auto each_kb = [&](auto f) {
-      if constexpr (DMAS == 2) f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>());
-      else if constexpr (DMAS == 4)
-        f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>()), f(std::integral_constant<int, 2>()), f(std::integral_constant<int, 3>());
-      else
-        f(std::integral_constant<int, 0>()), f(std::integral_constant<int, 1>()), f(std::integral_constant<int, 2>()), f(std::integral_constant<int, 3>()),
-        f(std::integral_constant<int, 4>()), f(std::integral_constant<int, 5>()), f(std::integral_constant<int, 6>()), f(std::integral_constant<int, 7>());
+    auto each_run = [&](auto f) {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) f(u);
     };
     // a block's 64 mask bytes for each wave (four times over: a DMA writes 4 bytes for every lane)
     auto fetch_mask = [&](int blk, int stage) {
@@ -519,12 +516,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     int e2 = entries_of(blo + 2);
     Pages pg = unpack(e0), pg1 = unpack(e1), pg2;   // of the blocks blk, blk + 1, blk + 2
     loads_done();
-    Source src;
-    source_k(src, blo, pg);
-    source_v(src, blo, pg);
-    each_kb([&](auto kb) { fetch_k(src, 0, kb); });
+    Source src = source(blo, pg), src1 = source(blo + 1, pg1);   // of the blocks whose values and whose keys come next
+    each_run([&](int u) { fetch_k(src, 0, u); });
     if (a.mask) fetch_mask(blo, 0);
-    each_kb([&](auto kb) { fetch_v(src, 0, kb); });
+    each_run([&](int u) { fetch_v(src, 0, u); });
 
     // S^T row x of a half block is key x with bits 2 and 3 of x exchanged
     const int kr = (l32 & 19) | ((l32 >> 2) & 1) << 3 | ((l32 >> 3) & 1) << 2;
@@ -654,19 +649,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
         }
         if constexpr (f < SLOTS && !(f < KS ? what & kLast : what & kStart)) frag[f % AHEAD] = operand(ks, vs, half, f);
         if constexpr (f >= SLOTS && (what & kFirst) && !(what & kLast)) frag[f % AHEAD] = operand(ks, vs, half ^ 1, f - SLOTS);
-        if constexpr ((what & kFirst) && !(what & kLast)) {   // the loads of the blocks to come, which wait for one another, spread out
-          constexpr int per = 2 * DMAS;
-          if constexpr (per <= SLOTS) {
-            if constexpr (i % (SLOTS / per) == 0) {
-              constexpr int x = i / (SLOTS / per);
-              if constexpr (x < DMAS) fetch_k(src, vs, std::integral_constant<int, x>());
-              else fetch_v(src, ks, std::integral_constant<int, x - DMAS>());
-            }
-          } else {
-            static_assert(per == 2 * SLOTS);
-            fetch_k(src, vs, at);
-            fetch_v(src, ks, at);
-          }
+        if constexpr ((what & kFirst) && !(what & kLast)) {   // the loads of the blocks to come
+          constexpr int apart = SLOTS / (2 * SUBS), x = i / apart;
+          if constexpr (i % apart == 0 && x < SUBS) fetch_k(src1, vs, x);
+          else if constexpr (i % apart == 0 && x < 2 * SUBS) fetch_v(src, ks, x - SUBS);
         }
         exps(PM * i, PM * (i + 1));
         if constexpr (PM == 2) {
@@ -726,8 +712,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
       read_ahead(0, 0, 1);
       step(zero, zero, one, std::integral_constant<int, kStart>(), sa, sb, blo * kKeyBlock + 32, (uint32_t)(show >> 32));
     }
-    source_k(src, blo + 1, pg1);
-    each_kb([&](auto kb) { fetch_k(src, 1, kb); });
+    src = src1;
+    each_run([&](int u) { fetch_k(src, 1, u); });
     if (a.mask) fetch_mask(blo + 1, 1);
     // When block blk begins, its values and the keys of the next one have come: the second step of its scores, with
     // the values of its first half, and the first step of the next block's, with those of its second.
@@ -741,8 +727,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
       pg2 = unpack(e2);                // (come with the loads waited for above)
       uint64_t ahead = 0;
       if (more) {
-        source_k(src, blk + 2, pg2);
-        source_v(src, blk + 1, pg1);
+        src = src1;
+        src1 = source(blk + 2, pg2);
         e2 = entries_of(blk + 3);
         ahead = shown_of(stage ^ 1, pg1);
         if (a.mask) fetch_mask(blk + 2, stage);
@@ -763,8 +749,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
         }
         if (partly) add_odd(blk, stage, show);
       } else if (more) {               // it only brings its part of the blocks
-        each_kb([&](auto kb) { fetch_k(src, stage, kb); });
-        each_kb([&](auto kb) { fetch_v(src, stage ^ 1, kb); });
+        each_run([&](int u) { fetch_k(src1, stage, u); });
+        each_run([&](int u) { fetch_v(src, stage ^ 1, u); });
       }
       show = ahead;
       pg = pg1, pg1 = pg2;
