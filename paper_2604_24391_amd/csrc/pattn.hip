@@ -380,20 +380,22 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 // 165 us before and 114 now, of 1024 397 and 323, ragged 310 and 254; of equal length 312 without queues
 // and 319 with).
 //
-// A wave goes half a block (32 keys) at a time: beside the exponentials of its scores run the products of the
-// next half's scores and of the last half's values, one exponential to a product, so that matrix and
-// vector unit work at the same time (with each kind in a run of its own two waves on a SIMD took the sum of
-// both: 544 us for a prompt of 8192 rows of 28 heads; with the values' products alone in a run 499; 471 now).  Keys are
-// therefore brought a block ahead of values, and operands are read from LDS four products before their use (eight: the
-// same).  No maximum is looked for (see `step`): a third fewer vector instructions.  Page numbers come by vector
-// loads a block ahead, as a scalar load would have every wait for LDS wait for it.
+// A wave goes half a block (32 keys) at a time: beside the exponentials of its scores run the products
+// of the next half's scores and of the last half's values, one exponential to a product, so that matrix
+// and vector unit work at the same time (with each kind in a run of its own two waves on a SIMD took
+// the sum of both: 544 us for a prompt of 8192 rows of 28 heads; with the values' products alone in a
+// run 499; 457 now).  Keys are therefore brought a block ahead of values, and operands are read from
+// LDS four products before their use (eight: the same).  No maximum is looked for (see `step`): a third
+// fewer vector instructions.  Page numbers come by vector loads a block ahead, as a scalar load would
+// have every wait for LDS wait for it.
 //
-// That prompt (0.48 TFLOP) takes 471 us, 1.02 PFLOP/s (of several cards the slowest took 560), the matrix unit busy for half of its
-// cycles, at a clock of 1.86 GHz of 2.4: power holds it there, and cycles saved (a seventh of them since
-// 531 us) came back as a lower clock.  Two row tiles in a wave would halve what LDS delivers for each
-// product, but the compiler keeps no 128 output registers out of the vector unit's way there (650 us).
-// 256 tokens over 2176 rows: 23 us, eight or nine blocks one after the other on 224 workgroups, and their
-// start and end.
+// That prompt (0.48 TFLOP) takes 435 to 457 us, 1.05 to 1.1 PFLOP/s, the matrix unit busy for 57 % of
+// its cycles, at a clock of 1.73 GHz of 2.4: power holds it there, and cycles saved come back in part
+// as a lower clock (893 to 812 thousand: 1.82 to 1.73 GHz).  A run's loads share one asm block and its
+// address serves keys and values: 457 to 443 us on one card, as scalar instructions take turns with the
+// others.  Two row tiles in a wave would halve what LDS delivers for each product, but the compiler
+// keeps no 128 output registers out of the vector unit's way there (650 us). 256 tokens over 2176 rows:
+// 21 us, eight or nine blocks one after the other on 224 workgroups, and their start and end.
 //
 // A row of keys is 16-byte pieces, stored at piece ^ f(row) so that the 16 lanes that a read serves
 // together (0-3, 12-15, 20-23, 24-27 and the other 16 of each half) fall on different banks; columns of
@@ -599,7 +601,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_pattn_rows(PAttnAr
     //
     // Exponents are taken relative to ref, which follows a row's largest score only where the sum of a lane's
     // probabilities shows that it has been left 2^16 behind (or where the row has seen no key yet): most
-    // steps need not look for their maximum, nor touch O (2^9: 495 us for the prompt above, 471 now).
+    // steps need not look for their maximum, nor touch O (2^9: 495 us for the prompt above, 471 so).
     // Each row's ref follows its own scores alone: another row's may come from keys that are hidden from
     // it, and would show in how this one's are rounded.
     constexpr int SLOTS = KS + 2 * DT, PM = 16 / SLOTS, AHEAD = 4;
