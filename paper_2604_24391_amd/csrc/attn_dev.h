@@ -144,10 +144,10 @@ __device__ __forceinline__ void dma16_run(uint64_t base, const int (&off)[N], ui
         "s_mov_b32 m0, %4\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:%c5\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(off[0]), "v"(off[1]), "s"(base), "s"(lds)
+        : "v"(off[0]), "v"(off[1]), "s"(base), "s"(lds), "i"(1024)
         : "memory");
   else
     asm volatile(
@@ -155,12 +155,12 @@ __device__ __forceinline__ void dma16_run(uint64_t base, const int (&off)[N], ui
         "s_mov_b32 m0, %6\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:%c7\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2 * %c7\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3 * %c7\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds)
+        : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds), "i"(1024)
         : "memory");
 }
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
