@@ -1157,8 +1157,9 @@ class PCache:
         """The keys (or values) of an item's table entries, in order: [n_kv, capacity, head_dim], 0
         where there is no page."""
         t = self.pages.table[item]
-        x = (self.v.transpose(-1, -2).reshape(self.k.shape) if values else self.k)[t.clamp(min=0).long()]
-        return torch.where((t >= 0)[:, None, None, None], x, 0).transpose(0, 1).flatten(1, 2)
+        there = (t >= 0) & (t < self.k.shape[0])
+        x = (self.v.transpose(-1, -2).reshape(self.k.shape) if values else self.k)[torch.where(there, t, 0).long()]
+        return torch.where(there[:, None, None, None], x, 0).transpose(0, 1).flatten(1, 2)
 
 
 def _page_args(dev: int, cache: PCache, x: torch.Tensor, name: str):

@@ -73,3 +73,25 @@ def test_handle_checks(fc):
 
 def test_state_bytes(fc):
     assert fc.pcache_state_bytes(3, 3, 5) == 68 and fc.pcache_state_bytes(0, 3, 5) == 0
+
+
+@pytest.fixture
+def on_cpu(fc, monkeypatch):
+    """Handles over CPU tensors: the check that refuses them is left out."""
+    monkeypatch.setattr(fc.freqcache, "_ptr", lambda t, dtype, numel, name: t.data_ptr())
+
+
+def test_rows_of_a_table_with_entries_that_are_no_page(fc, on_cpu):
+    """Entries below 0 and beyond the pool stand for no page: their rows are 0."""
+    n_kv, R, hd, P = 2, 16, 64, 5
+    state = fc.PageState.alloc(2, 4, P, device="cpu")
+    c = fc.PCache.alloc(state, n_kv, hd, R)
+    g = torch.Generator().manual_seed(1)
+    for t in (c.k, c.v):
+        t.copy_(torch.randn(t.shape, generator=g))
+    state.table.copy_(torch.tensor([[3, P, -7, P - 1], [2 ** 31 - 1, -2 ** 31, 0, 77]], dtype=torch.int32))
+    by_rows = c.v.transpose(-1, -2).reshape(c.k.shape)
+    for b, row in enumerate([[3, None, None, P - 1], [None, None, 0, None]]):
+        for pool, values in ((c.k, False), (by_rows, True)):
+            want = torch.cat([torch.zeros(n_kv, R, hd, dtype=torch.bfloat16) if p is None else pool[p] for p in row], 1)
+            assert torch.equal(c.rows(b, values), want)
