@@ -1149,7 +1149,7 @@ class PCache:
                 _ptr(t, _BF16, P * kv * rows * hd, name)
             _ptr(self.pages.state, _INT32, pcache_state_bytes(self.pages.B, self.pages.max_pages, P) // 4, "state")
             c = fc_pcache(*p, kv, hd, rows, P, self.pages.max_pages)
-            for name, x in (("_c", (p, c)), ("_raw", bytes(c)), ("_kp", p[0]), ("_vp", p[1])):
+            for name, x in (("_c", (p, c)), ("_raw", bytes(c)), ("_kp", p[0]), ("_vp", p[1]), ("_sp", p[2])):
                 object.__setattr__(self, name, x)
         return self._c[1]
 
@@ -1209,7 +1209,8 @@ def fc_pcache_attention(ctx: Context, cache: PCache, q: torch.Tensor, lens: torc
 
 
 _data_ptr = torch.Tensor.data_ptr
-_pc_k, _pc_v, _pc_kp, _pc_vp, _pc_raw, _pc_pages = map(operator.attrgetter, ("k", "v", "_kp", "_vp", "_raw", "pages"))
+_pc_k, _pc_v, _pc_kp, _pc_vp, _pc_sp, _pc_raw, _pc_pages = map(
+    operator.attrgetter, ("k", "v", "_kp", "_vp", "_sp", "_raw", "pages"))
 
 
 def _pcaches(dev: int, caches):
@@ -1221,7 +1222,7 @@ def _pcaches(dev: int, caches):
     n, pages = len(caches), caches[0].pages
     if not (list(map(_data_ptr, map(_pc_k, caches))) == list(map(_pc_kp, caches))
             and list(map(_data_ptr, map(_pc_v, caches))) == list(map(_pc_vp, caches))
-            and list(map(_pc_pages, caches)).count(pages) == n and caches[0]._c[0][2] == pages.state.data_ptr()
+            and list(map(_pc_pages, caches)).count(pages) == n and list(map(_pc_sp, caches)).count(pages.state.data_ptr()) == n
             and pages.state.get_device() == dev):
         for c in caches:
             if c.pages.state is not pages.state or c.pages.B != pages.B or c.k.get_device() != dev:

@@ -95,3 +95,20 @@ def test_rows_of_a_table_with_entries_that_are_no_page(fc, on_cpu):
         for pool, values in ((c.k, False), (by_rows, True)):
             want = torch.cat([torch.zeros(n_kv, R, hd, dtype=torch.bfloat16) if p is None else pool[p] for p in row], 1)
             assert torch.equal(c.rows(b, values), want)
+
+
+def test_layers_descriptors_after_the_state_has_moved(fc, on_cpu):
+    """Every layer's descriptor names the state's memory, also where a call on one layer alone has renewed its own."""
+    state = fc.PageState.alloc(2, 4, 9, device="cpu")
+    caches = [fc.PCache.alloc(state, 1, 64, 16) for _ in range(3)]
+    size = ctypes.sizeof(fc.freqcache.fc_pcache)
+
+    def states():
+        raw, n, pages = fc.freqcache._pcaches(-1, caches)      # (-1: a CPU tensor's device)
+        assert n == 3 and pages is state
+        return {fc.freqcache.fc_pcache.from_buffer_copy(raw, size * i).state for i in range(n)}
+    assert states() == {state.state.data_ptr()}
+    for renewed in (0, 2):
+        state.state.set_(state.state.clone())
+        caches[renewed].c()
+        assert states() == {state.state.data_ptr()}
