@@ -658,9 +658,10 @@ fc_status fc_pcache_step(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers,
                          const int32_t *src, const int32_t *len, const int32_t *n_new, int32_t n,
                          int32_t *granted, int32_t B, void *stream);
 
-/* Live pages (those with holders, L of them) moved to the numbers below L, in every layer: the
- * k-th live page from number L on goes to the k-th free page below it; the table and the holders
- * follow, and *live (device, may be NULL) receives L.  Pages from L on are then free, and their
+/* Live pages (those that table entries name, L of them) moved to the numbers below L, in every
+ * layer: the k-th live page from number L on goes to the k-th free page below it; the table follows
+ * (entries that are no page stay as they are), the holders are counted anew, and *live (device, may
+ * be NULL) receives L.  Pages from L on are then free, and their
  * memory can be given to something else.  Limits as for fc_pcache_step. */
 fc_status fc_pcache_compact(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers, int32_t *live,
                             int32_t B, void *stream);

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kPThreads) void k_pappend(PAppendArgs a) {
 
 // ------------------------------------------------------------------------------- pages
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr int kPlanPages = 7168;              // pages whose counts a plan holds in LDS: 8 bytes each, 56 KB
+constexpr int kPlanPages = 7168;              // pages whose counts a plan holds in LDS: up to 8 bytes each, 56 KB
 
 // Rows that a plan has copied or moved: a tile is eight rows of one head.
 struct PageMove {
@@ -153,7 +153,7 @@ struct PlanWs {
   int *table;                                 // the table before it is written: [B][width]
   int *need;                                  // [B] pages of the items before this one
   int *free;                                  // the pages given out; compact: where a page goes
-  int *holders, *last;                        // [pages] where they do not fit into LDS
+  int *holders, *last;                        // [pages] where they do not fit into LDS (compact: no last)
 };
 
 struct StepArgs {
@@ -318,16 +318,26 @@ struct CompactArgs {
   int B, width, pages, shift;
 };
 
-// As k_pstep: 3.6 us for a pool of 33 pages, 4.6 for 280.
+// As k_pstep.  Holders are counted anew here too, so that a page that the table names is never written over:
+// what they were before may be older than the table.
+template <bool LDS>
 __global__ __launch_bounds__(kPlanThreads) void k_pcompact(CompactArgs a) {
+  extern __shared__ int sm[];
   __shared__ int wsum[kPlanWaves];
   const int tid = threadIdx.x;
-  int *table = a.state, *holders = a.state + table_numbers(a.B, a.width);
+  int *table = a.state, *holders_out = a.state + table_numbers(a.B, a.width);
+  int *holders = LDS ? sm : a.ws.holders;
   const int size = a.B * a.width;
   int mine = 0, L;
+  for (int p = tid; p < a.pages; p += kPlanThreads) holders[p] = 0;
+  __syncthreads();
+  for (int x = tid; x < size; x += kPlanThreads) {
+    const int p = table[x];
+    if ((unsigned)p < (unsigned)a.pages) atomicAdd(&holders[p], 1);
+  }
+  __syncthreads();
   for (int p = tid; p < a.pages; p += kPlanThreads) mine += holders[p] > 0;
   plan_scan(mine, wsum, L);
-  for (int p = L + tid; p < a.pages; p += kPlanThreads) a.ws.free[p] = -1;
   // both ends of the k-th move; as many live pages lie behind the end as free ones before it
   int low = 0, high = 0;
   for (int p0 = 0; p0 < a.pages; p0 += kPlanThreads) {
@@ -354,11 +364,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_pcompact(CompactArgs a) {
     holders[mv.from] = 0;
   }
   __syncthreads();
-  // every live page from L on has moved; an entry whose page has no holder names none now
+  // every page from L on that an entry names has moved
   for (int x = tid; x < size; x += kPlanThreads) {
     const int p = table[x];
     if (p >= L && p < a.pages) table[x] = a.ws.free[p];
   }
+  for (int p = tid; p < a.pages; p += kPlanThreads) holders_out[p] = holders[p];
   if (tid == 0) {
     *a.ws.count = high;
     if (a.live) *a.live = L;
@@ -505,7 +516,10 @@ fc_status launch_pcache_compact(fc_ctx *ctx, const fc_pcache *c, int n_layers, i
   a.B = B, a.width = c->max_pages, a.pages = c->n_pages, a.shift = log2_of(c->page_rows);
   {
     ProfScope ps(ctx, st, "fc_pcompact");
-    hipLaunchKernelGGL(k_pcompact, dim3(1), dim3(kPlanThreads), 0, st, a);
+    if (c->n_pages <= kPlanPages)
+      hipLaunchKernelGGL(k_pcompact<true>, dim3(1), dim3(kPlanThreads), c->n_pages * sizeof(int), st, a);
+    else
+      hipLaunchKernelGGL(k_pcompact<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
     FC_LAUNCH_OK(st, "k_pcompact");
   }
   ProfScope ps(ctx, st, "fc_pcompact_move");
