@@ -618,14 +618,18 @@ fc_status fc_pcache_append(fc_ctx *ctx, const fc_pcache *cache, const fc_rope_ax
  * a key_mask, key_mask[b][j] not 0.  One token, a chunk or a whole prompt; the work is split over
  * the keys where there are few rows.
  *   q, out:   [B][n][n_heads][head_dim] bf16; out is softmax(scale q k) v, its probabilities
- *             rounded to bf16 before the product with v (their sum not); a token that sees no row
- *             gets 0; tokens from n_new[b] on are left as they are; no other buffer overlaps out;
+ *             rounded to bf16 before the product with v.  What divides it is their sum before that
+ *             rounding in calls of up to 32 rows of a key-value head (n n_heads / n_kv), and after it
+ *             in calls of more.  A token that sees no row gets 0; tokens from n_new[b] on are left as
+ *             they are; no other buffer overlaps out;
  *   key_mask: [B][max_pages page_rows] uint8 (16-byte aligned), or NULL: every row is seen;
  *   scale:    finite, usually 1 / sqrt(head_dim).
  * What is hidden from a token has no effect on it, whatever its bytes.  Outputs are summed in
  * float32, which holds every mean of finite numbers while the rows that a token sees times the
- * largest of their values are below 2^137; a probability below 2^-100 of the token's largest may
- * count as 0.  The output of a token that sees a value that is not finite is not finite there.
+ * largest of their values are below 2^137; at its lower end an output may lose 2^-100 for each row
+ * that the token sees.  A probability below 2^-100 of the token's largest may count as 0.  The output
+ * of a token that sees a value that is not finite is not finite there, and nowhere where one of its
+ * scores lies above float32 or is NaN.
  * The partial results use the context's partial-sum workspace: fewer splits where it is small.
  * FC_ERR_UNSUPPORTED, before anything is launched, for more than 65535 heads, 2^30 rows (tokens
  * times heads) an item, or 2^24 workgroups (one for each 128 rows of each item's key-value heads
@@ -649,9 +653,8 @@ fc_status fc_pcache_attention(fc_ctx *ctx, const fc_pcache *cache, const uint16_
  * free ones of lowest number, given to the items in order, first for a copy, then behind the kept
  * rows.  A partly filled last page that several table entries hold is copied, in every layer, for
  * each item about to write it, but for the last one where all its holders write: the copy's rows
- * are those held, rounded up to a multiple of eight.  Where a
- *            copy finds no page, its item is granted 0, and so is every later one that would
- *            write that page.
+ * are those held, rounded up to a multiple of eight.  Where a copy finds no page, its item is
+ * granted 0, and so is every later one that would write that page.
  * Uses the context's partial-sum workspace (FC_ERR_CAPACITY when B (max_pages + 1) + 3 n_pages +
  * 3 max(B, n_pages) + 8 numbers exceed it); allocates nothing. */
 fc_status fc_pcache_step(fc_ctx *ctx, const fc_pcache *caches, int32_t n_layers,

@@ -8,11 +8,14 @@
 // query row and its softmax is per-lane scalars; the rows of an S^T tile are permuted so that a
 // lane's probabilities are those of neighbouring keys, the B operand of the second product as it
 // stands.  Operands are bfloat16 as the cache stores them.  P is rounded to bfloat16 for the second
-// product (half a step, 2^-8 of each term of a float32 sum whose terms err apart).
+// product (half a step, 2^-8 of each term of a float32 sum whose terms err apart).  k_pattn divides by the
+// sum of unrounded ones, k_pattn_rows by that of rounded ones, which it adds up in pairs.
 //
 // Probabilities and their sums are held 2^-25 smaller than they are, which their quotient does not
 // show: there is room for a running reference 2^16 behind a row's largest probability, and sums of
 // outputs before the division still stay within float32 for 2^9 rows of bfloat16's largest numbers.
+// At the other end a product or a sum below 2^-126 may be lost: for each key seen up to 2^-125 of a sum that is
+// divided by 2^-25 or more, 2^-100 of an output.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
