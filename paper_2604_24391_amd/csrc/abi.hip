@@ -945,6 +945,7 @@ static fc_status check_pcache(fc_ctx *ctx, const fc_pcache *c, int B, const char
   if (B < 1 || c->n_kv_heads < 1 || (long)B * c->n_kv_heads > 65535)
     return fail(FC_ERR_SHAPE, "%s: B=%d items of %d key-value heads (B n_kv from 1 to 65535)", who, B,
                 c->n_kv_heads);
+  // (the attention's deal of blocks counts them in 32 bits: share_of)
   if ((long)B * c->max_pages > (1L << 28) || (long)B * c->max_pages * c->page_rows > (1L << 36))
     return fail(FC_ERR_UNSUPPORTED, "%s: a table of %d x %d pages (at most 2^28, of 2^36 rows)", who, B, c->max_pages);
   if ((long)c->n_pages * c->n_kv_heads > (1L << 41) / c->page_rows / c->head_dim)

@@ -83,7 +83,10 @@ __device__ __forceinline__ Share share_of(const A &a, int slot) {
     const int n = __builtin_amdgcn_readfirstlane(x), per = max(4, (n + a.slots - 1) / a.slots), used = (n + per - 1) / per;
     return Share{slot < used ? 0 : -1, 0, used, per, __builtin_amdgcn_readfirstlane(held), __builtin_amdgcn_readfirstlane(m)};
   }
-  // (counts below 2^30: a cache of 2^42 bytes is the largest there is)
+  // The calls' checks hold an 8-bit cache of heads of 64 dims and more to 2^42 bytes and a paged cache's table
+  // to 2^36 rows, whatever its pool, so all items hold up to 2^36 rows: 2^30 blocks, and one more for
+  // each of up to 65535 items (a paged capacity is a multiple of 16).  With at least three slots for two
+  // items, all + slots and lo + hi stay below 2^31.
   auto slots_of = [&](int per) {      // per 0: the blocks themselves
     int all = 0;
     for (int i = 0; i < a.B; i += 64) {

@@ -392,9 +392,10 @@ __global__ __launch_bounds__(256) void k_pattn_join(PAttnArgs a) {
 // fewer vector instructions.  Page numbers come by vector loads a block ahead, as a scalar load would
 // have every wait for LDS wait for it.
 //
-// That prompt (0.48 TFLOP) takes 435 to 457 us, 1.05 to 1.1 PFLOP/s, the matrix unit busy for 57 % of
-// its cycles, at a clock of 1.73 GHz of 2.4: power holds it there, and cycles saved come back in part
-// as a lower clock (893 to 812 thousand: 1.82 to 1.73 GHz).  A run's loads share one asm block and its
+// That prompt (0.48 TFLOP) takes 435 to 457 us back to back, 1.05 to 1.1 PFLOP/s.  Counted, at 470 us a
+// launch, it has 812 thousand cycles, a clock of 1.73 GHz of 2.4, and the matrix unit busy for 57 % of
+// them: power holds the clock there, and cycles saved come back in part as a lower one (from 893
+// thousand at 1.82 GHz).  A run's loads share one asm block and its
 // address serves keys and values: 457 to 443 us on one card, as scalar instructions take turns with the
 // others.  Two row tiles in a wave would halve what LDS delivers for each product, but the compiler
 // keeps no 128 output registers out of the vector unit's way there (650 us). 256 tokens over 2176 rows:
