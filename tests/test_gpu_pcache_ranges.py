@@ -63,6 +63,25 @@ def test_steps_over_more_layers_than_one_launch_takes(fc, ctx):  # noqa: F811
     assert compact(fc, ctx, caches) > 0
 
 
+def test_a_state_whose_memory_has_moved(fc, ctx):  # noqa: F811
+    """Calls over all layers after calls on one of them, and the rows of a table with entries that are no page."""
+    g = torch.Generator().manual_seed(4)
+    state = fc.PageState.alloc(2, 4, 9)
+    caches = [pool(g, state, 2, 64, 16, fc) for _ in range(3)]
+    for one in (0, 2):
+        state.state.set_(state.state.clone())
+        fc.fc_pcache_init(ctx, caches[one])
+        assert run_step(fc, ctx, caches, None, [0, 0], [30, 20], 64) == [30, 20]
+        run_step(fc, ctx, caches, [0, 0], [30, 30], [5, 5], 5)
+        compact(fc, ctx, caches)
+    state.table[0, 1], state.table[1, 0], state.table[1, 3] = 9, 2 ** 31 - 1, -2 ** 31
+    for b in range(2):
+        k, v, there = item_rows(caches[1], b)
+        assert not there.all()
+        for x, values in ((k, False), (v, True)):
+            np.testing.assert_array_equal(f64(caches[1].rows(b, values)), np.where(there[:, None], x, 0))
+
+
 # ------------------------------------------------------------------------------ few rows
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("heads,n", [("qwen", 1), ("qwen", 2), ("toy", 1), ("toy", 4)])
